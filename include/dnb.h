@@ -458,6 +458,51 @@ int dnb_op_maxpool3s2_bnrelu(const void* s, const void* fold, void* out, void* p
 int dnb_op_maxpool3s2_backward(const void* dout, const void* pos, void* din, int64_t n, int64_t h, int64_t w, int64_t c,
                                void* stream);
 
+/* ------------------------------------------------------------------------------------------
+ * Sequence operators: attention over packed sequences, rotary positions, the norms around a block, and
+ * the clipping of many gradients by their global norm.  Types: DNB_F32 or DNB_BF16 for the tensors named
+ * "of the type"; sums, statistics and softmax are fp32 in both.  Pointers, streams and errors as above;
+ * tensors of the type are 16-byte aligned.  No call allocates device memory, copies to the host or
+ * synchronises; all of them may be captured into a graph.
+ *
+ * Attention over packed sequences: for sequence s, head h and query i of nq (query rows
+ * q_offsets[s] .. q_offsets[s+1] - 1), with the nk keys and values from row k_offsets[s] on,
+ *   out_i = sum_j softmax_j(scale q_i . k_j) v_j        lse_i = log sum_j exp(scale q_i . k_j)
+ * over all j, or with `causal` over j <= i + nk - nq (the last query sees the last key).  nk is
+ * k_offsets[s+1] - k_offsets[s], or k_lengths[s] if k_lengths is given: then the rows up to the next
+ * offset are room of a cache that is not in use yet, and what they hold does not matter.  Head h reads
+ * key/value head h / (heads / kv_heads).  A query that sees no key has out 0, lse -inf and gradient 0.
+ *   q, out, dout, dq (rows_q, heads, head_dim); k, v, dk, dv (rows_k, kv_heads, head_dim): of the type.
+ *   lse (heads, rows_q) fp32.  q_offsets, k_offsets: sequences + 1 int32 on the device, not decreasing;
+ *   k_lengths: `sequences` int32 on the device or null.  Rows of no sequence are neither read nor
+ *   written; dk and dv of rows that are not in use yet are zero.  Offsets that leave the tensors are cut
+ *   to them, and offsets that decrease give undefined values in the outputs, but no access outside.
+ * A value that is infinite or NaN in a key or value reaches the queries that see it, and may reach those
+ * of the same sequence that a causal mask keeps from it. */
+typedef struct dnb_attn dnb_attn; /* opaque, host side only */
+typedef struct {
+  int32_t heads, kv_heads;  /* heads a multiple of kv_heads                                      */
+  int32_t head_dim;         /* a multiple of 8 up to 128 (else DNB_E_UNSUPPORTED)                */
+  int32_t sequences;        /* >= 1                                                              */
+  int64_t rows_q, rows_k;   /* rows of the tensors; 0 is allowed                                 */
+  int64_t q_stride;         /* elements between rows of q and dq, k and dk, v and dv; 0: dense.  */
+  int64_t k_stride;         /* Multiples of 16 bytes, at most 2^22; out and dout are dense, so   */
+  int64_t v_stride;         /* q, k and v may lie side by side in the rows of one product        */
+  int32_t dtype;            /* DNB_F32 | DNB_BF16                                                */
+  int32_t causal;
+  float scale;              /* 0: 1 / sqrt(head_dim)                                             */
+} dnb_attn_desc;
+int dnb_attn_create(const dnb_attn_desc* desc, dnb_attn** out);
+void dnb_attn_destroy(dnb_attn* plan);
+/* Scratch of either call below (16-byte aligned).  Nothing in it lasts from one call to the next. */
+size_t dnb_attn_workspace_bytes(const dnb_attn* plan);
+int dnb_attn_forward(const dnb_attn* plan, const void* q, const void* k, const void* v, const int32_t* q_offsets,
+                     const int32_t* k_offsets, const int32_t* k_lengths, void* out, float* lse, void* workspace, void* stream);
+/* out and lse are the forward's. */
+int dnb_attn_backward(const dnb_attn* plan, const void* q, const void* k, const void* v, const void* out, const float* lse,
+                      const void* dout, const int32_t* q_offsets, const int32_t* k_offsets, const int32_t* k_lengths, void* dq,
+                      void* dk, void* dv, void* workspace, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

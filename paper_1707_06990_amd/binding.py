@@ -38,6 +38,12 @@ class dnb_inet_desc(C.Structure):
                 ("classes", C.c_int32), ("schedule", C.c_int32), ("eps", C.c_float)]
 
 
+class dnb_attn_desc(C.Structure):
+    _fields_ = [("heads", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("sequences", C.c_int32),
+                ("rows_q", C.c_int64), ("rows_k", C.c_int64), ("q_stride", C.c_int64), ("k_stride", C.c_int64),
+                ("v_stride", C.c_int64), ("dtype", C.c_int32), ("causal", C.c_int32), ("scale", C.c_float)]
+
+
 class dnb_block_memory(C.Structure):
     _fields_ = [(n, C.c_uint64) for n in ("stored_fwd_bytes", "shared_fwd_bytes", "grad_bytes", "peak_bytes",
                                            "stats_bytes", "scratch_bytes", "workspace_bytes")]
@@ -129,6 +135,11 @@ _SIGS = {
     "dnb_op_stem_wgrad7": (C.c_int, [_vp, _vp, _vp, _i64, _i64, _i64, _vp, _vp]),
     "dnb_op_maxpool3s2_bnrelu": (C.c_int, [_vp, _vp, _vp, _vp, _i64, _i64, _i64, _i64, _vp]),
     "dnb_op_maxpool3s2_backward": (C.c_int, [_vp, _vp, _vp, _i64, _i64, _i64, _i64, _vp]),
+    "dnb_attn_create": (C.c_int, [C.POINTER(dnb_attn_desc), C.POINTER(_vp)]),
+    "dnb_attn_destroy": (None, [_vp]),
+    "dnb_attn_workspace_bytes": (_sz, [_vp]),
+    "dnb_attn_forward": (C.c_int, [_vp] * 11),
+    "dnb_attn_backward": (C.c_int, [_vp] * 15),
 }
 for _name, (_res, _args) in _SIGS.items():
     _f = getattr(_lib, _name)
@@ -516,3 +527,34 @@ def dnb_op_maxpool3s2_bnrelu(s, fold, out, pos, n, h, w, c, stream=None) -> None
 
 def dnb_op_maxpool3s2_backward(dout, pos, din, n, h, w, c, stream=None) -> None:
     _check(_lib.dnb_op_maxpool3s2_backward(_ptr(dout), _ptr(pos), _ptr(din), n, h, w, c, _stream(stream)))
+
+
+# ---------------------------------------------------------------- sequence operators
+
+def dnb_attn_create(heads, kv_heads, head_dim, sequences, rows_q, rows_k, dtype=DNB_BF16, causal=True, scale=0.0,
+                    q_stride=0, k_stride=0, v_stride=0):
+    desc = dnb_attn_desc(heads, kv_heads, head_dim, sequences, rows_q, rows_k, q_stride, k_stride, v_stride, dtype,
+                         int(bool(causal)), scale)
+    out = _vp()
+    _check(_lib.dnb_attn_create(C.byref(desc), C.byref(out)))
+    return out
+
+
+def dnb_attn_destroy(plan) -> None:
+    _lib.dnb_attn_destroy(plan)
+
+
+def dnb_attn_workspace_bytes(plan) -> int:
+    return int(_lib.dnb_attn_workspace_bytes(plan))
+
+
+def dnb_attn_forward(plan, q, k, v, q_offsets, k_offsets, k_lengths, out, lse, workspace, stream=None) -> None:
+    _check(_lib.dnb_attn_forward(plan, _ptr(q), _ptr(k), _ptr(v), _ptr(q_offsets), _ptr(k_offsets), _ptr(k_lengths),
+                                 _ptr(out), _ptr(lse), _ptr(workspace), _stream(stream)))
+
+
+def dnb_attn_backward(plan, q, k, v, out, lse, dout, q_offsets, k_offsets, k_lengths, dq, dk, dv, workspace,
+                      stream=None) -> None:
+    _check(_lib.dnb_attn_backward(plan, _ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(lse), _ptr(dout), _ptr(q_offsets),
+                                  _ptr(k_offsets), _ptr(k_lengths), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(workspace),
+                                  _stream(stream)))

@@ -1,0 +1,453 @@
+// Attention over packed sequences, forward: softmax(scale q k^T) v for each sequence and head, with
+// grouped key/value heads and a causal mask whose last query sees the last key.
+//
+// k_attn: a wave keeps 32 rows and walks over the keys in tiles that the workgroup's four waves share.
+// With grouped heads the `per` query heads of a key/value head are rows of one matrix ("packed rows":
+// packed row m is query m / per, head m % per of the group), so a tile of keys serves all of them.
+// One pass over the keys, with the running maximum and sum of the softmax (both fp32, in units of
+// log 2).  The sum so far and its weights are only rescaled when the maximum has grown by more than
+// 8 (a factor of 256, far from anything that fp32 sums lose), which after the first tiles it hardly does.
+//
+// k_attn_token / k_attn_join: for few rows a sequence (answering: one query a request) the work is split
+// over the keys instead, and is bound by reading them.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <new>
+
+#include "dnb_attn_dev.h"
+#include "dnb_attn.h"
+
+namespace dnb {
+namespace attn {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kRows = 128;  // packed rows of a workgroup of k_attn, 32 a wave
+
+// The state of 32 rows: O^T, running maximum (log2 units of the scaled scores) and this half's sum.
+template <int DB>
+struct Online {
+  f32x16 o[DB];
+  float m, l;
+  __device__ __forceinline__ void init() {
+#pragma unroll
+    for (int i = 0; i < DB; ++i) o[i] = (f32x16){};
+    m = -INFINITY;
+    l = 0.f;
+  }
+};
+
+// One more set of N blocks of 32 keys: scores s (scaled by c inside), values from `vt`.
+template <typename T, int DB, int N>
+__device__ __forceinline__ void online_step(Online<DB>& S, f32x16 (&s)[N], float c, const char* vt, int row0) {
+  float mx = -INFINITY;
+#pragma unroll
+  for (int b = 0; b < N; ++b)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[b][i]);
+  // c > 0: the scaled maximum is the maximum scaled
+  mx = half_max(mx) * c;
+  if (__any(mx > S.m + 8.f || (S.m == -INFINITY && mx > -INFINITY))) {
+    const float m = fmaxf(S.m, mx);
+    const float a = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(S.m - m);
+    S.m = m;
+    S.l *= a;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) S.o[db][i] *= a;
+  }
+  const float m = S.m == -INFINITY ? 0.f : S.m;  // nothing seen yet: exp2(-inf - 0) = 0
+#pragma unroll
+  for (int b = 0; b < N; ++b) {
+    float t = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], c, -m));
+      t += s[b][i];
+    }
+    S.l += t;
+  }
+#pragma unroll
+  for (int b = 0; b < N; ++b) col_mul<T, DB>(vt, row0 + 32 * b, s[b], S.o);
+}
+
+// Scores of keys key0 + row_of(i) that a query which sees keys below `sees` does not see
+__device__ __forceinline__ void hide(f32x16& s, int key0, int sees) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+    if (key0 + row_of(i) >= sees) s[i] = -INFINITY;
+}
+
+template <typename T, int DB>
+__global__ __launch_bounds__(kThreads, 2) void k_attn(Args A) {
+  using L = Tile<T, DB>;
+  constexpr int KT = L::ROWS, NB = KT / 32;
+  extern __shared__ __attribute__((aligned(16))) char lds[];  // [2][K tile, V tile]
+  const int g = blockIdx.x % A.kv, l = lane_id(), wave = threadIdx.x >> 6;
+  Seq S;
+  int t, count;
+  if (!find_tile(A, blockIdx.x / A.kv, [&](const Seq& s) { return (int)(((int64_t)s.nq * A.per + kRows - 1) / kRows); }, &S, &t, &count))
+    return;
+  if (A.causal) t = count - 1 - t;  // the rows that see most keys go first
+  const int M = S.nq * A.per, m0 = t * kRows, shift = S.nk - S.nq;
+  const int m = m0 + wave * 32 + (l & 31), row = m / A.per, sub = m - row * A.per;
+  const bool valid = m < M;
+  const int head = g * A.per + sub;
+  const int64_t qrow = (int64_t)S.q0 + row;
+  // keys that this lane's query sees, and at most / at least of the wave's; of the workgroup's
+  const int sees = A.causal ? min(max(row + shift + 1, 0), S.nk) : S.nk;
+  const int w0 = m0 + wave * 32, w1 = min(w0 + 31, M - 1);
+  const int most = w0 >= M ? 0 : A.causal ? min(max(w1 / A.per + shift + 1, 0), S.nk) : S.nk;
+  const int least = A.causal ? min(max(w0 / A.per + shift + 1, 0), S.nk) : S.nk;
+  const int all = A.causal ? min(max(min(m0 + kRows - 1, M - 1) / A.per + shift + 1, 0), S.nk) : S.nk;
+
+  Piece qf[L::NS];
+  load_cols<T, DB>(qf, (const T*)A.q + qrow * A.qs + (int64_t)head * A.d, valid, A.d);
+  Online<DB> R;
+  R.init();
+  const T* kb = (const T*)A.k + (int64_t)S.k0 * A.ks + (int64_t)g * A.d;
+  const T* vb = (const T*)A.v + (int64_t)S.k0 * A.vs + (int64_t)g * A.d;
+  Stage<T, DB, KT, kThreads> sk, sv;
+  sk.init(threadIdx.x, A.ks, A.d);
+  sv.init(threadIdx.x, A.vs, A.d);
+  auto fetch = [&](int k0) {
+    sk.load(kb + (int64_t)k0 * A.ks, A.ks, S.nk - k0, A.d);
+    sv.load(vb + (int64_t)k0 * A.vs, A.vs, S.nk - k0, A.d);
+  };
+  auto put = [&](int buf) {
+    sk.store(lds + buf * 2 * L::BYTES, threadIdx.x);
+    sv.store(lds + buf * 2 * L::BYTES + L::BYTES, threadIdx.x);
+  };
+  if (all > 0) {
+    fetch(0);
+    put(0);
+  }
+  __syncthreads();
+  int buf = 0;
+  for (int k0 = 0; k0 < all; k0 += KT, buf ^= 1) {
+    if (k0 + KT < all) fetch(k0 + KT);
+    if (k0 < most) {
+      const char* kt = lds + buf * 2 * L::BYTES;
+      f32x16 s[NB];
+#pragma unroll
+      for (int b = 0; b < NB; ++b) s[b] = row_mul<T, DB>(kt, 32 * b, qf);
+      if (k0 + KT > least) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b) hide(s[b], k0 + 32 * b, sees);
+      }
+      online_step<T, DB, NB>(R, s, A.c, kt + L::BYTES, 0);
+    }
+    if (k0 + KT < all) put(buf ^ 1);
+    __syncthreads();
+  }
+  const float sum = half_sum(R.l);
+  store_cols<T, DB>((T*)A.o + qrow * A.os + (int64_t)head * A.d, valid, A.d, R.o, sum == 0.f ? 0.f : 1.f / sum);
+  if (valid && l < 32) A.lse[(int64_t)head * A.rq + qrow] = sum == 0.f ? -INFINITY : (R.m + log2f(sum)) * kLn2;
+}
+
+// ---------------------------------------------------------------- few rows a sequence
+
+// Items are (sequence, tile of 32 packed rows, key/value head), in that order, a unit is 32 keys of an
+// item, and all units of all items lie on one line, which is cut into equal parts, one a wave: whatever
+// the lengths, no wave has more than one unit more than another.  A part of an item leaves O, m and l
+// in slot (wave + item): walking along the line, each next part has a next wave or a next item.
+constexpr int kItemRows = 32, kUnit = 32;
+
+struct Line {
+  int64_t units, items;  // of this lane's sequence
+};
+__device__ __forceinline__ Line line_of(const Args& A, const Seq& s) {
+  const int64_t items = ((int64_t)s.nq * A.per + kItemRows - 1) / kItemRows * A.kv;
+  return {items * ((s.nk + kUnit - 1) / kUnit), items};
+}
+__device__ __forceinline__ int64_t line_total(const Args& A) {
+  int64_t u = 0;
+  for (int i = lane_id(); i < A.n; i += 64) u += line_of(A, seq_at(A, i)).units;
+  return bcast64(wave_scan(u), 63);
+}
+constexpr int64_t slot_floats(int dp) { return (int64_t)kItemRows * dp + 2 * kItemRows; }
+
+template <typename T, int DB>
+__global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void k_attn_token(Args A) {
+  using L = Tile<T, DB>;
+  extern __shared__ __attribute__((aligned(16))) char lds[];  // a K and a V tile of 32 keys for each wave
+  const int l = lane_id(), wave = threadIdx.x >> 6;
+  char* kt = lds + wave * 2 * kUnit * L::PITCH;
+  char* vt = kt + kUnit * L::PITCH;
+  const int64_t total = line_total(A), W = min((int64_t)A.waves, total), w = (int64_t)blockIdx.x * 4 + wave;
+  if (w >= W) return;
+  int64_t a = w * total / W;
+  const int64_t b = (w + 1) * total / W;
+  Stage<T, DB, kUnit, 64> sk, sv;
+  sk.init(l, A.ks, A.d);
+  sv.init(l, A.vs, A.d);
+  int64_t u0 = 0, i0 = 0;  // units and items before the 64 sequences at hand
+  for (int base = 0; base < A.n && a < b; base += 64) {
+    Seq mine = {};
+    Line ln = {};
+    if (base + l < A.n) {
+      mine = seq_at(A, base + l);
+      ln = line_of(A, mine);
+    }
+    const int64_t ue = wave_scan(ln.units), ie = wave_scan(ln.items);
+    const int64_t u1 = u0 + bcast64(ue, 63);
+    while (a < b && a < u1) {
+      const int at = __builtin_ctzll(__ballot(u0 + ue > a));
+      const Seq S = bcast(mine, at);
+      const int64_t su = u0 + bcast64(ue, at) - bcast64(ln.units, at), si = i0 + bcast64(ie, at) - bcast64(ln.items, at);
+      const int len = (S.nk + kUnit - 1) / kUnit;
+      const int64_t j = (a - su) / len;
+      const int first = (int)(a - su - j * len), last = (int)min((int64_t)len, first + b - a);
+      const int g = (int)(j % A.kv), m0 = (int)(j / A.kv) * kItemRows, M = S.nq * A.per;
+      const int m = m0 + (l & 31), row = m / A.per, head = g * A.per + m - row * A.per;
+      const bool valid = m < M;
+      const int sees = A.causal ? min(max(row + S.nk - S.nq + 1, 0), S.nk) : S.nk;
+      const int least = A.causal ? min(max(m0 / A.per + S.nk - S.nq + 1, 0), S.nk) : S.nk;
+      Piece qf[L::NS];
+      load_cols<T, DB>(qf, (const T*)A.q + ((int64_t)S.q0 + row) * A.qs + (int64_t)head * A.d, valid, A.d);
+      Online<DB> R;
+      R.init();
+      const T* kb = (const T*)A.k + (int64_t)S.k0 * A.ks + (int64_t)g * A.d;
+      const T* vb = (const T*)A.v + (int64_t)S.k0 * A.vs + (int64_t)g * A.d;
+      auto fetch = [&](int u) {
+        sk.load(kb + (int64_t)u * kUnit * A.ks, A.ks, S.nk - u * kUnit, A.d);
+        sv.load(vb + (int64_t)u * kUnit * A.vs, A.vs, S.nk - u * kUnit, A.d);
+      };
+      fetch(first);
+      for (int u = first; u < last; ++u) {
+        // the tiles are this wave's own, and LDS serves a wave's accesses in their order
+        sk.store(kt, l);
+        sv.store(vt, l);
+        if (u + 1 < last) fetch(u + 1);
+        __builtin_amdgcn_wave_barrier();
+        f32x16 s[1] = {row_mul<T, DB>(kt, 0, qf)};
+        if ((u + 1) * kUnit > least) hide(s[0], u * kUnit, sees);
+        online_step<T, DB, 1>(R, s, A.c, vt, 0);
+        __builtin_amdgcn_wave_barrier();
+      }
+      const int64_t slot = w + si + j;
+      if (slot < A.slots) {
+        float* p = A.part + slot * slot_floats(32 * DB);
+        store_cols<float, DB>(p + (l & 31) * 32 * DB, valid, 32 * DB, R.o, 1.f);
+        const float sum = half_sum(R.l);
+        if (valid && l < 32) {
+          p[kItemRows * 32 * DB + l] = R.m;
+          p[kItemRows * 32 * DB + kItemRows + l] = sum;
+        }
+      }
+      a += last - first;
+    }
+    u0 = u1;
+    i0 += bcast64(ie, 63);
+  }
+}
+
+// Joins an item's parts: a wave for each (query row, head).
+template <typename T, int DB>
+__global__ __launch_bounds__(kThreads) void k_attn_join(Args A) {
+  constexpr int DP = 32 * DB;
+  const int l = lane_id();
+  const int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (id >= A.rq * A.heads) return;
+  const int64_t qrow = id / A.heads;
+  const int head = (int)(id - qrow * A.heads);
+  // the last sequence that holds the row: offsets are sorted, so it is the only one with rows there
+  int64_t u0 = 0, i0 = 0, su = 0, si = 0;
+  Seq S = {};
+  bool found = false;
+  for (int base = 0; base < A.n; base += 64) {
+    Seq mine = {};
+    Line ln = {};
+    if (base + l < A.n) {
+      mine = seq_at(A, base + l);
+      ln = line_of(A, mine);
+    }
+    const int64_t ue = wave_scan(ln.units), ie = wave_scan(ln.items);
+    const uint64_t holds = __ballot(mine.q0 <= qrow && qrow < (int64_t)mine.q0 + mine.nq);
+    if (holds) {
+      const int at = __builtin_ctzll(holds);
+      S = bcast(mine, at);
+      su = u0 + bcast64(ue, at) - bcast64(ln.units, at);
+      si = i0 + bcast64(ie, at) - bcast64(ln.items, at);
+      found = true;
+    }
+    u0 += bcast64(ue, 63);
+    i0 += bcast64(ie, 63);
+  }
+  if (!found) return;  // a row of no sequence
+  const int64_t total = u0, W = min((int64_t)A.waves, total);
+  const int g = head / A.per, m = (int)(qrow - S.q0) * A.per + head - g * A.per, r = m % kItemRows;
+  const int len = (S.nk + kUnit - 1) / kUnit;
+  const int64_t j = (int64_t)(m / kItemRows) * A.kv + g;
+  float M = -INFINITY, sum = 0.f, o0 = 0.f, o1 = 0.f;
+  if (len > 0) {
+    // unit u is wave ((u + 1) W - 1) / total's
+    const int64_t A0 = su + j * len;
+    const int64_t w0 = ((A0 + 1) * W - 1) / total, w1 = ((A0 + len) * W - 1) / total;
+    const float* p = A.part + (si + j + w0) * slot_floats(DP);
+    const int n = (int)(w1 - w0 + 1);
+    if (si + j + w1 >= A.slots) return;  // offsets that are not sorted
+    for (int i = l; i < n; i += 64) M = fmaxf(M, p[i * slot_floats(DP) + kItemRows * DP + r]);
+#pragma unroll
+    for (int o = 32; o; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
+    for (int i = 0; i < n; ++i) {
+      const float* q = p + i * slot_floats(DP);
+      const float mi = q[kItemRows * DP + r];
+      const float f = mi == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mi - M);
+      sum += f * q[kItemRows * DP + kItemRows + r];
+      if (l < DP / 2) {
+        const float2 v = *reinterpret_cast<const float2*>(q + r * DP + 2 * l);
+        o0 += f * v.x;
+        o1 += f * v.y;
+      }
+    }
+  }
+  const float inv = sum == 0.f ? 0.f : 1.f / sum;
+  if (2 * l < A.d) {
+    T* y = (T*)A.o + qrow * A.os + (int64_t)head * A.d + 2 * l;
+    y[0] = (T)(o0 * inv);
+    y[1] = (T)(o1 * inv);
+  }
+  if (l == 0) A.lse[(int64_t)head * A.rq + qrow] = sum == 0.f ? -INFINITY : (M + log2f(sum)) * kLn2;
+}
+
+template <typename T, int DB>
+hipError_t run_forward(const Args& A, bool token, hipStream_t st) {
+  using L = Tile<T, DB>;
+  if (token) {
+    hipLaunchKernelGGL((k_attn_token<T, DB>), dim3(A.waves / 4), dim3(kThreads), 8 * kUnit * L::PITCH, st, A);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((k_attn_join<T, DB>), dim3((unsigned)((A.rq * A.heads + 3) / 4)), dim3(kThreads), 0, st, A);
+  } else {
+    const int64_t tiles = (A.rq * A.per + kRows - 1) / kRows + A.n;
+    hipLaunchKernelGGL((k_attn<T, DB>), dim3((unsigned)(tiles * A.kv)), dim3(kThreads), 4 * L::BYTES, st, A);
+  }
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t run_forward_db(const Args& A, bool token, hipStream_t st) {
+  switch ((A.d + 31) / 32) {
+    case 1: return run_forward<T, 1>(A, token, st);
+    case 2: return run_forward<T, 2>(A, token, st);
+    case 3: return run_forward<T, 3>(A, token, st);
+    default: return run_forward<T, 4>(A, token, st);
+  }
+}
+
+inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+}  // namespace
+}  // namespace attn
+}  // namespace dnb
+
+using namespace dnb::attn;
+
+struct dnb_attn {
+  dnb_attn_desc d;
+  bool token;       // the forward's form
+  int waves;        // of the token form
+  int64_t slots;
+  size_t ws_part, ws_rowdot, ws_bytes;
+};
+
+namespace {
+
+void fill(const dnb_attn* p, Args* A) {
+  const dnb_attn_desc& d = p->d;
+  *A = Args{};
+  A->n = d.sequences; A->heads = d.heads; A->kv = d.kv_heads; A->per = d.heads / d.kv_heads; A->d = d.head_dim;
+  A->causal = d.causal != 0;
+  A->rq = d.rows_q; A->rk = d.rows_k; A->qs = d.q_stride; A->ks = d.k_stride; A->vs = d.v_stride;
+  A->os = (int64_t)d.heads * d.head_dim;
+  A->scale = d.scale;
+  A->c = d.scale * kLog2e;
+  A->waves = p->waves;
+  A->slots = p->slots;
+}
+
+}  // namespace
+
+extern "C" {
+
+int dnb_attn_create(const dnb_attn_desc* desc, dnb_attn** out) {
+  if (!desc || !out) return DNB_E_NULL;
+  dnb_attn_desc d = *desc;
+  if (d.heads < 1 || d.kv_heads < 1 || d.heads % d.kv_heads != 0 || d.head_dim < 1 || d.sequences < 1 || d.rows_q < 0 ||
+      d.rows_k < 0 || (d.dtype != DNB_F32 && d.dtype != DNB_BF16) || !(d.scale >= 0.f && d.scale < INFINITY))
+    return DNB_E_BADDESC;
+  if (d.head_dim % 8 != 0 || d.head_dim > 128) return DNB_E_UNSUPPORTED;
+  if (d.heads > 65536 || d.sequences > (1 << 20)) return DNB_E_RANGE;
+  const int64_t qd = (int64_t)d.heads * d.head_dim, kd = (int64_t)d.kv_heads * d.head_dim;
+  if (d.q_stride == 0) d.q_stride = qd;
+  if (d.k_stride == 0) d.k_stride = kd;
+  if (d.v_stride == 0) d.v_stride = kd;
+  if (d.scale == 0.f) d.scale = (float)(1.0 / sqrt((double)d.head_dim));
+  const int vec = d.dtype == DNB_BF16 ? 8 : 4, per = d.heads / d.kv_heads;
+  // rows are read in 16-byte pieces; a tile of 64 rows is addressed with 31 bits
+  for (const int64_t s : {d.q_stride, d.k_stride, d.v_stride})
+    if (s % vec != 0 || s > (1 << 22)) return DNB_E_RANGE;
+  if (d.q_stride < qd || d.k_stride < kd || d.v_stride < kd) return DNB_E_RANGE;
+  const int64_t most = 0x7fffffff;
+  if (d.rows_q > most || d.rows_k > most || d.rows_q * per > most - 256 || d.rows_q * d.heads > most ||
+      ((d.rows_q * per + 31) / 32 + d.sequences) * d.kv_heads > most || (d.rows_k / 32 + 1 + d.sequences) * d.kv_heads > most)
+    return DNB_E_RANGE;
+  dnb_attn* p = new (std::nothrow) dnb_attn();
+  if (!p) return DNB_E_NOMEM;
+  p->d = d;
+  // the token form takes a sequence's rows in tiles of 32: as long as they fit one on average
+  p->token = d.rows_q * per <= (int64_t)kItemRows * d.sequences;
+  const int dp = (d.head_dim + 31) / 32 * 32;
+  p->waves = d.dtype == DNB_BF16 ? 2048 : 1024;  // 256 compute units, two workgroups of four waves each, fp32 one
+  p->slots = p->token ? p->waves + ((d.rows_q * per + kItemRows - 1) / kItemRows + d.sequences) * d.kv_heads : 0;
+  p->ws_rowdot = 0;
+  p->ws_part = ((size_t)d.rows_q * d.heads * sizeof(float) + 255) / 256 * 256;
+  p->ws_bytes = p->ws_part + (size_t)p->slots * slot_floats(dp) * sizeof(float);
+  *out = p;
+  return DNB_OK;
+}
+
+void dnb_attn_destroy(dnb_attn* p) { delete p; }
+
+size_t dnb_attn_workspace_bytes(const dnb_attn* p) { return p ? p->ws_bytes : 0; }
+
+int dnb_attn_forward(const dnb_attn* p, const void* q, const void* k, const void* v, const int32_t* q_offsets,
+                     const int32_t* k_offsets, const int32_t* k_lengths, void* out, float* lse, void* workspace, void* stream) {
+  if (!p || !q_offsets || !k_offsets) return DNB_E_NULL;
+  if (p->d.rows_q == 0) return DNB_OK;
+  if (!q || !out || !lse || !workspace || (p->d.rows_k > 0 && (!k || !v))) return DNB_E_NULL;
+  for (const void* x : {q, k, v, (const void*)out, (const void*)workspace})
+    if (!aligned16(x)) return DNB_E_ALIGN;
+  Args A;
+  fill(p, &A);
+  A.q = q; A.k = k; A.v = v; A.o = out; A.lse = lse;
+  A.qo = q_offsets; A.ko = k_offsets; A.kl = k_lengths;
+  A.part = (float*)((char*)workspace + p->ws_part);
+  hipStream_t st = (hipStream_t)stream;
+  const hipError_t e = p->d.dtype == DNB_BF16 ? run_forward_db<__bf16>(A, p->token, st) : run_forward_db<float>(A, p->token, st);
+  return e == hipSuccess ? DNB_OK : DNB_E_LAUNCH;
+}
+
+int dnb_attn_backward(const dnb_attn* p, const void* q, const void* k, const void* v, const void* out, const float* lse,
+                      const void* dout, const int32_t* q_offsets, const int32_t* k_offsets, const int32_t* k_lengths, void* dq,
+                      void* dk, void* dv, void* workspace, void* stream) {
+  if (!p || !q_offsets || !k_offsets) return DNB_E_NULL;
+  const bool anyq = p->d.rows_q > 0, anyk = p->d.rows_k > 0;
+  if (anyq && (!q || !out || !lse || !dout || !dq || !workspace)) return DNB_E_NULL;
+  if (anyk && (!k || !v || !dk || !dv)) return DNB_E_NULL;
+  for (const void* x : {q, k, v, out, dout, (const void*)dq, (const void*)dk, (const void*)dv, (const void*)workspace})
+    if (!aligned16(x)) return DNB_E_ALIGN;
+  Args A;
+  fill(p, &A);
+  A.q = q; A.k = k; A.v = v; A.out = out; A.lse = (float*)lse; A.dout = dout;
+  A.dq = dq; A.dk = dk; A.dv = dv;
+  A.qo = q_offsets; A.ko = k_offsets; A.kl = k_lengths;
+  A.rowdot = (float*)((char*)workspace + p->ws_rowdot);
+  const hipError_t e = launch_backward(A, p->d.dtype == DNB_BF16, (hipStream_t)stream);
+  return e == hipSuccess ? DNB_OK : DNB_E_LAUNCH;
+}
+
+}  // extern "C"

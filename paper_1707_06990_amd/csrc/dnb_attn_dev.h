@@ -1,0 +1,289 @@
+// Device helpers of the packed-sequence attention kernels (dnb_attn.hip, dnb_attn_bwd.hip).
+//
+// One wave works on 32 rows (the columns of its matrix products) against tiles of the other side in
+// LDS.  Every product is one of two:
+//   row_mul   S[r][c]   = sum_d X[r][d] B[d][c]     X a tile in LDS, B this wave's 32 columns in registers
+//   col_mul   Y[d][c]  += sum_r X[r][d] S[r][c]     S as row_mul left it
+// With 32x32 products a lane holds column c = lane & 31 of S and its rows 8*(i/4) + 4*(lane>>5) + i%4,
+// i < 16.  That is also how the second product wants its right operand, up to an order of the rows over
+// which it sums, and any order will do as long as the left operand has the same one: S goes from one
+// product into the next without leaving its lane, and a softmax over r is 16 values a lane and one
+// exchange between the halves of the wave.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "../../include/dnb.h"
+
+namespace dnb {
+namespace attn {
+
+// What every kernel of an attention plan is given.  Strides in elements between rows.
+struct Args {
+  const void *q, *k, *v, *out, *dout;
+  void *o, *dq, *dk, *dv;  // o: the forward's output
+  float *lse;              // (heads, rows_q)
+  float *rowdot;           // backward: sum of dout * out of each row, (heads, rows_q)
+  float *part;             // token form: partial results
+  const int32_t *qo, *ko, *kl;
+  int n, heads, kv, per, d, causal;
+  int64_t rq, rk, qs, ks, vs, os;
+  float scale, c;          // c = scale * log2(e)
+  int waves;               // token form: waves of the launch
+  int64_t slots;           //             partial results that `part` has room for
+};
+
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+typedef unsigned short u16;
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+// 16 bytes of a row: 8 bf16 or 4 floats
+union Piece {
+  u32x4 q;
+  bf16x8 h;
+  __bf16 b[8];
+  float f[4];
+};
+
+__device__ __forceinline__ int lane_id() { return threadIdx.x & 63; }
+// row of element i of a 32x32 result in this lane
+__device__ __forceinline__ int row_of(int i) { return 8 * (i >> 2) + 4 * (lane_id() >> 5) + (i & 3); }
+
+__device__ __forceinline__ float half_max(float v) {
+  const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1]));
+}
+__device__ __forceinline__ float half_sum(float v) {
+  const auto s = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(s[0]) + __uint_as_float(s[1]);
+}
+
+// A tile in LDS: rows of PC pieces of 16 bytes, of which CH hold the row (head_dim padded with zeros to
+// DB blocks of 32).  Piece c of row r lies at c ^ swz(r): sixteen rows read at one c (row_mul), and four
+// rows read 64 bytes wide (col_mul in bf16) or rows r and r + 4 read 128 bytes wide (in fp32), each meet
+// all the banks.
+template <typename T, int DB>
+struct Tile {
+  static constexpr bool BF = sizeof(T) == 2;
+  static constexpr int EP = 16 / sizeof(T);            // elements of a piece
+  static constexpr int CH = DB * 32 / EP;
+  static constexpr int PC = BF ? (DB == 1 ? 4 : DB == 2 ? 8 : 16) : (DB == 1 ? 8 : DB == 2 ? 16 : 32);
+  static constexpr int PITCH = PC * 16;                // bytes
+  static constexpr int NS = CH / 2;                    // steps of row_mul: a lane's half of the wave takes piece 2s + half
+  static constexpr int ROWS = BF ? 64 : 32;            // rows of a shared tile
+  static constexpr int BYTES = ROWS * PITCH;
+  static __device__ __forceinline__ int swz(int r) {
+    if constexpr (BF) {
+      if constexpr (PC == 4) return (r >> 2) & 3;
+      else if constexpr (PC == 8) return (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
+      else return ((r & 3) << 2) | ((r >> 2) & 3);
+    } else {
+      if constexpr (PC == 8) return (r >> 1) & 7;
+      else return (((r >> 2) & 1) << 3) | (((r >> 3) & 1) << 2) | (r & 3);
+    }
+  }
+  static __device__ __forceinline__ int at(int r, int c) { return r * PITCH + ((c ^ swz(r)) << 4); }
+};
+
+// a wave's 32 columns: of each step, this lane's half
+template <typename T, int DB>
+using Columns = Piece[Tile<T, DB>::NS];
+
+__device__ __forceinline__ void mma(f32x16& acc, const Piece& a, const Piece& b, __bf16*) {
+  acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.h, b.h, acc, 0, 0, 0);
+}
+__device__ __forceinline__ void mma(f32x16& acc, const Piece& a, const Piece& b, float*) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a.f[j], b.f[j], acc, 0, 0, 0);
+}
+
+// rows row0 .. row0 + 31 of the tile times this wave's columns
+template <typename T, int DB>
+__device__ __forceinline__ f32x16 row_mul(const char* tile, int row0, const Columns<T, DB>& b) {
+  using L = Tile<T, DB>;
+  const int r = row0 + (lane_id() & 31), h = lane_id() >> 5;
+  f32x16 s = {};
+#pragma unroll
+  for (int k = 0; k < L::NS; ++k) {
+    Piece a;
+    a.q = *reinterpret_cast<const u32x4*>(tile + L::at(r, 2 * k + h));
+    mma(s, a, b[k], (T*)nullptr);
+  }
+  return s;
+}
+
+// bf16: rounding s to 8 bits of mantissa is what feeding the matrix cores at their bf16 rate costs;
+// the sums stay in fp32.
+template <typename T, int DB>
+__device__ __forceinline__ void col_mul(const char* tile, int row0, const f32x16& s, f32x16 (&acc)[DB]) {
+  using L = Tile<T, DB>;
+  const int l = lane_id();
+  if constexpr (L::BF) {
+    const int r = row0 + 4 * (l >> 5) + ((l >> 2) & 3), c = 2 * ((l >> 4) & 1) + ((l >> 1) & 1), o = (l & 1) * 8;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      Piece p;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) p.b[j] = (__bf16)s[8 * t + j];
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        using lds4 = __attribute__((address_space(3))) s16x4;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(tile + L::at(r + 16 * t, 4 * db + c) + o));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(tile + L::at(r + 16 * t + 8, 4 * db + c) + o));
+        const uint2 a = __builtin_bit_cast(uint2, lo), b = __builtin_bit_cast(uint2, hi);
+        Piece x;
+        x.q = (u32x4){a.x, a.y, b.x, b.y};
+        mma(acc[db], x, p, (T*)nullptr);
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const int r = row0 + 8 * (i >> 2) + 4 * (l >> 5) + (i & 3);
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        const float x = *reinterpret_cast<const float*>(tile + L::at(r, 8 * db + ((l & 31) >> 2)) + (l & 3) * 4);
+        acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, s[i], acc[db], 0, 0, 0);
+      }
+    }
+  }
+}
+
+// Rows of a tile on their way from memory to LDS, NT threads.  The loads go through a buffer descriptor
+// over exactly the rows that exist: what lies past them, and the pieces that pad head_dim, reads as zero.
+template <typename T, int DB, int ROWS, int NT>
+struct Stage {
+  using L = Tile<T, DB>;
+  static constexpr int U = ROWS * L::CH / NT;
+  static_assert(ROWS * L::CH % NT == 0, "whole pieces a thread");
+  u32x4 r[U];
+  uint32_t off[U];
+  __device__ __forceinline__ void init(int tid, int64_t stride, int d) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = tid + u * NT, row = i / L::CH, c = i - row * L::CH;
+      off[u] = c * L::EP < d ? (uint32_t)(row * (int)stride + c * L::EP) * (uint32_t)sizeof(T) : 0x80000000u;
+    }
+  }
+  // base: the first row; rows: how many there are from it on (uniform in the wave; 0 or less: none)
+  __device__ __forceinline__ void load(const T* base, int64_t stride, int rows, int d) {
+    const int n = rows > ROWS ? ROWS : rows;
+    const int bytes = n > 0 ? (int)(((n - 1) * (int)stride + d) * (int)sizeof(T)) : 0;
+    const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, bytes, 0x00027000);
+#pragma unroll
+    for (int u = 0; u < U; ++u) r[u] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, off[u], 0, 0);
+  }
+  __device__ __forceinline__ void store(char* tile, int tid) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = tid + u * NT, row = i / L::CH, c = i - row * L::CH;
+      *reinterpret_cast<u32x4*>(tile + L::at(row, c)) = r[u];
+    }
+  }
+};
+
+// This lane's column (its half of each step's two pieces) of a row of d elements; zeros if !valid.
+template <typename T, int DB>
+__device__ __forceinline__ void load_cols(Columns<T, DB>& f, const T* row, bool valid, int d) {
+  using L = Tile<T, DB>;
+  const int h = lane_id() >> 5;
+#pragma unroll
+  for (int k = 0; k < L::NS; ++k) {
+    const int e = (2 * k + h) * L::EP;
+    f[k].q = (u32x4){0u, 0u, 0u, 0u};
+    if (valid && e < d) f[k].q = *reinterpret_cast<const u32x4*>(row + e);
+  }
+}
+
+// Y[d][c] of a wave (col_mul's result) times f into row c
+template <typename T, int DB>
+__device__ __forceinline__ void store_cols(T* row, bool valid, int d, const f32x16 (&acc)[DB], float f) {
+  if (!valid) return;
+  const int h = lane_id() >> 5;
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int e = 32 * db + 8 * g + 4 * h;
+      if (e >= d) continue;
+      if constexpr (sizeof(T) == 2) {
+        typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+        bf16x4 y;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) y[j] = (__bf16)(acc[db][4 * g + j] * f);
+        *reinterpret_cast<bf16x4*>(row + e) = y;
+      } else {
+        *reinterpret_cast<float4*>(row + e) =
+            make_float4(acc[db][4 * g] * f, acc[db][4 * g + 1] * f, acc[db][4 * g + 2] * f, acc[db][4 * g + 3] * f);
+      }
+    }
+}
+
+// One sequence, as its offsets say; whatever they hold, the rows stay inside the tensors.
+struct Seq {
+  int q0, nq, k0, nk, span;  // span: rows of k up to the next sequence's, of which nk are in use
+};
+__device__ __forceinline__ Seq seq_at(const Args& A, int i) {
+  Seq s;
+  const int64_t q0 = min(max((int64_t)A.qo[i], (int64_t)0), A.rq), q1 = min(max((int64_t)A.qo[i + 1], q0), A.rq);
+  const int64_t k0 = min(max((int64_t)A.ko[i], (int64_t)0), A.rk), k1 = min(max((int64_t)A.ko[i + 1], k0), A.rk);
+  s.q0 = (int)q0; s.nq = (int)(q1 - q0); s.k0 = (int)k0; s.span = (int)(k1 - k0);
+  s.nk = A.kl ? min(max(A.kl[i], 0), s.span) : s.span;
+  return s;
+}
+
+__device__ __forceinline__ int64_t wave_scan(int64_t v) {  // inclusive
+  const int l = lane_id();
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int64_t t = __shfl_up(v, o);
+    if (l >= o) v += t;
+  }
+  return v;
+}
+__device__ __forceinline__ int bcast(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }
+__device__ __forceinline__ Seq bcast(const Seq& s, int lane) {
+  return {bcast(s.q0, lane), bcast(s.nq, lane), bcast(s.k0, lane), bcast(s.nk, lane), bcast(s.span, lane)};
+}
+__device__ __forceinline__ int64_t bcast64(int64_t v, int lane) {
+  return (int64_t)(((uint64_t)(uint32_t)bcast((int)(v >> 32), lane) << 32) | (uint32_t)bcast((int)v, lane));
+}
+
+// The sequence that tile number `tile` of all sequences' tiles belongs to, and its number there.
+// tiles_of(seq) is a sequence's count.  Every wave finds it for itself from the offsets, 64 sequences at a
+// time: no launch and no host copy comes before.  False: there are fewer tiles.
+template <typename F>
+__device__ __forceinline__ bool find_tile(const Args& A, int64_t tile, F tiles_of, Seq* s, int* t, int* count) {
+  const int l = lane_id();
+  int64_t base = 0;
+  for (int i0 = 0; i0 < A.n; i0 += 64) {
+    Seq mine = {};
+    int c = 0;
+    if (i0 + l < A.n) {
+      mine = seq_at(A, i0 + l);
+      c = tiles_of(mine);
+    }
+    const int64_t end = wave_scan(c);
+    const uint64_t past = __ballot(base + end > tile);
+    if (past) {
+      const int at = __builtin_ctzll(past);
+      *s = bcast(mine, at);
+      *count = bcast(c, at);
+      *t = (int)(tile - base - (bcast64(end, at) - *count));
+      return true;
+    }
+    base += bcast64(end, 63);
+  }
+  return false;
+}
+
+}  // namespace
+}  // namespace attn
+}  // namespace dnb
