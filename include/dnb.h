@@ -503,6 +503,55 @@ int dnb_attn_backward(const dnb_attn* plan, const void* q, const void* k, const 
                       const void* dout, const int32_t* q_offsets, const int32_t* k_offsets, const int32_t* k_lengths, void* dq,
                       void* dk, void* dv, void* workspace, void* stream);
 
+/* Rotary positions: of every head of x (rows, heads, head_dim), pair i of the first rotary_dim values is
+ * turned by positions[row] * turns[i] full turns and multiplied by `factor`, the rest is copied.  Pair i
+ * is (i, i + rotary_dim / 2) with DNB_ROPE_HALF, (2i, 2i + 1) with DNB_ROPE_INTERLEAVED.  turns:
+ * rotary_dim / 2 doubles on the device (angle per position / 2 pi), which is where a context is
+ * stretched (other bases, divided or blended turns) at no cost; angles are taken in 64 bits.
+ * backward: dx = the adjoint for dy (turned back, times factor).  x and y may be the same memory, and
+ * strides (elements between rows, even; 0: dense) may take some heads out of wider rows.  head_dim even,
+ * up to 1024; heads up to 4096 (else DNB_E_RANGE). */
+enum { DNB_ROPE_HALF = 0, DNB_ROPE_INTERLEAVED = 1 };
+int dnb_op_rope_forward(const void* x, const int32_t* positions, const double* turns, void* y, int64_t rows, int64_t heads,
+                        int64_t head_dim, int64_t rotary_dim, int order, float factor, int dtype, int64_t x_stride,
+                        int64_t y_stride, void* stream);
+int dnb_op_rope_backward(const void* dy, const int32_t* positions, const double* turns, void* dx, int64_t rows, int64_t heads,
+                         int64_t head_dim, int64_t rotary_dim, int order, float factor, int dtype, int64_t dy_stride,
+                         int64_t dx_stride, void* stream);
+
+/* The norms around a block, whose output is b and whose residual is r, (rows, width) of the type:
+ *   h_new = scale r + gate * (b / rms(b) * w_post)      y = h_new / rms(h_new) * w_pre
+ * with rms(x) = sqrt(mean(x^2) + eps) of a row.  w_post null: b is not normed.  gate: none (1), a vector
+ * (width, fp32) or full (rows, width, of the type).  w_post, w_pre and their gradients fp32.  y is taken
+ * from h_new before it is rounded.
+ * backward: from b, h_new, and the gradients dh of h_new and dy of y, gives db, dr, dw_post (if w_post),
+ * dgate (fp32 vector or full) and dw_pre.  scratch: dnb_op_norm_residual_scratch_bytes.
+ * width a multiple of 8 (else DNB_E_UNSUPPORTED) up to 16384 (else DNB_E_RANGE). */
+enum { DNB_GATE_NONE = 0, DNB_GATE_VECTOR = 1, DNB_GATE_FULL = 2 };
+size_t dnb_op_norm_residual_scratch_bytes(int64_t rows, int64_t width, int gate_kind);
+int dnb_op_norm_residual_forward(const void* b, const void* r, const float* w_post, const void* gate, const float* w_pre,
+                                 void* h_new, void* y, int64_t rows, int64_t width, float scale, float eps, int gate_kind,
+                                 int dtype, void* stream);
+int dnb_op_norm_residual_backward(const void* b, const void* h_new, const float* w_post, const void* gate, const float* w_pre,
+                                  const void* dh, const void* dy, void* db, void* dr, float* dw_post, void* dgate,
+                                  float* dw_pre, int64_t rows, int64_t width, float scale, float eps, int gate_kind, int dtype,
+                                  void* scratch, void* stream);
+
+/* Clipping by the global norm of many tensors: with norm = sqrt(sum of all squares) and
+ * coef = min(1, max_norm / (norm + 1e-6)), dst[i] = coef * src[i] (the same memory is allowed) and
+ * norm[0] = norm, norm[1] = coef (two floats on the device).  The squares are summed in 64 bits across
+ * a tensor's parts, in an order that does not change.  A plan is made of the tensors' addresses, counts
+ * and types; its table is copied to the device by the caller (dnb_clip_table writes it to host memory)
+ * and given to every run, with a workspace (both 16-byte aligned). */
+typedef struct dnb_clip dnb_clip; /* opaque, host side only */
+int dnb_clip_create(const void* const* src, void* const* dst, const int64_t* counts, const int32_t* dtypes, int64_t tensors,
+                    dnb_clip** out);
+void dnb_clip_destroy(dnb_clip* plan);
+size_t dnb_clip_table_bytes(const dnb_clip* plan);
+int dnb_clip_table(const dnb_clip* plan, void* host);
+size_t dnb_clip_workspace_bytes(const dnb_clip* plan);
+int dnb_clip_run(const dnb_clip* plan, const void* table, float max_norm, float* norm, void* workspace, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

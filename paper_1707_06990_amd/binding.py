@@ -14,6 +14,8 @@ DNB_OK = 0
 DNB_E_BADDESC, DNB_E_NULL, DNB_E_ALIGN, DNB_E_LAUNCH, DNB_E_UNSUPPORTED, DNB_E_RANGE, DNB_E_NOMEM = range(-1, -8, -1)
 DNB_F32, DNB_BF16 = 0, 1
 DNB_NCHW, DNB_NHWC = 0, 1
+DNB_ROPE_HALF, DNB_ROPE_INTERLEAVED = 0, 1
+DNB_GATE_NONE, DNB_GATE_VECTOR, DNB_GATE_FULL = 0, 1, 2
 DNB_SCHED_SHARED, DNB_SCHED_STORE_ALL, DNB_SCHED_FUSED = 0, 1, 2
 DNB_P_G1, DNB_P_B1, DNB_P_W1, DNB_P_G2, DNB_P_B2, DNB_P_W3 = range(6)
 (DNB_NP_STEM, DNB_NP_BLOCK0, DNB_NP_BLOCK1, DNB_NP_BLOCK2, DNB_NP_TRANS0_G, DNB_NP_TRANS0_B, DNB_NP_TRANS0_W,
@@ -140,6 +142,17 @@ _SIGS = {
     "dnb_attn_workspace_bytes": (_sz, [_vp]),
     "dnb_attn_forward": (C.c_int, [_vp] * 11),
     "dnb_attn_backward": (C.c_int, [_vp] * 15),
+    "dnb_op_rope_forward": (C.c_int, [_vp] * 4 + [_i64] * 4 + [C.c_int, C.c_float, C.c_int, _i64, _i64, _vp]),
+    "dnb_op_rope_backward": (C.c_int, [_vp] * 4 + [_i64] * 4 + [C.c_int, C.c_float, C.c_int, _i64, _i64, _vp]),
+    "dnb_op_norm_residual_scratch_bytes": (_sz, [_i64, _i64, C.c_int]),
+    "dnb_op_norm_residual_forward": (C.c_int, [_vp] * 7 + [_i64, _i64, C.c_float, C.c_float, C.c_int, C.c_int, _vp]),
+    "dnb_op_norm_residual_backward": (C.c_int, [_vp] * 12 + [_i64, _i64, C.c_float, C.c_float, C.c_int, C.c_int, _vp, _vp]),
+    "dnb_clip_create": (C.c_int, [C.POINTER(_vp), C.POINTER(_vp), C.POINTER(_i64), C.POINTER(C.c_int32), _i64, C.POINTER(_vp)]),
+    "dnb_clip_destroy": (None, [_vp]),
+    "dnb_clip_table_bytes": (_sz, [_vp]),
+    "dnb_clip_table": (C.c_int, [_vp, _vp]),
+    "dnb_clip_workspace_bytes": (_sz, [_vp]),
+    "dnb_clip_run": (C.c_int, [_vp, _vp, C.c_float, _vp, _vp, _vp]),
 }
 for _name, (_res, _args) in _SIGS.items():
     _f = getattr(_lib, _name)
@@ -558,3 +571,69 @@ def dnb_attn_backward(plan, q, k, v, out, lse, dout, q_offsets, k_offsets, k_len
     _check(_lib.dnb_attn_backward(plan, _ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(lse), _ptr(dout), _ptr(q_offsets),
                                   _ptr(k_offsets), _ptr(k_lengths), _ptr(dq), _ptr(dk), _ptr(dv), _ptr(workspace),
                                   _stream(stream)))
+
+
+def dnb_op_rope_forward(x, positions, turns, y, rows, heads, head_dim, rotary_dim, order, factor=1.0, dtype=DNB_BF16,
+                        x_stride=0, y_stride=0, stream=None) -> None:
+    _check(_lib.dnb_op_rope_forward(_ptr(x), _ptr(positions), _ptr(turns), _ptr(y), rows, heads, head_dim, rotary_dim,
+                                    order, factor, dtype, x_stride, y_stride, _stream(stream)))
+
+
+def dnb_op_rope_backward(dy, positions, turns, dx, rows, heads, head_dim, rotary_dim, order, factor=1.0, dtype=DNB_BF16,
+                         dy_stride=0, dx_stride=0, stream=None) -> None:
+    _check(_lib.dnb_op_rope_backward(_ptr(dy), _ptr(positions), _ptr(turns), _ptr(dx), rows, heads, head_dim, rotary_dim,
+                                     order, factor, dtype, dy_stride, dx_stride, _stream(stream)))
+
+
+def dnb_op_norm_residual_scratch_bytes(rows, width, gate_kind) -> int:
+    return int(_lib.dnb_op_norm_residual_scratch_bytes(rows, width, gate_kind))
+
+
+def dnb_op_norm_residual_forward(b, r, w_post, gate, w_pre, h_new, y, rows, width, scale, eps, gate_kind, dtype,
+                                 stream=None) -> None:
+    _check(_lib.dnb_op_norm_residual_forward(_ptr(b), _ptr(r), _ptr(w_post), _ptr(gate), _ptr(w_pre), _ptr(h_new),
+                                             _ptr(y), rows, width, scale, eps, gate_kind, dtype, _stream(stream)))
+
+
+def dnb_op_norm_residual_backward(b, h_new, w_post, gate, w_pre, dh, dy, db, dr, dw_post, dgate, dw_pre, rows, width,
+                                  scale, eps, gate_kind, dtype, scratch, stream=None) -> None:
+    _check(_lib.dnb_op_norm_residual_backward(_ptr(b), _ptr(h_new), _ptr(w_post), _ptr(gate), _ptr(w_pre), _ptr(dh),
+                                              _ptr(dy), _ptr(db), _ptr(dr), _ptr(dw_post), _ptr(dgate), _ptr(dw_pre),
+                                              rows, width, scale, eps, gate_kind, dtype, _ptr(scratch), _stream(stream)))
+
+
+def dnb_clip_create(src, dst, dtypes, counts=None):
+    """src, dst: tensors (or addresses, with their counts)."""
+    n = len(src)
+    if counts is None:
+        counts = [t.numel() for t in src]
+    if not len(dst) == len(dtypes) == len(counts) == n:
+        raise ValueError("src, dst, dtypes and counts differ in length")
+    out = _vp()
+    _check(_lib.dnb_clip_create((_vp * n)(*map(_ptr, src)), (_vp * n)(*map(_ptr, dst)), (_i64 * n)(*counts),
+                                (C.c_int32 * n)(*dtypes), n, C.byref(out)))
+    return out
+
+
+def dnb_clip_destroy(plan) -> None:
+    _lib.dnb_clip_destroy(plan)
+
+
+def dnb_clip_table(plan):
+    """The plan's table as a numpy array of bytes, to be copied to the device."""
+    import numpy as np
+    table = np.empty(int(_lib.dnb_clip_table_bytes(plan)), dtype=np.uint8)
+    _check(_lib.dnb_clip_table(plan, table.ctypes.data))
+    return table
+
+
+def dnb_clip_table_bytes(plan) -> int:
+    return int(_lib.dnb_clip_table_bytes(plan))
+
+
+def dnb_clip_workspace_bytes(plan) -> int:
+    return int(_lib.dnb_clip_workspace_bytes(plan))
+
+
+def dnb_clip_run(plan, table, max_norm, norm, workspace, stream=None) -> None:
+    _check(_lib.dnb_clip_run(plan, _ptr(table), max_norm, _ptr(norm), _ptr(workspace), _stream(stream)))
