@@ -14,6 +14,7 @@
 
 #include <cmath>
 #include <new>
+#include <type_traits>
 
 #include "dnb_attn_dev.h"
 #include "dnb_attn.h"
@@ -39,8 +40,8 @@ struct Online {
 };
 
 // One more set of N blocks of 32 keys: scores s (scaled by c inside), values from `vt`.
-template <typename T, int DB, int N>
-__device__ __forceinline__ void online_step(Online<DB>& S, f32x16 (&s)[N], float c, const char* vt, int row0) {
+template <typename T, int DB, int N, bool HOLD>
+__device__ __forceinline__ void online_step(Online<DB>& S, f32x16 (&s)[N], float c, lds_t vt, int row0) {
   float mx = -INFINITY;
 #pragma unroll
   for (int b = 0; b < N; ++b)
@@ -70,21 +71,23 @@ __device__ __forceinline__ void online_step(Online<DB>& S, f32x16 (&s)[N], float
     S.l += t;
   }
 #pragma unroll
-  for (int b = 0; b < N; ++b) col_mul<T, DB>(vt, row0 + 32 * b, s[b], S.o);
+  for (int b = 0; b < N; ++b) col_mul<T, DB, HOLD>(vt, row0 + 32 * b, s[b], S.o);
 }
 
 // Scores of keys key0 + row_of(i) that a query which sees keys below `sees` does not see
 __device__ __forceinline__ void hide(f32x16& s, int key0, int sees) {
 #pragma unroll
   for (int i = 0; i < 16; ++i)
-    if (key0 + row_of(i) >= sees) s[i] = -INFINITY;
+    s[i] = key0 + row_of(i) >= sees ? -INFINITY : s[i];
 }
 
 template <typename T, int DB>
 __global__ __launch_bounds__(kThreads, 2) void k_attn(Args A) {
   using L = Tile<T, DB>;
   constexpr int KT = L::ROWS, NB = KT / 32;
-  extern __shared__ __attribute__((aligned(16))) char lds[];  // [2][K tile, V tile]
+  constexpr bool HOLD = L::BF || DB <= 2;
+  extern __shared__ __attribute__((aligned(512))) char shared[];  // [2][K tile, V tile]
+  const lds_t lds = lds_start(shared);
   const int g = blockIdx.x % A.kv, l = lane_id(), wave = threadIdx.x >> 6;
   Seq S;
   int t, count;
@@ -125,22 +128,26 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn(Args A) {
     put(0);
   }
   __syncthreads();
-  int buf = 0;
-  for (int k0 = 0; k0 < all; k0 += KT, buf ^= 1) {
+  auto step = [&](int k0, auto which) {
+    constexpr int BUF = which;
     if (k0 + KT < all) fetch(k0 + KT);
     if (k0 < most) {
-      const char* kt = lds + buf * 2 * L::BYTES;
+      const lds_t kt = lds + BUF * 2 * L::BYTES;
       f32x16 s[NB];
 #pragma unroll
-      for (int b = 0; b < NB; ++b) s[b] = row_mul<T, DB>(kt, 32 * b, qf);
+      for (int b = 0; b < NB; ++b) s[b] = row_mul<T, DB, HOLD>(kt, 32 * b, qf);
       if (k0 + KT > least) {
 #pragma unroll
         for (int b = 0; b < NB; ++b) hide(s[b], k0 + 32 * b, sees);
       }
-      online_step<T, DB, NB>(R, s, A.c, kt + L::BYTES, 0);
+      online_step<T, DB, NB, HOLD>(R, s, A.c, kt + L::BYTES, 0);
     }
-    if (k0 + KT < all) put(buf ^ 1);
+    if (k0 + KT < all) put(BUF ^ 1);
     __syncthreads();
+  };
+  for (int k0 = 0; k0 < all; k0 += 2 * KT) {
+    step(k0, std::integral_constant<int, 0>());
+    if (k0 + KT < all) step(k0 + KT, std::integral_constant<int, 1>());
   }
   const float sum = half_sum(R.l);
   store_cols<T, DB>((T*)A.o + qrow * A.os + (int64_t)head * A.d, valid, A.d, R.o, sum == 0.f ? 0.f : 1.f / sum);
@@ -172,10 +179,10 @@ constexpr int64_t slot_floats(int dp) { return (int64_t)kItemRows * dp + 2 * kIt
 template <typename T, int DB>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void k_attn_token(Args A) {
   using L = Tile<T, DB>;
-  extern __shared__ __attribute__((aligned(16))) char lds[];  // a K and a V tile of 32 keys for each wave
+  extern __shared__ __attribute__((aligned(512))) char shared[];  // a K and a V tile of 32 keys for each wave
+  const lds_t lds = lds_start(shared);
   const int l = lane_id(), wave = threadIdx.x >> 6;
-  char* kt = lds + wave * 2 * kUnit * L::PITCH;
-  char* vt = kt + kUnit * L::PITCH;
+  const lds_t kt = lds + wave * 2 * kUnit * L::PITCH, vt = kt + kUnit * L::PITCH;
   const int64_t total = line_total(A), W = min((int64_t)A.waves, total), w = (int64_t)blockIdx.x * 4 + wave;
   if (w >= W) return;
   int64_t a = w * total / W;
@@ -224,7 +231,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void k_attn_token
         __builtin_amdgcn_wave_barrier();
         f32x16 s[1] = {row_mul<T, DB>(kt, 0, qf)};
         if ((u + 1) * kUnit > least) hide(s[0], u * kUnit, sees);
-        online_step<T, DB, 1>(R, s, A.c, vt, 0);
+        online_step<T, DB, 1, false>(R, s, A.c, vt, 0);
         __builtin_amdgcn_wave_barrier();
       }
       const int64_t slot = w + si + j;
@@ -405,7 +412,9 @@ int dnb_attn_create(const dnb_attn_desc* desc, dnb_attn** out) {
   p->slots = p->token ? p->waves + ((d.rows_q * per + kItemRows - 1) / kItemRows + d.sequences) * d.kv_heads : 0;
   p->ws_rowdot = 0;
   p->ws_part = ((size_t)d.rows_q * d.heads * sizeof(float) + 255) / 256 * 256;
-  p->ws_bytes = p->ws_part + (size_t)p->slots * slot_floats(dp) * sizeof(float);
+  const size_t fwd = (size_t)p->slots * slot_floats(dp) * sizeof(float);
+  const size_t bwd = backward_part_bytes(d.rows_q, d.rows_k, d.sequences, d.kv_heads, per, d.head_dim, d.dtype == DNB_BF16);
+  p->ws_bytes = p->ws_part + (fwd > bwd ? fwd : bwd);
   *out = p;
   return DNB_OK;
 }
@@ -446,6 +455,7 @@ int dnb_attn_backward(const dnb_attn* p, const void* q, const void* k, const voi
   A.dq = dq; A.dk = dk; A.dv = dv;
   A.qo = q_offsets; A.ko = k_offsets; A.kl = k_lengths;
   A.rowdot = (float*)((char*)workspace + p->ws_rowdot);
+  A.part = (float*)((char*)workspace + p->ws_part);
   const hipError_t e = launch_backward(A, p->d.dtype == DNB_BF16, (hipStream_t)stream);
   return e == hipSuccess ? DNB_OK : DNB_E_LAUNCH;
 }

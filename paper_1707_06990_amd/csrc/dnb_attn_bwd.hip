@@ -7,6 +7,8 @@
 // over the rows of all heads of a group for 32 keys a wave (the sum over shared heads is part of it).
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "dnb_attn.h"
 
 namespace dnb {
@@ -14,13 +16,15 @@ namespace attn {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kRows = 128;  // packed rows, or keys, of a workgroup, 32 a wave
+constexpr int kRows = 128;  // packed rows of a workgroup of k_attn_dq, 32 a wave
 
 template <typename T, int DB>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void k_attn_dq(Args A) {
   using L = Tile<T, DB>;
   constexpr int KT = L::ROWS, NB = KT / 32;
-  extern __shared__ __attribute__((aligned(16))) char lds[];  // [2][K tile, V tile]
+  constexpr bool HOLD = DB <= 3;
+  extern __shared__ __attribute__((aligned(512))) char shared[];  // [2][K tile, V tile]
+  const lds_t lds = lds_start(shared);
   const int g = blockIdx.x % A.kv, l = lane_id(), wave = threadIdx.x >> 6;
   Seq S;
   int t, count;
@@ -66,6 +70,10 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void k_attn_dq(Ar
     if (v != -INFINITY) lse2 = v * kLog2e;
     if (l < 32) A.rowdot[(int64_t)head * A.rq + qrow] = D;
   }
+  // Rounding ds to bf16 is off by as much as rounding dq itself is; where a row sees few keys, D adds the
+  // rounding of out, which is large there, and so is dq.  Waves that see up to 128 keys multiply what the
+  // rounding left as well.
+  const bool fine = most <= 128;
   f32x16 acc[DB];
 #pragma unroll
   for (int i = 0; i < DB; ++i) acc[i] = (f32x16){};
@@ -87,130 +95,397 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void k_attn_dq(Ar
     put(0);
   }
   __syncthreads();
-  int buf = 0;
-  for (int k0 = 0; k0 < all; k0 += KT, buf ^= 1) {
+  auto step = [&](int k0, auto which) {
+    constexpr int BUF = which;
     if (k0 + KT < all) fetch(k0 + KT);
     if (k0 < most) {
-      const char* kt = lds + buf * 2 * L::BYTES;
+      const lds_t kt = lds + BUF * 2 * L::BYTES;
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
-        f32x16 s = row_mul<T, DB>(kt, 32 * b, qf);
-        const f32x16 dp = row_mul<T, DB>(kt + L::BYTES, 32 * b, df);
+        f32x16 s = row_mul<T, DB, HOLD>(kt, 32 * b, qf);
+        const f32x16 dp = row_mul<T, DB, HOLD>(kt + L::BYTES, 32 * b, df);
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], A.c, -lse2)) * (dp[i] - D);
         if (k0 + 32 * b + 32 > least) {
 #pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (k0 + 32 * b + row_of(i) >= sees) s[i] = 0.f;
+          for (int i = 0; i < 16; ++i) s[i] = k0 + 32 * b + row_of(i) >= sees ? 0.f : s[i];
         }
-        col_mul<T, DB>(kt, 32 * b, s, acc);
+        col_mul<T, DB, HOLD>(kt, 32 * b, s, acc);
+        if (L::BF && fine) {
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[i] -= (float)(__bf16)s[i];
+          col_mul<T, DB, HOLD>(kt, 32 * b, s, acc);
+        }
       }
     }
-    if (k0 + KT < all) put(buf ^ 1);
+    if (k0 + KT < all) put(BUF ^ 1);
     __syncthreads();
+  };
+  for (int k0 = 0; k0 < all; k0 += 2 * KT) {
+    step(k0, std::integral_constant<int, 0>());
+    if (k0 + KT < all) step(k0 + KT, std::integral_constant<int, 1>());
   }
   store_cols<T, DB>((T*)A.dq + qrow * A.qs + (int64_t)head * A.d, valid, A.d, acc, A.scale);
 }
 
+// row_mul with the columns in LDS too: rows brow0 .. brow0 + 31 of tile bt
 template <typename T, int DB>
-__global__ __launch_bounds__(kThreads, 1) void k_attn_dkv(Args A) {
-  using L = Tile<T, DB>;
-  constexpr int QT = L::ROWS, NB = QT / 32;
-  // [2][Q tile, dout tile, lse and D of the rows]
-  extern __shared__ __attribute__((aligned(16))) char lds[];
-  constexpr int BUF = 2 * L::BYTES + 2 * QT * 4;
-  const int g = blockIdx.x % A.kv, l = lane_id(), wave = threadIdx.x >> 6;
-  Seq S;
-  int t, count;
-  if (!find_tile(A, blockIdx.x / A.kv, [&](const Seq& s) { return (s.span + kRows - 1) / kRows; }, &S, &t, &count)) return;
-  const int c0 = t * kRows, w0 = c0 + wave * 32, key = w0 + (l & 31), shift = S.nk - S.nq;
-  const bool valid = key < S.nk;
-  // query i sees key j if j <= i + shift: rows from `first` on see some key of the workgroup
-  const int first = A.causal ? min(max(c0 - shift, 0), S.nq) : 0;
-  const int tiles = c0 < S.nk ? (S.nq - first + QT - 1) / QT : 0, steps = tiles * A.per;
-
-  const int64_t krow = (int64_t)S.k0 + key;
-  Piece kf[L::NS], vf[L::NS];
-  load_cols<T, DB>(kf, (const T*)A.k + krow * A.ks + (int64_t)g * A.d, valid, A.d);
-  load_cols<T, DB>(vf, (const T*)A.v + krow * A.vs + (int64_t)g * A.d, valid, A.d);
-  f32x16 dk[DB], dv[DB];
+__device__ __forceinline__ f32x16 row_mul_lds(lds_t tile, int row0, lds_t bt, int brow0) {
+  const lds_t at = row_address<T, DB>(row0), bat = row_address<T, DB>(brow0);
+  f32x16 s = {};
 #pragma unroll
-  for (int i = 0; i < DB; ++i) dk[i] = dv[i] = (f32x16){};
-
-  Stage<T, DB, QT, kThreads> sq, sd;
-  sq.init(threadIdx.x, A.qs, A.d);
-  sd.init(threadIdx.x, A.os, A.d);
-  float st = 0.f;  // lse of row tid, or D of row tid - QT
-  auto fetch = [&](int step) {
-    const int sub = step / tiles, r0 = first + (step - sub * tiles) * QT, head = g * A.per + sub;
-    const int64_t q0 = (int64_t)S.q0 + r0;
-    sq.load((const T*)A.q + q0 * A.qs + (int64_t)head * A.d, A.qs, S.nq - r0, A.d);
-    sd.load((const T*)A.dout + q0 * A.os + (int64_t)head * A.d, A.os, S.nq - r0, A.d);
-    if ((int)threadIdx.x < 2 * QT) {
-      const int r = threadIdx.x & (QT - 1);
-      const bool is_lse = (int)threadIdx.x < QT;
-      st = is_lse ? INFINITY : 0.f;
-      if (r0 + r < S.nq) {
-        const float x = (is_lse ? A.lse : A.rowdot)[(int64_t)head * A.rq + q0 + r];
-        if (!is_lse) st = x;
-        else if (x != -INFINITY) st = x * kLog2e;
-      }
-    }
-  };
-  auto put = [&](int buf) {
-    char* b = lds + buf * BUF;
-    sq.store(b, threadIdx.x);
-    sd.store(b + L::BYTES, threadIdx.x);
-    if ((int)threadIdx.x < 2 * QT) reinterpret_cast<float*>(b + 2 * L::BYTES)[threadIdx.x] = st;
-  };
-  if (steps > 0) {
-    fetch(0);
-    put(0);
+  for (int k = 0; k < Tile<T, DB>::NS; ++k) {
+    Piece a, b;
+    a.q = lds_read<u32x4>((at ^ (k << 5)) + tile);
+    b.q = lds_read<u32x4>((bat ^ (k << 5)) + bt);
+    mma(s, a, b, (T*)nullptr);
   }
-  __syncthreads();
-  int buf = 0, tile = 0;
-  for (int step = 0; step < steps; ++step, buf ^= 1) {
-    if (step + 1 < steps) fetch(step + 1);
-    const char* qt = lds + buf * BUF;
-    const char* dt = qt + L::BYTES;
-    const float* rows = reinterpret_cast<const float*>(dt + L::BYTES);
+  return s;
+}
+
+constexpr int kQRows = 64;      // packed rows of a step of k_attn_dkv
+constexpr int kItemCost = 192;  // what an item costs beside its rows, in rows
+constexpr int kLeast = 256;     // cost of the smallest part worth a workgroup
+
+// Keys of an item of k_attn_dkv, 32 for each of two waves.  bf16 above head_dim 96: eight waves and 128
+// keys, since the two waves that fit each SIMD have no registers left for more of the rows on their way
+// to LDS than a thread of a large workgroup has.
+constexpr int keys_of(bool bf16, int blocks) { return bf16 && blocks == 4 ? 128 : 64; }
+
+// Items are (sequence, key/value head, KEYS keys), in that order.  An item's cost is the packed rows that see
+// its keys; with a causal mask the first items of a long sequence cost far more than the last, and few
+// key/value heads make few items.  So all items lie on one line, as long as they cost, which is cut into
+// equal parts, one a workgroup; what several workgroups did of one item k_attn_dkv_join adds.
+template <int KEYS>
+struct KeyLine {
+  int64_t nq, nk, per, tiles, used, full;  // tiles of the span; of those in use; of the latter, those that every row sees
+  bool causal;
+  __device__ __forceinline__ KeyLine(const Args& A, const Seq& s) {
+    nq = s.nq; nk = s.nk; per = A.per; causal = A.causal;
+    tiles = (s.span + KEYS - 1) / KEYS;
+    used = (nk + KEYS - 1) / KEYS;
+    const int64_t shift = nk - nq;
+    full = !causal ? used : shift < 0 ? 0 : min(used, shift / KEYS + 1);
+  }
+  // rows that see some key of tile t
+  __device__ __forceinline__ int64_t rows(int64_t t) const { return t >= used ? 0 : (t < full ? nq : min(nq, nk - KEYS * t)) * per; }
+  // cost of the tiles before t
+  __device__ __forceinline__ int64_t before(int64_t t) const {
+    const int64_t u = min(t, used), a = min(u, full);
+    return (a * nq + (u - a) * nk - KEYS * ((u - 1) * u - (a - 1) * a) / 2) * per + kItemCost * t;
+  }
+  // where a cut at x of an item's cost lies in its rows
+  __device__ __forceinline__ int64_t cut(int64_t t, int64_t x) const {
+    const int64_t r = rows(t);
+    if (x >= r + kItemCost) return r;
+    return x <= kItemCost ? 0 : (x - kItemCost) / kQRows * kQRows;
+  }
+};
+
+// Workgroups that take part: none for less than kLeast.
+__device__ __forceinline__ int64_t key_parts(int64_t total, int most) { return max((int64_t)1, min((int64_t)most, total / kLeast)); }
+template <int KEYS>
+__device__ __forceinline__ int64_t key_total(const Args& A) {
+  int64_t u = 0;
+  for (int i = lane_id(); i < A.n; i += 64) {
+    const KeyLine<KEYS> k(A, seq_at(A, i));
+    u += k.before(k.tiles) * A.kv;
+  }
+  return bcast64(wave_scan(u), 63);
+}
+
+// The item at position x of the line (x < key_total), and how far into its cost x is.
+struct KeyAt {
+  Seq s;
+  int g;
+  int64_t t, lo, item;
+};
+template <int KEYS>
+__device__ __forceinline__ KeyAt key_at(const Args& A, int64_t x) {
+  const int l = lane_id();
+  KeyAt r = {};
+  int64_t u0 = 0, i0 = 0;  // cost and items before the 64 sequences at hand
+  for (int base = 0; base < A.n; base += 64) {
+    Seq mine = {};
+    int64_t cost = 0, items = 0;
+    if (base + l < A.n) {
+      mine = seq_at(A, base + l);
+      const KeyLine<KEYS> k(A, mine);
+      cost = k.before(k.tiles) * A.kv;
+      items = k.tiles * A.kv;
+    }
+    const int64_t ue = wave_scan(cost), ie = wave_scan(items);
+    const uint64_t past = __ballot(u0 + ue > x);
+    if (past) {
+      const int at = __builtin_ctzll(past);
+      r.s = bcast(mine, at);
+      const KeyLine<KEYS> line(A, r.s);
+      const int64_t head_cost = line.before(line.tiles), in = x - u0 - bcast64(ue - cost, at);
+      r.g = (int)(in / head_cost);
+      const int64_t off = in - r.g * head_cost;
+      // the last tile that starts at or before off, 64 candidates at a time
+      for (int64_t span = line.tiles; span > 1;) {
+        const int64_t step = (span + 63) / 64;
+        r.t += (__popcll(__ballot(l * step < span && line.before(r.t + l * step) <= off)) - 1) * step;
+        span = min(step, line.tiles - r.t);
+      }
+      r.lo = off - line.before(r.t);
+      r.item = i0 + bcast64(ie - items, at) + r.g * line.tiles + r.t;
+      return r;
+    }
+    u0 += bcast64(ue, 63);
+    i0 += bcast64(ie, 63);
+  }
+  return r;
+}
+
+// Half of the waves takes the first 32 rows of every step, the other half the second, each wave 32 keys;
+// the two sums over the rows are added at the end.  k and v stay in LDS, not in registers: with dk and dv (128 registers at head_dim 128)
+// that leaves room for two waves on each SIMD, one's exponentials under the other's products.
+template <typename T, int DB>
+__global__ __launch_bounds__(4 * keys_of(sizeof(T) == 2, DB), sizeof(T) == 2 || DB <= 2 ? 2 : 1) void k_attn_dkv(Args A) {
+  using L = Tile<T, DB>;
+  constexpr int KEYS = keys_of(sizeof(T) == 2, DB), KB = KEYS / 32, NT = 4 * KEYS;
+  constexpr int KBYTES = KEYS * L::PITCH, QBYTES = kQRows * L::PITCH;
+  extern __shared__ __attribute__((aligned(512))) char shared[];  // k, v, q, dout tiles; lse and D of the rows
+  const lds_t kt = lds_start(shared), vt = kt + KBYTES, qt = vt + KBYTES, dt = qt + QBYTES, rows = dt + QBYTES;
+  const int l = lane_id(), wave = threadIdx.x >> 6, kb = 32 * (wave & (KB - 1)), per = A.per;
+  const bool second = wave >= KB;
+  const int qb = second ? 32 : 0;
+  // x / per for 0 <= x < 64 + per: a quotient of at most 65 and, at per > 64, less than 2, half a step of
+  // 1 / per away from the next whole number, against an fp32 error of 2^-23 of it (per <= 65536)
+  const float inv = 1.f / per;
+  auto over = [&](int x) { return (int)(((float)x + 0.5f) * inv); };
+
+  const int64_t total = key_total<KEYS>(A), W = key_parts(total, A.waves);
+  // neighbours on the line read the same rows: they go to one of the 8 XCDs, whose workgroups are every 8th
+  const int64_t w = W % 8 == 0 ? (int64_t)(blockIdx.x % 8) * (W / 8) + blockIdx.x / 8 : blockIdx.x;
+  if (blockIdx.x >= W) return;
+  int64_t a = w * total / W;
+  const int64_t b = (w + 1) * total / W;
+  // what the search needs is looked up again for every item: it would not fit the registers beside dk and dv
+  while (a < b) {
+    {
+      const KeyAt at = key_at<KEYS>(A, a);
+      const Seq S = at.s;
+      const KeyLine<KEYS> line(A, S);
+      const int g = at.g;
+      const int64_t t = at.t, lo = at.lo, full = line.before(t + 1) - line.before(t), hi = min(full, lo + b - a), item = at.item;
+      a += hi - lo;
+
+      const int c0 = (int)t * KEYS, w0 = c0 + kb, key = w0 + (l & 31), shift = S.nk - S.nq;
+      const bool valid = key < S.nk;
+      // query i sees key j if j <= i + shift: rows from `first` on see some key of the item
+      const int first = A.causal ? min(max(c0 - shift, 0), S.nq) : 0;
+      const int left = (int)line.cut(t, hi);  // packed rows m0 .. left - 1, counted from query `first` on
+      int m0 = (int)line.cut(t, lo);
+      f32x16 dk[DB], dv[DB];
 #pragma unroll
-    for (int b = 0; b < NB; ++b) {
-      const int r0 = first + tile * QT + 32 * b;
-      // uniform in the wave: some row of the block sees some key of the wave
-      if (w0 < S.nk && r0 < S.nq && (!A.causal || r0 + 31 + shift >= w0)) {
-        f32x16 s = row_mul<T, DB>(qt, 32 * b, kf);
-        f32x16 dp = row_mul<T, DB>(dt, 32 * b, vf);
-        const bool edge = w0 + 32 > S.nk || (A.causal && r0 + shift < w0 + 31);
+      for (int i = 0; i < DB; ++i) dk[i] = dv[i] = (f32x16){};
+
+      __syncthreads();  // the item before is done with LDS
+      if (m0 < left) {  // uniform in the workgroup
+        Stage<T, DB, KEYS, NT> sk;
+        sk.init(threadIdx.x, A.ks, A.d);
+        sk.load((const T*)A.k + ((int64_t)S.k0 + c0) * A.ks + (int64_t)g * A.d, A.ks, S.nk - c0, A.d);
+        sk.store(kt, threadIdx.x);
+        sk.init(threadIdx.x, A.vs, A.d);
+        sk.load((const T*)A.v + ((int64_t)S.k0 + c0) * A.vs + (int64_t)g * A.d, A.vs, S.nk - c0, A.d);
+        sk.store(vt, threadIdx.x);
+      }
+      // the first packed row that sees this lane's key; the wave's first key, its last
+      auto first_for = [&](int k) { return A.causal ? (int)min(max(((int64_t)k - shift - first) * per, (int64_t)0), (int64_t)left) : 0; };
+      const int need = valid ? first_for(key) : left, need0 = first_for(w0), need1 = w0 + 32 > S.nk ? left : first_for(w0 + 31);
+      // the step at hand starts at packed row m0: query q0 of the sequence, head s0 of the group
+      int q0 = first + m0 / per, s0 = m0 % per;
+      constexpr int U = kQRows * L::CH / NT;
+      static_assert(kQRows * L::CH % NT == 0, "whole pieces a thread");
+      u32x4 rq[U], rd[U];
+      float st = 0.f;  // threads 0 .. 63: lse of a row, 64 .. 127: D
+      auto fetch = [&](int m, int q, int s) {
+        const auto qr = __builtin_amdgcn_make_buffer_rsrc((T*)A.q + ((int64_t)S.q0 + q) * A.qs + (int64_t)g * per * A.d, 0, 0x7fffffff, 0x00027000);
+        const auto dr = __builtin_amdgcn_make_buffer_rsrc((T*)A.dout + ((int64_t)S.q0 + q) * A.os + (int64_t)g * per * A.d, 0, 0x7fffffff, 0x00027000);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const float4 le = *reinterpret_cast<const float4*>(rows + 32 * b + 8 * q + 4 * (l >> 5));
-          const float4 Dd = *reinterpret_cast<const float4*>(rows + QT + 32 * b + 8 * q + 4 * (l >> 5));
-          const float le_[4] = {le.x, le.y, le.z, le.w}, D_[4] = {Dd.x, Dd.y, Dd.z, Dd.w};
-#pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const float p = __builtin_amdgcn_exp2f(fmaf(s[4 * q + j], A.c, -le_[j]));
-            s[4 * q + j] = p;
-            dp[4 * q + j] = p * (dp[4 * q + j] - D_[j]);
+        for (int u = 0; u < U; ++u) {
+          const int i = threadIdx.x + u * NT, row = i / L::CH, c = i - row * L::CH;
+          const int x = over(s + row), e = (s + row - x * per) * A.d + c * L::EP;
+          const bool ok = m + row < left && c * L::EP < A.d;
+          rq[u] = __builtin_amdgcn_raw_buffer_load_b128(qr, ok ? (uint32_t)(x * (int)A.qs + e) * (uint32_t)sizeof(T) : 0x80000000u, 0, 0);
+          rd[u] = __builtin_amdgcn_raw_buffer_load_b128(dr, ok ? (uint32_t)(x * (int)A.os + e) * (uint32_t)sizeof(T) : 0x80000000u, 0, 0);
+        }
+        if ((int)threadIdx.x < 2 * kQRows) {
+          const int r = threadIdx.x & (kQRows - 1), x = over(s + r);
+          const bool is_lse = (int)threadIdx.x < kQRows;
+          st = is_lse ? INFINITY : 0.f;
+          if (m + r < left) {
+            const float v = (is_lse ? A.lse : A.rowdot)[(int64_t)(g * per + s + r - x * per) * A.rq + S.q0 + q + x];
+            if (!is_lse) st = v;
+            else if (v != -INFINITY) st = v * kLog2e;
           }
         }
-        if (edge) {
-#pragma unroll
-          for (int i = 0; i < 16; ++i)
-            if (!valid || (A.causal && r0 + row_of(i) + shift < key)) s[i] = dp[i] = 0.f;
+      };
+      if (m0 < left) fetch(m0, q0, s0);
+      for (; m0 < left; m0 += kQRows) {
+        __syncthreads();  // the step before is done with the tiles
+        store_pieces<T, DB, U, NT>(qt, threadIdx.x, rq);
+        store_pieces<T, DB, U, NT>(dt, threadIdx.x, rd);
+        if ((int)threadIdx.x < 2 * kQRows) lds_write(rows + 4 * threadIdx.x, st);
+        __syncthreads();
+        s0 += kQRows % per;
+        q0 += kQRows / per;
+        if (s0 >= per) {
+          s0 -= per;
+          ++q0;
         }
-        col_mul<T, DB>(dt, 32 * b, s, dv);
-        col_mul<T, DB>(qt, 32 * b, dp, dk);
+        if (m0 + kQRows < left) fetch(m0 + kQRows, q0, s0);
+        // uniform in the wave: some row of the block sees some key of the wave
+        if (w0 < S.nk && m0 + qb < left && m0 + qb + 31 >= need0) {
+          f32x16 s = row_mul_lds<T, DB>(qt, qb, kt, kb);
+          f32x16 dp = row_mul_lds<T, DB>(dt, qb, vt, kb);
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const f32x4 le = lds_read<f32x4>(rows + 4 * (qb + 8 * q + 4 * (l >> 5)));
+            const f32x4 Dd = lds_read<f32x4>(rows + 4 * (kQRows + qb + 8 * q + 4 * (l >> 5)));
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              const float p = __builtin_amdgcn_exp2f(fmaf(s[4 * q + j], A.c, -le[j]));
+              s[4 * q + j] = p;
+              dp[4 * q + j] = p * (dp[4 * q + j] - Dd[j]);
+            }
+          }
+          if (m0 + qb < need1) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const bool sees = m0 + qb + row_of(i) >= need;
+              s[i] = sees ? s[i] : 0.f;
+              dp[i] = sees ? dp[i] : 0.f;
+            }
+          }
+          col_mul<T, DB>(dt, qb, s, dv);
+          col_mul<T, DB>(qt, qb, dp, dk);
+        }
+      }
+      // The first half of the waves finishes dk, the second dv: each gives the other sum to its partner.
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        f32x16 keep, give;
+        if (second) { keep = dv[db]; give = dk[db]; }
+        else { keep = dk[db]; give = dv[db]; }
+        dk[db] = keep;
+        dv[db] = give;
+      }
+      constexpr int R = DB > 2 ? DB - 2 : DB;  // blocks at a time: what LDS has room for
+#pragma unroll
+      for (int d0 = 0; d0 < DB; d0 += R) {
+        __syncthreads();
+        float4* gives = reinterpret_cast<float4*>(shared) + wave * R * 4 * 64;
+        const float4* takes = reinterpret_cast<const float4*>(shared) + (second ? wave - KB : wave + KB) * R * 4 * 64;
+#pragma unroll
+        for (int db = d0; db < d0 + R && db < DB; ++db)
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            gives[((db - d0) * 4 + q) * 64 + l] = make_float4(dv[db][4 * q], dv[db][4 * q + 1], dv[db][4 * q + 2], dv[db][4 * q + 3]);
+        __syncthreads();
+#pragma unroll
+        for (int db = d0; db < d0 + R && db < DB; ++db)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const float4 x = takes[((db - d0) * 4 + q) * 64 + l];
+            dk[db][4 * q] += x.x;
+            dk[db][4 * q + 1] += x.y;
+            dk[db][4 * q + 2] += x.z;
+            dk[db][4 * q + 3] += x.w;
+          }
+      }
+      if (lo == 0 && hi == full) {  // rows of the sequence's span that are not in use get zeros
+        const int64_t krow = (int64_t)S.k0 + key, to = krow * (second ? A.vs : A.ks) + (int64_t)g * A.d;
+        store_cols<T, DB>((T*)(second ? A.dv : A.dk) + to, key < S.span, A.d, dk, second ? 1.f : A.scale);
+      } else if (w + item < A.slots) {
+        float4* part = reinterpret_cast<float4*>(A.part) + ((w + item) * 2 * KB + wave) * DB * 4 * 64;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+          for (int q = 0; q < 4; ++q)
+            part[(db * 4 + q) * 64 + l] = make_float4(dk[db][4 * q], dk[db][4 * q + 1], dk[db][4 * q + 2], dk[db][4 * q + 3]);
       }
     }
-    if (++tile == tiles) tile = 0;
-    if (step + 1 < steps) put(buf ^ 1);
-    __syncthreads();
   }
-  // rows of the sequence's span that are not in use get zeros
-  const bool own = key < S.span;
-  store_cols<T, DB>((T*)A.dk + krow * A.ks + (int64_t)g * A.d, own, A.d, dk, A.scale);
-  store_cols<T, DB>((T*)A.dv + krow * A.vs + (int64_t)g * A.d, own, A.d, dv, 1.f);
+}
+
+// Adds the parts of an item that several workgroups share, in the line's order; a workgroup an item.
+template <typename T, int DB>
+__global__ __launch_bounds__(4 * keys_of(sizeof(T) == 2, DB)) void k_attn_dkv_join(Args A) {
+  constexpr int KEYS = keys_of(sizeof(T) == 2, DB), KB = KEYS / 32;
+  const int l = lane_id(), wave = threadIdx.x >> 6;
+  int64_t u0 = 0, i0 = 0, su = 0, si = 0;
+  Seq S = {};
+  bool found = false;
+  for (int base = 0; base < A.n; base += 64) {
+    Seq mine = {};
+    int64_t cost = 0, items = 0;
+    if (base + l < A.n) {
+      mine = seq_at(A, base + l);
+      const KeyLine<KEYS> k(A, mine);
+      cost = k.before(k.tiles) * A.kv;
+      items = k.tiles * A.kv;
+    }
+    const int64_t ue = wave_scan(cost), ie = wave_scan(items);
+    const uint64_t past = __ballot(i0 + ie > (int64_t)blockIdx.x);
+    if (past && !found) {
+      const int at = __builtin_ctzll(past);
+      S = bcast(mine, at);
+      su = u0 + bcast64(ue - cost, at);
+      si = i0 + bcast64(ie - items, at);
+      found = true;
+    }
+    u0 += bcast64(ue, 63);
+    i0 += bcast64(ie, 63);
+  }
+  if (!found) return;
+  const KeyLine<KEYS> line(A, S);
+  const int64_t total = u0, W = key_parts(total, A.waves), item = blockIdx.x;
+  const int g = (int)((item - si) / line.tiles);
+  const int64_t t = (item - si) - g * line.tiles;
+  const int64_t from = su + g * line.before(line.tiles) + line.before(t), to = from + line.before(t + 1) - line.before(t);
+  // unit u of the line is workgroup ((u + 1) W - 1) / total's
+  const int64_t w0 = ((from + 1) * W - 1) / total, w1 = (to * W - 1) / total;
+  if (w0 == w1 || w1 + item >= A.slots) return;
+  f32x16 sum[DB];
+#pragma unroll
+  for (int i = 0; i < DB; ++i) sum[i] = (f32x16){};
+  for (int64_t w = w0; w <= w1; ++w) {
+    const float4* part = reinterpret_cast<const float4*>(A.part) + ((w + item) * 2 * KB + wave) * DB * 4 * 64;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const float4 x = part[(db * 4 + q) * 64 + l];
+        sum[db][4 * q] += x.x;
+        sum[db][4 * q + 1] += x.y;
+        sum[db][4 * q + 2] += x.z;
+        sum[db][4 * q + 3] += x.w;
+      }
+  }
+  const bool second = wave >= KB;
+  const int key = (int)t * KEYS + 32 * (wave & (KB - 1)) + (l & 31);
+  const int64_t krow = (int64_t)S.k0 + key, at = krow * (second ? A.vs : A.ks) + (int64_t)g * A.d;
+  store_cols<T, DB>((T*)(second ? A.dv : A.dk) + at, key < S.span, A.d, sum, second ? 1.f : A.scale);
+}
+
+struct KeyPlan {
+  int groups;      // workgroups of k_attn_dkv: as many as 256 compute units hold at once, one each of eight waves or
+                   // of four that take the registers of eight, else two
+  int64_t items;   // at most
+  int64_t slots;   // partial results that may be left: a part's place is its workgroup + its item
+};
+KeyPlan key_plan(int64_t rq, int64_t rk, int n, int kv, int per, int d, bool bf16) {
+  const int blocks = (d + 31) / 32, keys = keys_of(bf16, blocks);
+  const int64_t items = (rk / keys + 1 + n) * kv;
+  const int most = keys == 128 || (!bf16 && blocks > 2) ? 256 : 512;
+  // no item costs more than this: fewer workgroups where all of them together cannot have work for that many
+  const double total = (double)items * ((double)rq * per + kItemCost);
+  const int groups = total / kLeast < most ? (int)(total / kLeast) + 1 : most;
+  return {groups, items, groups > 1 ? groups + items : 0};
 }
 
 template <typename T, int DB>
@@ -223,8 +498,15 @@ hipError_t run(const Args& A, hipStream_t st) {
     if (e != hipSuccess) return e;
   }
   if (A.rk > 0) {
-    const int64_t tiles = (A.rk + kRows - 1) / kRows + A.n;
-    hipLaunchKernelGGL((k_attn_dkv<T, DB>), dim3((unsigned)(tiles * A.kv)), dim3(kThreads), 4 * L::BYTES + 4 * L::ROWS * 4, st, A);
+    constexpr int KEYS = keys_of(sizeof(T) == 2, DB);
+    const KeyPlan p = key_plan(A.rq, A.rk, A.n, A.kv, A.per, A.d, sizeof(T) == 2);
+    Args B = A;
+    B.waves = p.groups;
+    B.slots = p.slots;
+    hipLaunchKernelGGL((k_attn_dkv<T, DB>), dim3((unsigned)p.groups), dim3(4 * KEYS), 2 * (KEYS + kQRows) * L::PITCH + 2 * kQRows * 4, st, B);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    if (p.groups > 1) hipLaunchKernelGGL((k_attn_dkv_join<T, DB>), dim3((unsigned)p.items), dim3(4 * KEYS), 0, st, B);
   }
   return hipGetLastError();
 }
@@ -240,6 +522,11 @@ hipError_t run_db(const Args& A, hipStream_t st) {
 }
 
 }  // namespace
+
+size_t backward_part_bytes(int64_t rq, int64_t rk, int n, int kv, int per, int d, bool bf16) {
+  const int blocks = (d + 31) / 32;
+  return rk > 0 ? (size_t)key_plan(rq, rk, n, kv, per, d, bf16).slots * 2 * keys_of(bf16, blocks) * blocks * 32 * sizeof(float) : 0;
+}
 
 hipError_t launch_backward(const Args& A, bool bf16, hipStream_t st) { return bf16 ? run_db<__bf16>(A, st) : run_db<float>(A, st); }
 

@@ -25,12 +25,13 @@ struct Args {
   void *o, *dq, *dk, *dv;  // o: the forward's output
   float *lse;              // (heads, rows_q)
   float *rowdot;           // backward: sum of dout * out of each row, (heads, rows_q)
-  float *part;             // token form: partial results
+  float *part;             // partial results of work that is split
+
   const int32_t *qo, *ko, *kl;
   int n, heads, kv, per, d, causal;
   int64_t rq, rk, qs, ks, vs, os;
   float scale, c;          // c = scale * log2(e)
-  int waves;               // token form: waves of the launch
+  int waves;               // split work: parts of it, one a wave or a workgroup
   int64_t slots;           //             partial results that `part` has room for
 };
 
@@ -38,6 +39,7 @@ namespace {
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 typedef unsigned short u16;
@@ -104,16 +106,46 @@ __device__ __forceinline__ void mma(f32x16& acc, const Piece& a, const Piece& b,
   for (int j = 0; j < 4; ++j) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a.f[j], b.f[j], acc, 0, 0, 0);
 }
 
+// Addresses in LDS as bytes from its start: what differs between a wave's reads of a tile is then a
+// constant that the instruction holds, or one that is xored to a common address.
+typedef uint32_t lds_t;
+template <typename V>
+__device__ __forceinline__ V lds_read(lds_t at) {
+  return *(const __attribute__((address_space(3))) V*)(uintptr_t)at;
+}
+template <typename V>
+__device__ __forceinline__ void lds_write(lds_t at, const V& v) {
+  *(__attribute__((address_space(3))) V*)(uintptr_t)at = v;
+}
+// The kernels have no LDS but what the launch gives them, which starts at 0: a constant, so that it goes into
+// the instructions (31 additions a step of k_attn less than with the address of the array).
+__device__ __forceinline__ constexpr lds_t lds_start(const void*) { return 0; }
+// Keeps the compiler from holding every address derived from `a` in a register of its own over a whole
+// loop: with dk, dv and a step's tiles in registers there is no room for them, and a spilled address is
+// read back behind the loads of the next tile, for which it then waits.
+// (HOLD: where there is room it may do so, which saves an instruction a read: k_attn, 211 -> 247
+// registers, 452 -> 383 us for 12597 packed queries of 32 heads.)
+template <bool HOLD = false>
+__device__ __forceinline__ lds_t at_hand(lds_t a) {
+  if (!HOLD) asm volatile("" : "+v"(a));
+  return a;
+}
+// piece `half` of row row0 + (lane & 31) of a tile; piece 2k + half is at this ^ (k << 5)
+template <typename T, int DB, bool HOLD = false>
+__device__ __forceinline__ lds_t row_address(int row0) {
+  return at_hand<HOLD>(Tile<T, DB>::at(row0 + (lane_id() & 31), lane_id() >> 5));
+}
+
 // rows row0 .. row0 + 31 of the tile times this wave's columns
-template <typename T, int DB>
-__device__ __forceinline__ f32x16 row_mul(const char* tile, int row0, const Columns<T, DB>& b) {
+template <typename T, int DB, bool HOLD = false>
+__device__ __forceinline__ f32x16 row_mul(lds_t tile, int row0, const Columns<T, DB>& b) {
   using L = Tile<T, DB>;
-  const int r = row0 + (lane_id() & 31), h = lane_id() >> 5;
+  const lds_t at = row_address<T, DB, HOLD>(row0);
   f32x16 s = {};
 #pragma unroll
   for (int k = 0; k < L::NS; ++k) {
     Piece a;
-    a.q = *reinterpret_cast<const u32x4*>(tile + L::at(r, 2 * k + h));
+    a.q = lds_read<u32x4>((at ^ (k << 5)) + tile);
     mma(s, a, b[k], (T*)nullptr);
   }
   return s;
@@ -121,12 +153,13 @@ __device__ __forceinline__ f32x16 row_mul(const char* tile, int row0, const Colu
 
 // bf16: rounding s to 8 bits of mantissa is what feeding the matrix cores at their bf16 rate costs;
 // the sums stay in fp32.
-template <typename T, int DB>
-__device__ __forceinline__ void col_mul(const char* tile, int row0, const f32x16& s, f32x16 (&acc)[DB]) {
+template <typename T, int DB, bool HOLD = false>
+__device__ __forceinline__ void col_mul(lds_t tile, int row0, const f32x16& s, f32x16 (&acc)[DB]) {
   using L = Tile<T, DB>;
   const int l = lane_id();
   if constexpr (L::BF) {
-    const int r = row0 + 4 * (l >> 5) + ((l >> 2) & 3), c = 2 * ((l >> 4) & 1) + ((l >> 1) & 1), o = (l & 1) * 8;
+    // row0 is a multiple of 32: rows 8 on lie at piece ^ 2, rows 16 on at the same pieces
+    const lds_t at = at_hand<HOLD>(L::at(row0 + 4 * (l >> 5) + ((l >> 2) & 3), 2 * ((l >> 4) & 1) + ((l >> 1) & 1)) + (l & 1) * 8);
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       Piece p;
@@ -135,8 +168,8 @@ __device__ __forceinline__ void col_mul(const char* tile, int row0, const f32x16
 #pragma unroll
       for (int db = 0; db < DB; ++db) {
         using lds4 = __attribute__((address_space(3))) s16x4;
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(tile + L::at(r + 16 * t, 4 * db + c) + o));
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(tile + L::at(r + 16 * t + 8, 4 * db + c) + o));
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(uintptr_t)((at ^ (db << 6)) + (tile + 16 * t * L::PITCH)));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(uintptr_t)((at ^ (db << 6) ^ 32) + (tile + (16 * t + 8) * L::PITCH)));
         const uint2 a = __builtin_bit_cast(uint2, lo), b = __builtin_bit_cast(uint2, hi);
         Piece x;
         x.q = (u32x4){a.x, a.y, b.x, b.y};
@@ -144,14 +177,33 @@ __device__ __forceinline__ void col_mul(const char* tile, int row0, const f32x16
       }
     }
   } else {
+const lds_t at = at_hand<HOLD>(L::at(row0 + 4 * (l >> 5), (l & 31) >> 2) + (l & 3) * 4);
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      const int r = row0 + 8 * (i >> 2) + 4 * (l >> 5) + (i & 3);
+      const int r = 8 * (i >> 2) + (i & 3);
 #pragma unroll
       for (int db = 0; db < DB; ++db) {
-        const float x = *reinterpret_cast<const float*>(tile + L::at(r, 8 * db + ((l & 31) >> 2)) + (l & 3) * 4);
+        const float x = lds_read<float>((at ^ (db << 7) ^ (L::swz(r) << 4)) + (tile + r * L::PITCH));
         acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(x, s[i], acc[db], 0, 0, 0);
       }
+    }
+  }
+}
+
+// Pieces tid, tid + NT, ... of a tile's rows
+template <typename T, int DB, int U, int NT>
+__device__ __forceinline__ void store_pieces(lds_t tile, int tid, const u32x4 (&r)[U]) {
+  using L = Tile<T, DB>;
+  if constexpr (NT % L::CH == 0) {
+    constexpr int STEP = NT / L::CH;  // a power of two, above the thread's first row
+    const lds_t at = at_hand(L::at(tid / L::CH, tid % L::CH));
+#pragma unroll
+    for (int u = 0; u < U; ++u) lds_write((at ^ (L::swz(u * STEP) << 4)) + (tile + u * STEP * L::PITCH), r[u]);
+  } else {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = tid + u * NT, row = i / L::CH, c = i - row * L::CH;
+      lds_write(tile + L::at(row, c), r[u]);
     }
   }
 }
@@ -180,12 +232,8 @@ struct Stage {
 #pragma unroll
     for (int u = 0; u < U; ++u) r[u] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, off[u], 0, 0);
   }
-  __device__ __forceinline__ void store(char* tile, int tid) {
-#pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int i = tid + u * NT, row = i / L::CH, c = i - row * L::CH;
-      *reinterpret_cast<u32x4*>(tile + L::at(row, c)) = r[u];
-    }
+  __device__ __forceinline__ void store(lds_t tile, int tid) {
+store_pieces<T, DB, U, NT>(tile, tid, r);
   }
 };
 
