@@ -251,16 +251,17 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void k_attn_token
   }
 }
 
-// Joins an item's parts: a wave for each (query row, head).
+// Joins an item's parts: a workgroup for each (query row, head).  32 lanes (at head_dim 128) hold a row and
+// eight such groups take every eighth part, each with its own running maximum, so that all of its reads are
+// on their way at once: a part comes from another XCD, which takes some 2 us, and a wave that went through
+// 51 parts of a row 8 at a time took 20 us.
 template <typename T, int DB>
 __global__ __launch_bounds__(kThreads) void k_attn_join(Args A) {
-  constexpr int DP = 32 * DB;
+  constexpr int DP = 32 * DB, LANES = DP / 4, G = kThreads / LANES;
+  __shared__ float red[G][DP + 2];
   const int l = lane_id();
-  const int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (id >= A.rq * A.heads) return;
-  const int64_t qrow = id / A.heads;
+  const int64_t id = blockIdx.x, qrow = id / A.heads;
   const int head = (int)(id - qrow * A.heads);
-  // the last sequence that holds the row: offsets are sorted, so it is the only one with rows there
   int64_t u0 = 0, i0 = 0, su = 0, si = 0;
   Seq S = {};
   bool found = false;
@@ -276,8 +277,8 @@ __global__ __launch_bounds__(kThreads) void k_attn_join(Args A) {
     if (holds) {
       const int at = __builtin_ctzll(holds);
       S = bcast(mine, at);
-      su = u0 + bcast64(ue, at) - bcast64(ln.units, at);
-      si = i0 + bcast64(ie, at) - bcast64(ln.items, at);
+      su = u0 + bcast64(ue - ln.units, at);
+      si = i0 + bcast64(ie - ln.items, at);
       found = true;
     }
     u0 += bcast64(ue, 63);
@@ -288,36 +289,55 @@ __global__ __launch_bounds__(kThreads) void k_attn_join(Args A) {
   const int g = head / A.per, m = (int)(qrow - S.q0) * A.per + head - g * A.per, r = m % kItemRows;
   const int len = (S.nk + kUnit - 1) / kUnit;
   const int64_t j = (int64_t)(m / kItemRows) * A.kv + g;
-  float M = -INFINITY, sum = 0.f, o0 = 0.f, o1 = 0.f;
+  const int grp = threadIdx.x / LANES, c = threadIdx.x - grp * LANES;
+  float M = -INFINITY, sum = 0.f;
+  f32x4 o = {};
   if (len > 0) {
     // unit u is wave ((u + 1) W - 1) / total's
-    const int64_t A0 = su + j * len;
-    const int64_t w0 = ((A0 + 1) * W - 1) / total, w1 = ((A0 + len) * W - 1) / total;
+    const int64_t first = su + j * len;
+    const int64_t w0 = ((first + 1) * W - 1) / total, w1 = ((first + len) * W - 1) / total;
+    if (si + j + w1 >= A.slots) return;  // offsets that are not sorted
     const float* p = A.part + (si + j + w0) * slot_floats(DP);
     const int n = (int)(w1 - w0 + 1);
-    if (si + j + w1 >= A.slots) return;  // offsets that are not sorted
-    for (int i = l; i < n; i += 64) M = fmaxf(M, p[i * slot_floats(DP) + kItemRows * DP + r]);
+    if (grp < G) {
+#pragma unroll 8
+      for (int i = grp; i < n; i += G) {
+        const float* q = p + i * slot_floats(DP);
+        const f32x4 v = *reinterpret_cast<const f32x4*>(q + r * DP + 4 * c);
+        const float mi = q[kItemRows * DP + r], li = q[kItemRows * DP + kItemRows + r];
+        const float top = fmaxf(M, mi), t = top == -INFINITY ? 0.f : top;
+        const float a = __builtin_amdgcn_exp2f(M - t), b = __builtin_amdgcn_exp2f(mi - t);
+        M = top;
+        sum = sum * a + li * b;
 #pragma unroll
-    for (int o = 32; o; o >>= 1) M = fmaxf(M, __shfl_xor(M, o));
-    for (int i = 0; i < n; ++i) {
-      const float* q = p + i * slot_floats(DP);
-      const float mi = q[kItemRows * DP + r];
-      const float f = mi == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(mi - M);
-      sum += f * q[kItemRows * DP + kItemRows + r];
-      if (l < DP / 2) {
-        const float2 v = *reinterpret_cast<const float2*>(q + r * DP + 2 * l);
-        o0 += f * v.x;
-        o1 += f * v.y;
+        for (int k = 0; k < 4; ++k) o[k] = o[k] * a + v[k] * b;
       }
     }
   }
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;
-  if (2 * l < A.d) {
-    T* y = (T*)A.o + qrow * A.os + (int64_t)head * A.d + 2 * l;
-    y[0] = (T)(o0 * inv);
-    y[1] = (T)(o1 * inv);
+  if (grp < G) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) red[grp][4 * c + k] = o[k];
+    if (c == 0) {
+      red[grp][DP] = M;
+      red[grp][DP + 1] = sum;
+    }
   }
-  if (l == 0) A.lse[(int64_t)head * A.rq + qrow] = sum == 0.f ? -INFINITY : (M + log2f(sum)) * kLn2;
+  __syncthreads();
+  if (threadIdx.x >= DP) return;
+  M = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < G; ++i) M = fmaxf(M, red[i][DP]);
+  const float t = M == -INFINITY ? 0.f : M;
+  sum = 0.f;
+  float y = 0.f;
+#pragma unroll
+  for (int i = 0; i < G; ++i) {
+    const float f = __builtin_amdgcn_exp2f(red[i][DP] - t);
+    sum = fmaf(red[i][DP + 1], f, sum);
+    y = fmaf(red[i][threadIdx.x], f, y);
+  }
+  if ((int)threadIdx.x < A.d) ((T*)A.o)[qrow * A.os + (int64_t)head * A.d + threadIdx.x] = (T)(sum == 0.f ? 0.f : y / sum);
+  if (threadIdx.x == 0) A.lse[(int64_t)head * A.rq + qrow] = sum == 0.f ? -INFINITY : (M + log2f(sum)) * kLn2;
 }
 
 template <typename T, int DB>
@@ -327,7 +347,7 @@ hipError_t run_forward(const Args& A, bool token, hipStream_t st) {
     hipLaunchKernelGGL((k_attn_token<T, DB>), dim3(A.waves / 4), dim3(kThreads), 8 * kUnit * L::PITCH, st, A);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((k_attn_join<T, DB>), dim3((unsigned)((A.rq * A.heads + 3) / 4)), dim3(kThreads), 0, st, A);
+    hipLaunchKernelGGL((k_attn_join<T, DB>), dim3((unsigned)(A.rq * A.heads)), dim3(kThreads), 0, st, A);
   } else {
     const int64_t tiles = (A.rq * A.per + kRows - 1) / kRows + A.n;
     hipLaunchKernelGGL((k_attn<T, DB>), dim3((unsigned)(tiles * A.kv)), dim3(kThreads), 4 * L::BYTES, st, A);

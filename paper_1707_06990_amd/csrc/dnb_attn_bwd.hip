@@ -194,14 +194,15 @@ __device__ __forceinline__ int64_t key_total(const Args& A) {
   return bcast64(wave_scan(u), 63);
 }
 
-// The item at position x of the line (x < key_total), and how far into its cost x is.
+// The item at position x of the line (x < key_total), and how far into its cost x is; or item number x,
+// items -1 if there are fewer.
 struct KeyAt {
   Seq s;
   int g;
   int64_t t, lo, item;
 };
 template <int KEYS>
-__device__ __forceinline__ KeyAt key_at(const Args& A, int64_t x) {
+__device__ __forceinline__ KeyAt key_at(const Args& A, int64_t x, bool by_item) {
   const int l = lane_id();
   KeyAt r = {};
   int64_t u0 = 0, i0 = 0;  // cost and items before the 64 sequences at hand
@@ -215,11 +216,18 @@ __device__ __forceinline__ KeyAt key_at(const Args& A, int64_t x) {
       items = k.tiles * A.kv;
     }
     const int64_t ue = wave_scan(cost), ie = wave_scan(items);
-    const uint64_t past = __ballot(u0 + ue > x);
+    const uint64_t past = __ballot((by_item ? i0 + ie : u0 + ue) > x);
     if (past) {
       const int at = __builtin_ctzll(past);
       r.s = bcast(mine, at);
       const KeyLine<KEYS> line(A, r.s);
+      if (by_item) {
+        const int64_t in = x - i0 - bcast64(ie - items, at);
+        r.g = (int)(in / line.tiles);
+        r.t = in - r.g * line.tiles;
+        r.item = x;
+        return r;
+      }
       const int64_t head_cost = line.before(line.tiles), in = x - u0 - bcast64(ue - cost, at);
       r.g = (int)(in / head_cost);
       const int64_t off = in - r.g * head_cost;
@@ -236,6 +244,7 @@ __device__ __forceinline__ KeyAt key_at(const Args& A, int64_t x) {
     u0 += bcast64(ue, 63);
     i0 += bcast64(ie, 63);
   }
+  r.item = -1;
   return r;
 }
 
@@ -257,20 +266,25 @@ __global__ __launch_bounds__(4 * keys_of(sizeof(T) == 2, DB), sizeof(T) == 2 || 
   const float inv = 1.f / per;
   auto over = [&](int x) { return (int)(((float)x + 0.5f) * inv); };
 
-  const int64_t total = key_total<KEYS>(A), W = key_parts(total, A.waves);
-  // neighbours on the line read the same rows: they go to one of the 8 XCDs, whose workgroups are every 8th
-  const int64_t w = W % 8 == 0 ? (int64_t)(blockIdx.x % 8) * (W / 8) + blockIdx.x / 8 : blockIdx.x;
-  if (blockIdx.x >= W) return;
-  int64_t a = w * total / W;
-  const int64_t b = (w + 1) * total / W;
+  const bool whole = A.waves == 0;  // a workgroup an item, not a part of the line
+  int64_t w = blockIdx.x, a = 0, b = 1;
+  if (!whole) {
+    const int64_t total = key_total<KEYS>(A), W = key_parts(total, A.waves);
+    if (w >= W) return;
+    // neighbours on the line read the same rows: they go to one of the 8 XCDs, whose workgroups are every 8th
+    if (W % 8 == 0) w = (w % 8) * (W / 8) + w / 8;
+    a = w * total / W;
+    b = (w + 1) * total / W;
+  }
   // what the search needs is looked up again for every item: it would not fit the registers beside dk and dv
   while (a < b) {
     {
-      const KeyAt at = key_at<KEYS>(A, a);
+      const KeyAt at = key_at<KEYS>(A, whole ? w : a, whole);
+      if (at.item < 0) return;
       const Seq S = at.s;
       const KeyLine<KEYS> line(A, S);
       const int g = at.g;
-      const int64_t t = at.t, lo = at.lo, full = line.before(t + 1) - line.before(t), hi = min(full, lo + b - a), item = at.item;
+      const int64_t t = at.t, lo = at.lo, full = line.before(t + 1) - line.before(t), hi = whole ? full : min(full, lo + b - a), item = at.item;
       a += hi - lo;
 
       const int c0 = (int)t * KEYS, w0 = c0 + kb, key = w0 + (l & 31), shift = S.nk - S.nq;
@@ -472,20 +486,21 @@ __global__ __launch_bounds__(4 * keys_of(sizeof(T) == 2, DB)) void k_attn_dkv_jo
   store_cols<T, DB>((T*)(second ? A.dv : A.dk) + at, key < S.span, A.d, sum, second ? 1.f : A.scale);
 }
 
+// How k_attn_dkv is launched.  Up to 512 packed rows (8 steps an item) a workgroup takes an item: a launch
+// less, 13 us for a sequence of 33 rows where the line and its join took 16.  Otherwise the line, in as many
+// parts as 256 compute units hold workgroups at once: one each of eight waves, or of four that take the
+// registers of eight, else two.
 struct KeyPlan {
-  int groups;      // workgroups of k_attn_dkv: as many as 256 compute units hold at once, one each of eight waves or
-                   // of four that take the registers of eight, else two
+  int parts;       // of the line; 0: a workgroup an item
   int64_t items;   // at most
   int64_t slots;   // partial results that may be left: a part's place is its workgroup + its item
 };
 KeyPlan key_plan(int64_t rq, int64_t rk, int n, int kv, int per, int d, bool bf16) {
   const int blocks = (d + 31) / 32, keys = keys_of(bf16, blocks);
   const int64_t items = (rk / keys + 1 + n) * kv;
-  const int most = keys == 128 || (!bf16 && blocks > 2) ? 256 : 512;
-  // no item costs more than this: fewer workgroups where all of them together cannot have work for that many
-  const double total = (double)items * ((double)rq * per + kItemCost);
-  const int groups = total / kLeast < most ? (int)(total / kLeast) + 1 : most;
-  return {groups, items, groups > 1 ? groups + items : 0};
+  if (rq * per <= 512) return {0, items, 0};
+  const int parts = keys == 128 || (!bf16 && blocks > 2) ? 256 : 512;
+  return {parts, items, parts + items};
 }
 
 template <typename T, int DB>
@@ -501,12 +516,12 @@ hipError_t run(const Args& A, hipStream_t st) {
     constexpr int KEYS = keys_of(sizeof(T) == 2, DB);
     const KeyPlan p = key_plan(A.rq, A.rk, A.n, A.kv, A.per, A.d, sizeof(T) == 2);
     Args B = A;
-    B.waves = p.groups;
+    B.waves = p.parts;
     B.slots = p.slots;
-    hipLaunchKernelGGL((k_attn_dkv<T, DB>), dim3((unsigned)p.groups), dim3(4 * KEYS), 2 * (KEYS + kQRows) * L::PITCH + 2 * kQRows * 4, st, B);
+    hipLaunchKernelGGL((k_attn_dkv<T, DB>), dim3((unsigned)(p.parts ? p.parts : p.items)), dim3(4 * KEYS), 2 * (KEYS + kQRows) * L::PITCH + 2 * kQRows * 4, st, B);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    if (p.groups > 1) hipLaunchKernelGGL((k_attn_dkv_join<T, DB>), dim3((unsigned)p.items), dim3(4 * KEYS), 0, st, B);
+    if (p.parts) hipLaunchKernelGGL((k_attn_dkv_join<T, DB>), dim3((unsigned)p.items), dim3(4 * KEYS), 0, st, B);
   }
   return hipGetLastError();
 }
