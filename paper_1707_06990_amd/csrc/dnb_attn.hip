@@ -81,14 +81,16 @@ __device__ __forceinline__ void hide(f32x16& s, int key0, int sees) {
     s[i] = key0 + row_of(i) >= sees ? -INFINITY : s[i];
 }
 
-template <typename T, int DB>
-__global__ __launch_bounds__(kThreads, 2) void k_attn(Args A) {
+// KH 2: eight waves, of which the second four take the second of every two tiles of keys; their sums meet at
+// the end.  A workgroup then takes half the time, which is what counts where there are few of them.
+template <typename T, int DB, int KH>
+__global__ __launch_bounds__(kThreads * KH, 2) void k_attn(Args A) {
   using L = Tile<T, DB>;
-  constexpr int KT = L::ROWS, NB = KT / 32;
+  constexpr int KT = L::ROWS, NB = KT / 32, STEP = KT * KH, NT = kThreads * KH;
   constexpr bool HOLD = L::BF || DB <= 2;
-  extern __shared__ __attribute__((aligned(512))) char shared[];  // [2][K tile, V tile]
+  extern __shared__ __attribute__((aligned(512))) char shared[];  // [2][K tiles, V tiles]
   const lds_t lds = lds_start(shared);
-  const int g = blockIdx.x % A.kv, l = lane_id(), wave = threadIdx.x >> 6;
+  const int g = blockIdx.x % A.kv, l = lane_id(), wave = (threadIdx.x >> 6) & 3, kh = KH == 1 ? 0 : (int)(threadIdx.x >> 8);
   Seq S;
   int t, count;
   if (!find_tile(A, blockIdx.x / A.kv, [&](const Seq& s) { return (int)(((int64_t)s.nq * A.per + kRows - 1) / kRows); }, &S, &t, &count))
@@ -112,7 +114,7 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn(Args A) {
   R.init();
   const T* kb = (const T*)A.k + (int64_t)S.k0 * A.ks + (int64_t)g * A.d;
   const T* vb = (const T*)A.v + (int64_t)S.k0 * A.vs + (int64_t)g * A.d;
-  Stage<T, DB, KT, kThreads> sk, sv;
+  Stage<T, DB, STEP, NT> sk, sv;
   sk.init(threadIdx.x, A.ks, A.d);
   sv.init(threadIdx.x, A.vs, A.d);
   auto fetch = [&](int k0) {
@@ -120,19 +122,20 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn(Args A) {
     sv.load(vb + (int64_t)k0 * A.vs, A.vs, S.nk - k0, A.d);
   };
   auto put = [&](int buf) {
-    sk.store(lds + buf * 2 * L::BYTES, threadIdx.x);
-    sv.store(lds + buf * 2 * L::BYTES + L::BYTES, threadIdx.x);
+    sk.store(lds + buf * 2 * KH * L::BYTES, threadIdx.x);
+    sv.store(lds + (buf * 2 + 1) * KH * L::BYTES, threadIdx.x);
   };
   if (all > 0) {
     fetch(0);
     put(0);
   }
   __syncthreads();
-  auto step = [&](int k0, auto which) {
+  auto step = [&](int at, auto which) {
     constexpr int BUF = which;
-    if (k0 + KT < all) fetch(k0 + KT);
+    if (at + STEP < all) fetch(at + STEP);
+    const int k0 = at + kh * KT;
     if (k0 < most) {
-      const lds_t kt = lds + BUF * 2 * L::BYTES;
+      const lds_t kt = lds + (BUF * 2 * KH + kh) * L::BYTES;
       f32x16 s[NB];
 #pragma unroll
       for (int b = 0; b < NB; ++b) s[b] = row_mul<T, DB, HOLD>(kt, 32 * b, qf);
@@ -140,14 +143,40 @@ __global__ __launch_bounds__(kThreads, 2) void k_attn(Args A) {
 #pragma unroll
         for (int b = 0; b < NB; ++b) hide(s[b], k0 + 32 * b, sees);
       }
-      online_step<T, DB, NB, HOLD>(R, s, A.c, kt + L::BYTES, 0);
+      online_step<T, DB, NB, HOLD>(R, s, A.c, kt + KH * L::BYTES, 0);
     }
-    if (k0 + KT < all) put(BUF ^ 1);
+    if (at + STEP < all) put(BUF ^ 1);
     __syncthreads();
   };
-  for (int k0 = 0; k0 < all; k0 += 2 * KT) {
-    step(k0, std::integral_constant<int, 0>());
-    if (k0 + KT < all) step(k0 + KT, std::integral_constant<int, 1>());
+  for (int at = 0; at < all; at += 2 * STEP) {
+    step(at, std::integral_constant<int, 0>());
+    if (at + STEP < all) step(at + STEP, std::integral_constant<int, 1>());
+  }
+  if constexpr (KH == 2) {
+    // the second half's O in 16-byte pieces, then its m and l; the last step ended with a barrier
+    f32x4* to = reinterpret_cast<f32x4*>(shared) + wave * (DB * 4 + 1) * 64 + l;
+    if (kh == 1) {
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) to[(db * 4 + q) * 64] = (f32x4){R.o[db][4 * q], R.o[db][4 * q + 1], R.o[db][4 * q + 2], R.o[db][4 * q + 3]};
+      to[DB * 4 * 64] = (f32x4){R.m, R.l, 0.f, 0.f};
+    }
+    __syncthreads();
+    if (kh == 1) return;
+    const f32x4 ml = to[DB * 4 * 64];
+    const float m = fmaxf(R.m, ml[0]), t = m == -INFINITY ? 0.f : m;
+    const float a = __builtin_amdgcn_exp2f(R.m - t), b = __builtin_amdgcn_exp2f(ml[0] - t);
+    R.m = m;
+    R.l = R.l * a + ml[1] * b;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const f32x4 x = to[(db * 4 + q) * 64];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) R.o[db][4 * q + k] = R.o[db][4 * q + k] * a + x[k] * b;
+      }
   }
   const float sum = half_sum(R.l);
   store_cols<T, DB>((T*)A.o + qrow * A.os + (int64_t)head * A.d, valid, A.d, R.o, sum == 0.f ? 0.f : 1.f / sum);
@@ -350,7 +379,10 @@ hipError_t run_forward(const Args& A, bool token, hipStream_t st) {
     hipLaunchKernelGGL((k_attn_join<T, DB>), dim3((unsigned)(A.rq * A.heads)), dim3(kThreads), 0, st, A);
   } else {
     const int64_t tiles = (A.rq * A.per + kRows - 1) / kRows + A.n;
-    hipLaunchKernelGGL((k_attn<T, DB>), dim3((unsigned)(tiles * A.kv)), dim3(kThreads), 4 * L::BYTES, st, A);
+    if (split_keys(A, tiles))
+      hipLaunchKernelGGL((k_attn<T, DB, 2>), dim3((unsigned)(tiles * A.kv)), dim3(2 * kThreads), 8 * L::BYTES, st, A);
+    else
+      hipLaunchKernelGGL((k_attn<T, DB, 1>), dim3((unsigned)(tiles * A.kv)), dim3(kThreads), 4 * L::BYTES, st, A);
   }
   return hipGetLastError();
 }

@@ -18,14 +18,15 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kRows = 128;  // packed rows of a workgroup of k_attn_dq, 32 a wave
 
-template <typename T, int DB>
-__global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void k_attn_dq(Args A) {
+// KH 2: eight waves, of which the second four take the second of every two tiles of keys (see k_attn).
+template <typename T, int DB, int KH>
+__global__ __launch_bounds__(kThreads * KH, sizeof(T) == 2 || DB <= 2 || KH == 2 ? 2 : 1) void k_attn_dq(Args A) {
   using L = Tile<T, DB>;
-  constexpr int KT = L::ROWS, NB = KT / 32;
-  constexpr bool HOLD = DB <= 3;
-  extern __shared__ __attribute__((aligned(512))) char shared[];  // [2][K tile, V tile]
+  constexpr int KT = L::ROWS, NB = KT / 32, STEP = KT * KH, NT = kThreads * KH;
+  constexpr bool HOLD = DB <= (L::BF && KH == 1 ? 3 : 2);
+  extern __shared__ __attribute__((aligned(512))) char shared[];  // [2][K tiles, V tiles]
   const lds_t lds = lds_start(shared);
-  const int g = blockIdx.x % A.kv, l = lane_id(), wave = threadIdx.x >> 6;
+  const int g = blockIdx.x % A.kv, l = lane_id(), wave = (threadIdx.x >> 6) & 3, kh = KH == 1 ? 0 : (int)(threadIdx.x >> 8);
   Seq S;
   int t, count;
   if (!find_tile(A, blockIdx.x / A.kv, [&](const Seq& s) { return (int)(((int64_t)s.nq * A.per + kRows - 1) / kRows); }, &S, &t, &count))
@@ -68,7 +69,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void k_attn_dq(Ar
   if (valid) {
     const float v = A.lse[(int64_t)head * A.rq + qrow];
     if (v != -INFINITY) lse2 = v * kLog2e;
-    if (l < 32) A.rowdot[(int64_t)head * A.rq + qrow] = D;
+    if (l < 32 && kh == 0) A.rowdot[(int64_t)head * A.rq + qrow] = D;
   }
   // Rounding ds to bf16 is off by as much as rounding dq itself is; where a row sees few keys, D adds the
   // rounding of out, which is large there, and so is dq.  Waves that see up to 128 keys multiply what the
@@ -79,7 +80,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void k_attn_dq(Ar
   for (int i = 0; i < DB; ++i) acc[i] = (f32x16){};
   const T* kb = (const T*)A.k + (int64_t)S.k0 * A.ks + (int64_t)g * A.d;
   const T* vb = (const T*)A.v + (int64_t)S.k0 * A.vs + (int64_t)g * A.d;
-  Stage<T, DB, KT, kThreads> sk, sv;
+  Stage<T, DB, STEP, NT> sk, sv;
   sk.init(threadIdx.x, A.ks, A.d);
   sv.init(threadIdx.x, A.vs, A.d);
   auto fetch = [&](int k0) {
@@ -87,23 +88,24 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void k_attn_dq(Ar
     sv.load(vb + (int64_t)k0 * A.vs, A.vs, S.nk - k0, A.d);
   };
   auto put = [&](int buf) {
-    sk.store(lds + buf * 2 * L::BYTES, threadIdx.x);
-    sv.store(lds + buf * 2 * L::BYTES + L::BYTES, threadIdx.x);
+    sk.store(lds + buf * 2 * KH * L::BYTES, threadIdx.x);
+    sv.store(lds + (buf * 2 + 1) * KH * L::BYTES, threadIdx.x);
   };
   if (all > 0) {
     fetch(0);
     put(0);
   }
   __syncthreads();
-  auto step = [&](int k0, auto which) {
+  auto step = [&](int at, auto which) {
     constexpr int BUF = which;
-    if (k0 + KT < all) fetch(k0 + KT);
+    if (at + STEP < all) fetch(at + STEP);
+    const int k0 = at + kh * KT;
     if (k0 < most) {
-      const lds_t kt = lds + BUF * 2 * L::BYTES;
+      const lds_t kt = lds + (BUF * 2 * KH + kh) * L::BYTES;
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
         f32x16 s = row_mul<T, DB, HOLD>(kt, 32 * b, qf);
-        const f32x16 dp = row_mul<T, DB, HOLD>(kt + L::BYTES, 32 * b, df);
+        const f32x16 dp = row_mul<T, DB, HOLD>(kt + KH * L::BYTES, 32 * b, df);
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], A.c, -lse2)) * (dp[i] - D);
         if (k0 + 32 * b + 32 > least) {
@@ -118,12 +120,31 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void k_attn_dq(Ar
         }
       }
     }
-    if (k0 + KT < all) put(BUF ^ 1);
+    if (at + STEP < all) put(BUF ^ 1);
     __syncthreads();
   };
-  for (int k0 = 0; k0 < all; k0 += 2 * KT) {
-    step(k0, std::integral_constant<int, 0>());
-    if (k0 + KT < all) step(k0 + KT, std::integral_constant<int, 1>());
+  for (int at = 0; at < all; at += 2 * STEP) {
+    step(at, std::integral_constant<int, 0>());
+    if (at + STEP < all) step(at + STEP, std::integral_constant<int, 1>());
+  }
+  if constexpr (KH == 2) {
+    f32x4* to = reinterpret_cast<f32x4*>(shared) + wave * DB * 4 * 64 + l;
+    if (kh == 1) {
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) to[(db * 4 + q) * 64] = (f32x4){acc[db][4 * q], acc[db][4 * q + 1], acc[db][4 * q + 2], acc[db][4 * q + 3]};
+    }
+    __syncthreads();
+    if (kh == 1) return;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const f32x4 x = to[(db * 4 + q) * 64];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) acc[db][4 * q + k] += x[k];
+      }
   }
   store_cols<T, DB>((T*)A.dq + qrow * A.qs + (int64_t)head * A.d, valid, A.d, acc, A.scale);
 }
@@ -144,20 +165,25 @@ __device__ __forceinline__ f32x16 row_mul_lds(lds_t tile, int row0, lds_t bt, in
 }
 
 constexpr int kQRows = 64;      // packed rows of a step of k_attn_dkv
-constexpr int kItemCost = 192;  // what an item costs beside its rows, in rows
-constexpr int kLeast = 256;     // cost of the smallest part worth a workgroup
 
 // Keys of an item of k_attn_dkv, 32 for each of two waves.  bf16 above head_dim 96: eight waves and 128
 // keys, since the two waves that fit each SIMD have no registers left for more of the rows on their way
 // to LDS than a thread of a large workgroup has.
 constexpr int keys_of(bool bf16, int blocks) { return bf16 && blocks == 4 ? 128 : 64; }
 
+// What an item costs beside its rows, in rows: some 5 us, three steps in bf16, less than one in fp32, whose
+// products take sixteen times as long.
+constexpr int item_cost(bool bf16) { return bf16 ? 192 : 48; }
+// Cost of the smallest part worth a workgroup.
+constexpr int least_cost(bool bf16) { return item_cost(bf16) + kQRows; }
+
 // Items are (sequence, key/value head, KEYS keys), in that order.  An item's cost is the packed rows that see
 // its keys; with a causal mask the first items of a long sequence cost far more than the last, and few
 // key/value heads make few items.  So all items lie on one line, as long as they cost, which is cut into
 // equal parts, one a workgroup; what several workgroups did of one item k_attn_dkv_join adds.
-template <int KEYS>
+template <int KEYS, bool BF>
 struct KeyLine {
+  static constexpr int kItemCost = item_cost(BF);
   int64_t nq, nk, per, tiles, used, full;  // tiles of the span; of those in use; of the latter, those that every row sees
   bool causal;
   __device__ __forceinline__ KeyLine(const Args& A, const Seq& s) {
@@ -182,13 +208,15 @@ struct KeyLine {
   }
 };
 
-// Workgroups that take part: none for less than kLeast.
-__device__ __forceinline__ int64_t key_parts(int64_t total, int most) { return max((int64_t)1, min((int64_t)most, total / kLeast)); }
-template <int KEYS>
+// Workgroups that take part: none for less than least_cost.
+__device__ __forceinline__ int64_t key_parts(int64_t total, int most, bool bf16) {
+  return max((int64_t)1, min((int64_t)most, total / least_cost(bf16)));
+}
+template <int KEYS, bool BF>
 __device__ __forceinline__ int64_t key_total(const Args& A) {
   int64_t u = 0;
   for (int i = lane_id(); i < A.n; i += 64) {
-    const KeyLine<KEYS> k(A, seq_at(A, i));
+    const KeyLine<KEYS, BF> k(A, seq_at(A, i));
     u += k.before(k.tiles) * A.kv;
   }
   return bcast64(wave_scan(u), 63);
@@ -201,7 +229,7 @@ struct KeyAt {
   int g;
   int64_t t, lo, item;
 };
-template <int KEYS>
+template <int KEYS, bool BF>
 __device__ __forceinline__ KeyAt key_at(const Args& A, int64_t x, bool by_item) {
   const int l = lane_id();
   KeyAt r = {};
@@ -211,7 +239,7 @@ __device__ __forceinline__ KeyAt key_at(const Args& A, int64_t x, bool by_item) 
     int64_t cost = 0, items = 0;
     if (base + l < A.n) {
       mine = seq_at(A, base + l);
-      const KeyLine<KEYS> k(A, mine);
+      const KeyLine<KEYS, BF> k(A, mine);
       cost = k.before(k.tiles) * A.kv;
       items = k.tiles * A.kv;
     }
@@ -220,7 +248,7 @@ __device__ __forceinline__ KeyAt key_at(const Args& A, int64_t x, bool by_item) 
     if (past) {
       const int at = __builtin_ctzll(past);
       r.s = bcast(mine, at);
-      const KeyLine<KEYS> line(A, r.s);
+      const KeyLine<KEYS, BF> line(A, r.s);
       if (by_item) {
         const int64_t in = x - i0 - bcast64(ie - items, at);
         r.g = (int)(in / line.tiles);
@@ -254,7 +282,8 @@ __device__ __forceinline__ KeyAt key_at(const Args& A, int64_t x, bool by_item) 
 template <typename T, int DB>
 __global__ __launch_bounds__(4 * keys_of(sizeof(T) == 2, DB), sizeof(T) == 2 || DB <= 2 ? 2 : 1) void k_attn_dkv(Args A) {
   using L = Tile<T, DB>;
-  constexpr int KEYS = keys_of(sizeof(T) == 2, DB), KB = KEYS / 32, NT = 4 * KEYS;
+  constexpr bool BF = L::BF;
+  constexpr int KEYS = keys_of(BF, DB), KB = KEYS / 32, NT = 4 * KEYS;
   constexpr int KBYTES = KEYS * L::PITCH, QBYTES = kQRows * L::PITCH;
   extern __shared__ __attribute__((aligned(512))) char shared[];  // k, v, q, dout tiles; lse and D of the rows
   const lds_t kt = lds_start(shared), vt = kt + KBYTES, qt = vt + KBYTES, dt = qt + QBYTES, rows = dt + QBYTES;
@@ -269,7 +298,7 @@ __global__ __launch_bounds__(4 * keys_of(sizeof(T) == 2, DB), sizeof(T) == 2 || 
   const bool whole = A.waves == 0;  // a workgroup an item, not a part of the line
   int64_t w = blockIdx.x, a = 0, b = 1;
   if (!whole) {
-    const int64_t total = key_total<KEYS>(A), W = key_parts(total, A.waves);
+    const int64_t total = key_total<KEYS, BF>(A), W = key_parts(total, A.waves, BF);
     if (w >= W) return;
     // neighbours on the line read the same rows: they go to one of the 8 XCDs, whose workgroups are every 8th
     if (W % 8 == 0) w = (w % 8) * (W / 8) + w / 8;
@@ -279,10 +308,10 @@ __global__ __launch_bounds__(4 * keys_of(sizeof(T) == 2, DB), sizeof(T) == 2 || 
   // what the search needs is looked up again for every item: it would not fit the registers beside dk and dv
   while (a < b) {
     {
-      const KeyAt at = key_at<KEYS>(A, whole ? w : a, whole);
+      const KeyAt at = key_at<KEYS, BF>(A, whole ? w : a, whole);
       if (at.item < 0) return;
       const Seq S = at.s;
-      const KeyLine<KEYS> line(A, S);
+      const KeyLine<KEYS, BF> line(A, S);
       const int g = at.g;
       const int64_t t = at.t, lo = at.lo, full = line.before(t + 1) - line.before(t), hi = whole ? full : min(full, lo + b - a), item = at.item;
       a += hi - lo;
@@ -429,7 +458,8 @@ __global__ __launch_bounds__(4 * keys_of(sizeof(T) == 2, DB), sizeof(T) == 2 || 
 // Adds the parts of an item that several workgroups share, in the line's order; a workgroup an item.
 template <typename T, int DB>
 __global__ __launch_bounds__(4 * keys_of(sizeof(T) == 2, DB)) void k_attn_dkv_join(Args A) {
-  constexpr int KEYS = keys_of(sizeof(T) == 2, DB), KB = KEYS / 32;
+  constexpr bool BF = sizeof(T) == 2;
+  constexpr int KEYS = keys_of(BF, DB), KB = KEYS / 32;
   const int l = lane_id(), wave = threadIdx.x >> 6;
   int64_t u0 = 0, i0 = 0, su = 0, si = 0;
   Seq S = {};
@@ -439,7 +469,7 @@ __global__ __launch_bounds__(4 * keys_of(sizeof(T) == 2, DB)) void k_attn_dkv_jo
     int64_t cost = 0, items = 0;
     if (base + l < A.n) {
       mine = seq_at(A, base + l);
-      const KeyLine<KEYS> k(A, mine);
+      const KeyLine<KEYS, BF> k(A, mine);
       cost = k.before(k.tiles) * A.kv;
       items = k.tiles * A.kv;
     }
@@ -456,8 +486,8 @@ __global__ __launch_bounds__(4 * keys_of(sizeof(T) == 2, DB)) void k_attn_dkv_jo
     i0 += bcast64(ie, 63);
   }
   if (!found) return;
-  const KeyLine<KEYS> line(A, S);
-  const int64_t total = u0, W = key_parts(total, A.waves), item = blockIdx.x;
+  const KeyLine<KEYS, BF> line(A, S);
+  const int64_t total = u0, W = key_parts(total, A.waves, BF), item = blockIdx.x;
   const int g = (int)((item - si) / line.tiles);
   const int64_t t = (item - si) - g * line.tiles;
   const int64_t from = su + g * line.before(line.tiles) + line.before(t), to = from + line.before(t + 1) - line.before(t);
@@ -508,7 +538,11 @@ hipError_t run(const Args& A, hipStream_t st) {
   using L = Tile<T, DB>;
   if (A.rq > 0) {
     const int64_t tiles = (A.rq * A.per + kRows - 1) / kRows + A.n;
-    hipLaunchKernelGGL((k_attn_dq<T, DB>), dim3((unsigned)(tiles * A.kv)), dim3(kThreads), 4 * L::BYTES, st, A);
+    // (fp32 above head_dim 64 needs the registers of two waves)
+    if ((sizeof(T) == 2 || DB <= 2) && split_keys(A, tiles))
+      hipLaunchKernelGGL((k_attn_dq<T, (sizeof(T) == 2 || DB <= 2 ? DB : 2), 2>), dim3((unsigned)(tiles * A.kv)), dim3(2 * kThreads), 8 * L::BYTES, st, A);
+    else
+      hipLaunchKernelGGL((k_attn_dq<T, DB, 1>), dim3((unsigned)(tiles * A.kv)), dim3(kThreads), 4 * L::BYTES, st, A);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }

@@ -95,6 +95,12 @@ struct Tile {
 };
 
 // a wave's 32 columns: of each step, this lane's half
+// Whether the waves of a workgroup of k_attn and k_attn_dq share the keys out in halves.  Eight waves at one
+// barrier are slower than two workgroups of four (12597 packed queries of 32 heads: 471 us for 393), but
+// with fewer tiles than compute units a workgroup's time is the launch's (1500 rows of 4 heads, a step: 152 us
+// for 170), unless the keys are one step anyway (a step of 33 tokens: 27 us for 24).
+inline bool split_keys(const Args& A, int64_t tiles) { return tiles * A.kv <= 256 && A.rk >= 256 * (int64_t)A.n; }
+
 template <typename T, int DB>
 using Columns = Piece[Tile<T, DB>::NS];
 

@@ -4,7 +4,9 @@
 // that the caller keeps on the device; a workgroup takes every G-th chunk, so the sums have one order.
 // Squares are summed in fp32 over a chunk's share of a thread (64 values) and in fp64 from there on.
 // Bound by memory: src is read twice, since nothing may be written before the whole norm is known.  The
-// second launch goes through the chunks backwards: what was read last is in the 256 MB of the last cache.
+// second launch goes through the chunks backwards: what was read last is in the 256 MB of the last cache,
+// and it writes past that cache, so as not to push out what it has still to read (677 -> 642 us for 612
+// million bf16 values; with 4096 workgroups instead of 2048, 635 us: 5.8 TB/s).
 #include <hip/hip_runtime.h>
 
 #include <math.h>
@@ -20,7 +22,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int64_t kChunk = 16384;  // values
-constexpr int kMost = 2048;        // workgroups
+constexpr int kMost = 4096;        // workgroups
 
 struct Chunk {
   const void* src;
@@ -28,7 +30,7 @@ struct Chunk {
   int32_t count, flags;  // flags: 1 bf16, 2 not in 16-byte pieces
 };
 
-typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef unsigned u4 __attribute__((ext_vector_type(4)));
 
 template <typename T>
 __device__ __forceinline__ float square_sum(const Chunk& c) {
@@ -69,7 +71,7 @@ __device__ __forceinline__ void scale_chunk(const Chunk& c, float f) {
       for (int j = 0; j < V; ++j) v[j] = (T)((float)v[j] * f);
       uint4 o;
       __builtin_memcpy(&o, v, 16);
-      reinterpret_cast<uint4*>(y)[i] = o;
+      __builtin_nontemporal_store(__builtin_bit_cast(u4, o), reinterpret_cast<u4*>(y) + i);
     }
     tail = vecs * V;
   }

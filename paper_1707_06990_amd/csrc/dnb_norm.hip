@@ -38,17 +38,24 @@ __device__ __forceinline__ void load8(float (&v)[8], const T* p) {
     }
   }
 }
-template <typename T>
+// STREAM: past the caches.  The backward pass writes so: its outputs would push out what it has still to
+// read of the forward's (a step of 6272 rows of 2208 fp32: 143 -> 130 us; the forward's outputs so: 136 us).
+template <bool STREAM = false, typename T>
 __device__ __forceinline__ void store8(T* p, const float (&v)[8]) {
+  typedef float f4 __attribute__((ext_vector_type(4)));
+  typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+  auto put = [](auto* q, auto x) {
+    if (STREAM) __builtin_nontemporal_store(x, q);
+    else *q = x;
+  };
   if constexpr (sizeof(T) == 4) {
-    *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-    *reinterpret_cast<float4*>(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
+    put(reinterpret_cast<f4*>(p), (f4){v[0], v[1], v[2], v[3]});
+    put(reinterpret_cast<f4*>(p) + 1, (f4){v[4], v[5], v[6], v[7]});
   } else {
-    typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
     bf16x8 y;
 #pragma unroll
     for (int i = 0; i < 8; ++i) y[i] = (__bf16)v[i];
-    *reinterpret_cast<bf16x8*>(p) = y;
+    put(reinterpret_cast<bf16x8*>(p), y);
   }
 }
 
@@ -220,14 +227,14 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void k_norm_backward(NormArg
     for (int i = 0; i < NV; ++i) {
       if (!in[i]) continue;
       const int c = (t + i * TPR) * 8;
-      if (GATE == DNB_GATE_FULL) store8((T*)A.dgate + at + c, h[i]);
+      if (GATE == DNB_GATE_FULL) store8<true>((T*)A.dgate + at + c, h[i]);
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
         if (POST) dy[i][j] = ib * (dy[i][j] - b[i][j] * m);
         dh[i][j] *= A.scale;
       }
-      store8((T*)A.db + at + c, dy[i]);
-      store8((T*)A.dr + at + c, dh[i]);
+      store8<true>((T*)A.db + at + c, dy[i]);
+      store8<true>((T*)A.dr + at + c, dh[i]);
     }
   }
   // part rows: (workgroup, row of it)
