@@ -40,7 +40,7 @@ struct Online {
 };
 
 // One more set of N blocks of 32 keys: scores s (scaled by c inside), values from `vt`.
-template <typename T, int DB, int N, bool HOLD>
+template <typename T, int DB, int N, bool HOLD, int TR>
 __device__ __forceinline__ void online_step(Online<DB>& S, f32x16 (&s)[N], float c, lds_t vt, int row0) {
   float mx = -INFINITY;
 #pragma unroll
@@ -71,7 +71,7 @@ __device__ __forceinline__ void online_step(Online<DB>& S, f32x16 (&s)[N], float
     S.l += t;
   }
 #pragma unroll
-  for (int b = 0; b < N; ++b) col_mul<T, DB, HOLD>(vt, row0 + 32 * b, s[b], S.o);
+  for (int b = 0; b < N; ++b) col_mul<T, DB, HOLD, TR>(vt, row0 + 32 * b, s[b], S.o);
 }
 
 // Scores of keys key0 + row_of(i) that a query which sees keys below `sees` does not see
@@ -86,9 +86,11 @@ __device__ __forceinline__ void hide(f32x16& s, int key0, int sees) {
 template <typename T, int DB, int KH>
 __global__ __launch_bounds__(kThreads * KH, 2) void k_attn(Args A) {
   using L = Tile<T, DB>;
+  using E = elem_t<T>;
   constexpr int KT = L::ROWS, NB = KT / 32, STEP = KT * KH, NT = kThreads * KH;
-  constexpr bool HOLD = L::BF || DB <= 2;
-  extern __shared__ __attribute__((aligned(512))) char shared[];  // [2][K tiles, V tiles]
+  constexpr bool HOLD = L::PL == 1 || DB <= 2;
+  constexpr int BUFS = buffers<T>(DB);
+  extern __shared__ __attribute__((aligned(512))) char shared[];  // [BUFS][K tiles, V tiles]
   const lds_t lds = lds_start(shared);
   const int g = blockIdx.x % A.kv, l = lane_id(), wave = (threadIdx.x >> 6) & 3, kh = KH == 1 ? 0 : (int)(threadIdx.x >> 8);
   Seq S;
@@ -108,12 +110,12 @@ __global__ __launch_bounds__(kThreads * KH, 2) void k_attn(Args A) {
   const int least = A.causal ? min(max(w0 / A.per + shift + 1, 0), S.nk) : S.nk;
   const int all = A.causal ? min(max(min(m0 + kRows - 1, M - 1) / A.per + shift + 1, 0), S.nk) : S.nk;
 
-  Piece qf[L::NS];
-  load_cols<T, DB>(qf, (const T*)A.q + qrow * A.qs + (int64_t)head * A.d, valid, A.d);
+  Columns<T, DB> qf;
+  load_cols<T, DB>(qf, (const E*)A.q + qrow * A.qs + (int64_t)head * A.d, valid, A.d);
   Online<DB> R;
   R.init();
-  const T* kb = (const T*)A.k + (int64_t)S.k0 * A.ks + (int64_t)g * A.d;
-  const T* vb = (const T*)A.v + (int64_t)S.k0 * A.vs + (int64_t)g * A.d;
+  const E* kb = (const E*)A.k + (int64_t)S.k0 * A.ks + (int64_t)g * A.d;
+  const E* vb = (const E*)A.v + (int64_t)S.k0 * A.vs + (int64_t)g * A.d;
   Stage<T, DB, STEP, NT> sk, sv;
   sk.init(threadIdx.x, A.ks, A.d);
   sv.init(threadIdx.x, A.vs, A.d);
@@ -135,17 +137,20 @@ __global__ __launch_bounds__(kThreads * KH, 2) void k_attn(Args A) {
     if (at + STEP < all) fetch(at + STEP);
     const int k0 = at + kh * KT;
     if (k0 < most) {
-      const lds_t kt = lds + (BUF * 2 * KH + kh) * L::BYTES;
+      const lds_t kt = lds + (BUFS == 1 ? 0 : BUF * 2 * KH * L::BYTES) + kh * KT * L::PITCH;
       f32x16 s[NB];
 #pragma unroll
-      for (int b = 0; b < NB; ++b) s[b] = row_mul<T, DB, HOLD>(kt, 32 * b, qf);
+      for (int b = 0; b < NB; ++b) s[b] = row_mul<T, DB, HOLD, STEP>(kt, 32 * b, qf);
       if (k0 + KT > least) {
 #pragma unroll
         for (int b = 0; b < NB; ++b) hide(s[b], k0 + 32 * b, sees);
       }
-      online_step<T, DB, NB, HOLD>(R, s, A.c, kt + KH * L::BYTES, 0);
+      online_step<T, DB, NB, HOLD, STEP>(R, s, A.c, kt + KH * L::BYTES, 0);
     }
-    if (at + STEP < all) put(BUF ^ 1);
+    if (at + STEP < all) {
+      if (BUFS == 1) __syncthreads();
+      put(BUFS == 1 ? 0 : BUF ^ 1);
+    }
     __syncthreads();
   };
   for (int at = 0; at < all; at += 2 * STEP) {
@@ -179,7 +184,7 @@ __global__ __launch_bounds__(kThreads * KH, 2) void k_attn(Args A) {
       }
   }
   const float sum = half_sum(R.l);
-  store_cols<T, DB>((T*)A.o + qrow * A.os + (int64_t)head * A.d, valid, A.d, R.o, sum == 0.f ? 0.f : 1.f / sum);
+  store_cols<E, DB>((E*)A.o + qrow * A.os + (int64_t)head * A.d, valid, A.d, R.o, sum == 0.f ? 0.f : 1.f / sum);
   if (valid && l < 32) A.lse[(int64_t)head * A.rq + qrow] = sum == 0.f ? -INFINITY : (R.m + log2f(sum)) * kLn2;
 }
 
@@ -241,7 +246,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void k_attn_token
       const bool valid = m < M;
       const int sees = A.causal ? min(max(row + S.nk - S.nq + 1, 0), S.nk) : S.nk;
       const int least = A.causal ? min(max(m0 / A.per + S.nk - S.nq + 1, 0), S.nk) : S.nk;
-      Piece qf[L::NS];
+      Columns<T, DB> qf;
       load_cols<T, DB>(qf, (const T*)A.q + ((int64_t)S.q0 + row) * A.qs + (int64_t)head * A.d, valid, A.d);
       Online<DB> R;
       R.init();
@@ -258,9 +263,9 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void k_attn_token
         sv.store(vt, l);
         if (u + 1 < last) fetch(u + 1);
         __builtin_amdgcn_wave_barrier();
-        f32x16 s[1] = {row_mul<T, DB>(kt, 0, qf)};
+        f32x16 s[1] = {row_mul<T, DB, false, kUnit>(kt, 0, qf)};
         if ((u + 1) * kUnit > least) hide(s[0], u * kUnit, sees);
-        online_step<T, DB, 1, false>(R, s, A.c, vt, 0);
+        online_step<T, DB, 1, false, kUnit>(R, s, A.c, vt, 0);
         __builtin_amdgcn_wave_barrier();
       }
       const int64_t slot = w + si + j;
@@ -371,19 +376,21 @@ __global__ __launch_bounds__(kThreads) void k_attn_join(Args A) {
 
 template <typename T, int DB>
 hipError_t run_forward(const Args& A, bool token, hipStream_t st) {
-  using L = Tile<T, DB>;
   if (token) {
-    hipLaunchKernelGGL((k_attn_token<T, DB>), dim3(A.waves / 4), dim3(kThreads), 8 * kUnit * L::PITCH, st, A);
+    constexpr int PITCH = Tile<T, DB>::PITCH;
+    hipLaunchKernelGGL((k_attn_token<T, DB>), dim3(A.waves / 4), dim3(kThreads), 8 * kUnit * PITCH, st, A);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     hipLaunchKernelGGL((k_attn_join<T, DB>), dim3((unsigned)(A.rq * A.heads)), dim3(kThreads), 0, st, A);
-  } else {
-    const int64_t tiles = (A.rq * A.per + kRows - 1) / kRows + A.n;
-    if (split_keys(A, tiles))
-      hipLaunchKernelGGL((k_attn<T, DB, 2>), dim3((unsigned)(tiles * A.kv)), dim3(2 * kThreads), 8 * L::BYTES, st, A);
-    else
-      hipLaunchKernelGGL((k_attn<T, DB, 1>), dim3((unsigned)(tiles * A.kv)), dim3(kThreads), 4 * L::BYTES, st, A);
+    return hipGetLastError();
   }
+  using M = typename std::conditional<std::is_same<T, float>::value, Split, T>::type;
+  constexpr int BYTES = Tile<M, DB>::BYTES;
+  const int64_t tiles = (A.rq * A.per + kRows - 1) / kRows + A.n;
+  if (split_keys(A, tiles))
+    hipLaunchKernelGGL((k_attn<M, DB, 2>), dim3((unsigned)(tiles * A.kv)), dim3(2 * kThreads), 4 * buffers<M>(DB) * BYTES, st, A);
+  else
+    hipLaunchKernelGGL((k_attn<M, DB, 1>), dim3((unsigned)(tiles * A.kv)), dim3(kThreads), 2 * buffers<M>(DB) * BYTES, st, A);
   return hipGetLastError();
 }
 

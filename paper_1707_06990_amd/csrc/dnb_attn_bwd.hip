@@ -18,12 +18,17 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kRows = 128;  // packed rows of a workgroup of k_attn_dq, 32 a wave
 
+// Two rows of registers for q and dout: above head_dim 64 Split takes those of two waves.
+template <typename T>
+constexpr bool crowded(int blocks) { return std::is_same<T, Split>::value && blocks > 2; }
+
 // KH 2: eight waves, of which the second four take the second of every two tiles of keys (see k_attn).
 template <typename T, int DB, int KH>
-__global__ __launch_bounds__(kThreads * KH, sizeof(T) == 2 || DB <= 2 || KH == 2 ? 2 : 1) void k_attn_dq(Args A) {
+__global__ __launch_bounds__(kThreads * KH, crowded<T>(DB) ? 1 : 2) void k_attn_dq(Args A) {
   using L = Tile<T, DB>;
+  using E = elem_t<T>;
   constexpr int KT = L::ROWS, NB = KT / 32, STEP = KT * KH, NT = kThreads * KH;
-  constexpr bool HOLD = DB <= (L::BF && KH == 1 ? 3 : 2);
+  constexpr bool HOLD = DB <= (L::PL == 1 && KH == 1 ? 3 : 2);
   extern __shared__ __attribute__((aligned(512))) char shared[];  // [2][K tiles, V tiles]
   const lds_t lds = lds_start(shared);
   const int g = blockIdx.x % A.kv, l = lane_id(), wave = (threadIdx.x >> 6) & 3, kh = KH == 1 ? 0 : (int)(threadIdx.x >> 8);
@@ -43,27 +48,10 @@ __global__ __launch_bounds__(kThreads * KH, sizeof(T) == 2 || DB <= 2 || KH == 2
   const int least = A.causal ? min(max(w0 / A.per + shift + 1, 0), S.nk) : S.nk;
   const int all = A.causal ? min(max(min(m0 + kRows - 1, M - 1) / A.per + shift + 1, 0), S.nk) : S.nk;
 
-  Piece qf[L::NS], df[L::NS];
-  load_cols<T, DB>(qf, (const T*)A.q + qrow * A.qs + (int64_t)head * A.d, valid, A.d);
-  load_cols<T, DB>(df, (const T*)A.dout + qrow * A.os + (int64_t)head * A.d, valid, A.d);
-  // D of this lane's row: each half of the wave has half of the pieces
-  float D = 0.f;
-  {
-    const T* o = (const T*)A.out + qrow * A.os + (int64_t)head * A.d;
-#pragma unroll
-    for (int k = 0; k < L::NS; ++k) {
-      const int e = (2 * k + (l >> 5)) * L::EP;
-      Piece x;
-      x.q = (u32x4){0u, 0u, 0u, 0u};
-      if (valid && e < A.d) x.q = *reinterpret_cast<const u32x4*>(o + e);
-#pragma unroll
-      for (int j = 0; j < L::EP; ++j) {
-        if constexpr (L::BF) D = fmaf((float)x.b[j], (float)df[k].b[j], D);
-        else D = fmaf(x.f[j], df[k].f[j], D);
-      }
-    }
-    D = half_sum(D);
-  }
+  Columns<T, DB> qf, df;
+  load_cols<T, DB>(qf, (const E*)A.q + qrow * A.qs + (int64_t)head * A.d, valid, A.d);
+  load_cols<T, DB>(df, (const E*)A.dout + qrow * A.os + (int64_t)head * A.d, valid, A.d);
+  const float D = dot_rows<T, DB>((const E*)A.out + qrow * A.os + (int64_t)head * A.d, (const E*)A.dout + qrow * A.os + (int64_t)head * A.d, valid, A.d);
   // lse = -inf: the row sees no key, and none of its p may be anything but 0
   float lse2 = INFINITY;
   if (valid) {
@@ -78,8 +66,8 @@ __global__ __launch_bounds__(kThreads * KH, sizeof(T) == 2 || DB <= 2 || KH == 2
   f32x16 acc[DB];
 #pragma unroll
   for (int i = 0; i < DB; ++i) acc[i] = (f32x16){};
-  const T* kb = (const T*)A.k + (int64_t)S.k0 * A.ks + (int64_t)g * A.d;
-  const T* vb = (const T*)A.v + (int64_t)S.k0 * A.vs + (int64_t)g * A.d;
+  const E* kb = (const E*)A.k + (int64_t)S.k0 * A.ks + (int64_t)g * A.d;
+  const E* vb = (const E*)A.v + (int64_t)S.k0 * A.vs + (int64_t)g * A.d;
   Stage<T, DB, STEP, NT> sk, sv;
   sk.init(threadIdx.x, A.ks, A.d);
   sv.init(threadIdx.x, A.vs, A.d);
@@ -101,22 +89,22 @@ __global__ __launch_bounds__(kThreads * KH, sizeof(T) == 2 || DB <= 2 || KH == 2
     if (at + STEP < all) fetch(at + STEP);
     const int k0 = at + kh * KT;
     if (k0 < most) {
-      const lds_t kt = lds + (BUF * 2 * KH + kh) * L::BYTES;
+      const lds_t kt = lds + BUF * 2 * KH * L::BYTES + kh * KT * L::PITCH;
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
-        f32x16 s = row_mul<T, DB, HOLD>(kt, 32 * b, qf);
-        const f32x16 dp = row_mul<T, DB, HOLD>(kt + KH * L::BYTES, 32 * b, df);
+        f32x16 s = row_mul<T, DB, HOLD, STEP>(kt, 32 * b, qf);
+        const f32x16 dp = row_mul<T, DB, HOLD, STEP>(kt + KH * L::BYTES, 32 * b, df);
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], A.c, -lse2)) * (dp[i] - D);
         if (k0 + 32 * b + 32 > least) {
 #pragma unroll
           for (int i = 0; i < 16; ++i) s[i] = k0 + 32 * b + row_of(i) >= sees ? 0.f : s[i];
         }
-        col_mul<T, DB, HOLD>(kt, 32 * b, s, acc);
-        if (L::BF && fine) {
+        col_mul<T, DB, HOLD, STEP>(kt, 32 * b, s, acc);
+        if (sizeof(E) == 2 && fine) {
 #pragma unroll
           for (int i = 0; i < 16; ++i) s[i] -= (float)(__bf16)s[i];
-          col_mul<T, DB, HOLD>(kt, 32 * b, s, acc);
+          col_mul<T, DB, HOLD, STEP>(kt, 32 * b, s, acc);
         }
       }
     }
@@ -146,19 +134,23 @@ __global__ __launch_bounds__(kThreads * KH, sizeof(T) == 2 || DB <= 2 || KH == 2
         for (int k = 0; k < 4; ++k) acc[db][4 * q + k] += x[k];
       }
   }
-  store_cols<T, DB>((T*)A.dq + qrow * A.qs + (int64_t)head * A.d, valid, A.d, acc, A.scale);
+  store_cols<E, DB>((E*)A.dq + qrow * A.qs + (int64_t)head * A.d, valid, A.d, acc, A.scale);
 }
 
-// row_mul with the columns in LDS too: rows brow0 .. brow0 + 31 of tile bt
-template <typename T, int DB>
+// row_mul with the columns in LDS too: rows brow0 .. brow0 + 31 of tile bt, of BR rows
+template <typename T, int DB, int TR, int BR>
 __device__ __forceinline__ f32x16 row_mul_lds(lds_t tile, int row0, lds_t bt, int brow0) {
+  using L = Tile<T, DB>;
   const lds_t at = row_address<T, DB>(row0), bat = row_address<T, DB>(brow0);
   f32x16 s = {};
 #pragma unroll
-  for (int k = 0; k < Tile<T, DB>::NS; ++k) {
-    Piece a, b;
-    a.q = lds_read<u32x4>((at ^ (k << 5)) + tile);
-    b.q = lds_read<u32x4>((bat ^ (k << 5)) + bt);
+  for (int k = 0; k < L::NS; ++k) {
+    Pieces<T, DB> a, b;
+#pragma unroll
+    for (int p = 0; p < L::PL; ++p) {
+      a[p].q = lds_read<u32x4>((at ^ (k << 5)) + (tile + p * TR * L::PITCH));
+      b[p].q = lds_read<u32x4>((bat ^ (k << 5)) + (bt + p * BR * L::PITCH));
+    }
     mma(s, a, b, (T*)nullptr);
   }
   return s;
@@ -168,8 +160,9 @@ constexpr int kQRows = 64;      // packed rows of a step of k_attn_dkv
 
 // Keys of an item of k_attn_dkv, 32 for each of two waves.  bf16 above head_dim 96: eight waves and 128
 // keys, since the two waves that fit each SIMD have no registers left for more of the rows on their way
-// to LDS than a thread of a large workgroup has.
-constexpr int keys_of(bool bf16, int blocks) { return bf16 && blocks == 4 ? 128 : 64; }
+// to LDS than a thread of a large workgroup has.  fp32 up to 64: eight, since LDS holds one workgroup's
+// tiles; above: four, with k and v in registers, since LDS holds no more than the rows' tiles.
+constexpr int keys_of(bool bf16, int blocks) { return bf16 ? (blocks == 4 ? 128 : 64) : blocks <= 2 ? 128 : 64; }
 
 // What an item costs beside its rows, in rows: some 5 us, three steps in bf16, less than one in fp32, whose
 // products take sixteen times as long.
@@ -280,12 +273,13 @@ __device__ __forceinline__ KeyAt key_at(const Args& A, int64_t x, bool by_item) 
 // the two sums over the rows are added at the end.  k and v stay in LDS, not in registers: with dk and dv (128 registers at head_dim 128)
 // that leaves room for two waves on each SIMD, one's exponentials under the other's products.
 template <typename T, int DB>
-__global__ __launch_bounds__(4 * keys_of(sizeof(T) == 2, DB), sizeof(T) == 2 || DB <= 2 ? 2 : 1) void k_attn_dkv(Args A) {
+__global__ __launch_bounds__(4 * keys_of(sizeof(elem_t<T>) == 2, DB), crowded<T>(DB) ? 1 : 2) void k_attn_dkv(Args A) {
   using L = Tile<T, DB>;
-  constexpr bool BF = L::BF;
+  using E = elem_t<T>;
+  constexpr bool BF = sizeof(E) == 2, COLS = crowded<T>(DB);
   constexpr int KEYS = keys_of(BF, DB), KB = KEYS / 32, NT = 4 * KEYS;
-  constexpr int KBYTES = KEYS * L::PITCH, QBYTES = kQRows * L::PITCH;
-  extern __shared__ __attribute__((aligned(512))) char shared[];  // k, v, q, dout tiles; lse and D of the rows
+  constexpr int KBYTES = COLS ? 0 : KEYS * L::PITCH * L::PL, QBYTES = kQRows * L::PITCH * L::PL;
+  extern __shared__ __attribute__((aligned(512))) char shared[];  // k and v tiles unless COLS, q and dout tiles; lse and D of the rows
   const lds_t kt = lds_start(shared), vt = kt + KBYTES, qt = vt + KBYTES, dt = qt + QBYTES, rows = dt + QBYTES;
   const int l = lane_id(), wave = threadIdx.x >> 6, kb = 32 * (wave & (KB - 1)), per = A.per;
   const bool second = wave >= KB;
@@ -327,13 +321,18 @@ __global__ __launch_bounds__(4 * keys_of(sizeof(T) == 2, DB), sizeof(T) == 2 || 
       for (int i = 0; i < DB; ++i) dk[i] = dv[i] = (f32x16){};
 
       __syncthreads();  // the item before is done with LDS
-      if (m0 < left) {  // uniform in the workgroup
+      Columns<T, DB> kf, vf;
+      if (COLS) {
+        const int64_t krow = (int64_t)S.k0 + key;
+        load_cols<T, DB>(kf, (const E*)A.k + krow * A.ks + (int64_t)g * A.d, valid && m0 < left, A.d);
+        load_cols<T, DB>(vf, (const E*)A.v + krow * A.vs + (int64_t)g * A.d, valid && m0 < left, A.d);
+      } else if (m0 < left) {  // uniform in the workgroup
         Stage<T, DB, KEYS, NT> sk;
         sk.init(threadIdx.x, A.ks, A.d);
-        sk.load((const T*)A.k + ((int64_t)S.k0 + c0) * A.ks + (int64_t)g * A.d, A.ks, S.nk - c0, A.d);
+        sk.load((const E*)A.k + ((int64_t)S.k0 + c0) * A.ks + (int64_t)g * A.d, A.ks, S.nk - c0, A.d);
         sk.store(kt, threadIdx.x);
         sk.init(threadIdx.x, A.vs, A.d);
-        sk.load((const T*)A.v + ((int64_t)S.k0 + c0) * A.vs + (int64_t)g * A.d, A.vs, S.nk - c0, A.d);
+        sk.load((const E*)A.v + ((int64_t)S.k0 + c0) * A.vs + (int64_t)g * A.d, A.vs, S.nk - c0, A.d);
         sk.store(vt, threadIdx.x);
       }
       // the first packed row that sees this lane's key; the wave's first key, its last
@@ -341,20 +340,24 @@ __global__ __launch_bounds__(4 * keys_of(sizeof(T) == 2, DB), sizeof(T) == 2 || 
       const int need = valid ? first_for(key) : left, need0 = first_for(w0), need1 = w0 + 32 > S.nk ? left : first_for(w0 + 31);
       // the step at hand starts at packed row m0: query q0 of the sequence, head s0 of the group
       int q0 = first + m0 / per, s0 = m0 % per;
-      constexpr int U = kQRows * L::CH / NT;
-      static_assert(kQRows * L::CH % NT == 0, "whole pieces a thread");
-      u32x4 rq[U], rd[U];
+      constexpr int U = (kQRows * L::CH + NT - 1) / NT;
+      u32x4 rq[U * L::LD], rd[U * L::LD];
       float st = 0.f;  // threads 0 .. 63: lse of a row, 64 .. 127: D
       auto fetch = [&](int m, int q, int s) {
-        const auto qr = __builtin_amdgcn_make_buffer_rsrc((T*)A.q + ((int64_t)S.q0 + q) * A.qs + (int64_t)g * per * A.d, 0, 0x7fffffff, 0x00027000);
-        const auto dr = __builtin_amdgcn_make_buffer_rsrc((T*)A.dout + ((int64_t)S.q0 + q) * A.os + (int64_t)g * per * A.d, 0, 0x7fffffff, 0x00027000);
+        const auto qr = __builtin_amdgcn_make_buffer_rsrc((E*)A.q + ((int64_t)S.q0 + q) * A.qs + (int64_t)g * per * A.d, 0, 0x7fffffff, 0x00027000);
+        const auto dr = __builtin_amdgcn_make_buffer_rsrc((E*)A.dout + ((int64_t)S.q0 + q) * A.os + (int64_t)g * per * A.d, 0, 0x7fffffff, 0x00027000);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
           const int i = threadIdx.x + u * NT, row = i / L::CH, c = i - row * L::CH;
           const int x = over(s + row), e = (s + row - x * per) * A.d + c * L::EP;
-          const bool ok = m + row < left && c * L::EP < A.d;
-          rq[u] = __builtin_amdgcn_raw_buffer_load_b128(qr, ok ? (uint32_t)(x * (int)A.qs + e) * (uint32_t)sizeof(T) : 0x80000000u, 0, 0);
-          rd[u] = __builtin_amdgcn_raw_buffer_load_b128(dr, ok ? (uint32_t)(x * (int)A.os + e) * (uint32_t)sizeof(T) : 0x80000000u, 0, 0);
+          const bool ok = row < kQRows && m + row < left && c * L::EP < A.d;
+          const uint32_t oq = ok ? (uint32_t)(x * (int)A.qs + e) * (uint32_t)sizeof(E) : 0x80000000u;
+          const uint32_t od = ok ? (uint32_t)(x * (int)A.os + e) * (uint32_t)sizeof(E) : 0x80000000u;
+#pragma unroll
+          for (int p = 0; p < L::LD; ++p) {
+            rq[u * L::LD + p] = __builtin_amdgcn_raw_buffer_load_b128(qr, oq + 16 * p, 0, 0);
+            rd[u * L::LD + p] = __builtin_amdgcn_raw_buffer_load_b128(dr, od + 16 * p, 0, 0);
+          }
         }
         if ((int)threadIdx.x < 2 * kQRows) {
           const int r = threadIdx.x & (kQRows - 1), x = over(s + r);
@@ -370,8 +373,8 @@ __global__ __launch_bounds__(4 * keys_of(sizeof(T) == 2, DB), sizeof(T) == 2 || 
       if (m0 < left) fetch(m0, q0, s0);
       for (; m0 < left; m0 += kQRows) {
         __syncthreads();  // the step before is done with the tiles
-        store_pieces<T, DB, U, NT>(qt, threadIdx.x, rq);
-        store_pieces<T, DB, U, NT>(dt, threadIdx.x, rd);
+        store_pieces<T, DB, U, NT, kQRows>(qt, threadIdx.x, rq);
+        store_pieces<T, DB, U, NT, kQRows>(dt, threadIdx.x, rd);
         if ((int)threadIdx.x < 2 * kQRows) lds_write(rows + 4 * threadIdx.x, st);
         __syncthreads();
         s0 += kQRows % per;
@@ -383,8 +386,14 @@ __global__ __launch_bounds__(4 * keys_of(sizeof(T) == 2, DB), sizeof(T) == 2 || 
         if (m0 + kQRows < left) fetch(m0 + kQRows, q0, s0);
         // uniform in the wave: some row of the block sees some key of the wave
         if (w0 < S.nk && m0 + qb < left && m0 + qb + 31 >= need0) {
-          f32x16 s = row_mul_lds<T, DB>(qt, qb, kt, kb);
-          f32x16 dp = row_mul_lds<T, DB>(dt, qb, vt, kb);
+          f32x16 s, dp;
+          if constexpr (COLS) {
+            s = row_mul<T, DB, false, kQRows>(qt, qb, kf);
+            dp = row_mul<T, DB, false, kQRows>(dt, qb, vf);
+          } else {
+            s = row_mul_lds<T, DB, kQRows, KEYS>(qt, qb, kt, kb);
+            dp = row_mul_lds<T, DB, kQRows, KEYS>(dt, qb, vt, kb);
+          }
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
             const f32x4 le = lds_read<f32x4>(rows + 4 * (qb + 8 * q + 4 * (l >> 5)));
@@ -404,8 +413,8 @@ __global__ __launch_bounds__(4 * keys_of(sizeof(T) == 2, DB), sizeof(T) == 2 || 
               dp[i] = sees ? dp[i] : 0.f;
             }
           }
-          col_mul<T, DB>(dt, qb, s, dv);
-          col_mul<T, DB>(qt, qb, dp, dk);
+          col_mul<T, DB, false, kQRows>(dt, qb, s, dv);
+          col_mul<T, DB, false, kQRows>(qt, qb, dp, dk);
         }
       }
       // The first half of the waves finishes dk, the second dv: each gives the other sum to its partner.
@@ -442,7 +451,7 @@ __global__ __launch_bounds__(4 * keys_of(sizeof(T) == 2, DB), sizeof(T) == 2 || 
       }
       if (lo == 0 && hi == full) {  // rows of the sequence's span that are not in use get zeros
         const int64_t krow = (int64_t)S.k0 + key, to = krow * (second ? A.vs : A.ks) + (int64_t)g * A.d;
-        store_cols<T, DB>((T*)(second ? A.dv : A.dk) + to, key < S.span, A.d, dk, second ? 1.f : A.scale);
+        store_cols<E, DB>((E*)(second ? A.dv : A.dk) + to, key < S.span, A.d, dk, second ? 1.f : A.scale);
       } else if (w + item < A.slots) {
         float4* part = reinterpret_cast<float4*>(A.part) + ((w + item) * 2 * KB + wave) * DB * 4 * 64;
 #pragma unroll
@@ -529,33 +538,34 @@ KeyPlan key_plan(int64_t rq, int64_t rk, int n, int kv, int per, int d, bool bf1
   const int blocks = (d + 31) / 32, keys = keys_of(bf16, blocks);
   const int64_t items = (rk / keys + 1 + n) * kv;
   if (rq * per <= 512) return {0, items, 0};
-  const int parts = keys == 128 || (!bf16 && blocks > 2) ? 256 : 512;
+  const int parts = bf16 && keys == 64 ? 512 : 256;
   return {parts, items, parts + items};
 }
 
-template <typename T, int DB>
+template <typename E, int DB>
 hipError_t run(const Args& A, hipStream_t st) {
+  using T = typename std::conditional<std::is_same<E, float>::value, Split, E>::type;
   using L = Tile<T, DB>;
   if (A.rq > 0) {
     const int64_t tiles = (A.rq * A.per + kRows - 1) / kRows + A.n;
-    // (fp32 above head_dim 64 needs the registers of two waves)
-    if ((sizeof(T) == 2 || DB <= 2) && split_keys(A, tiles))
-      hipLaunchKernelGGL((k_attn_dq<T, (sizeof(T) == 2 || DB <= 2 ? DB : 2), 2>), dim3((unsigned)(tiles * A.kv)), dim3(2 * kThreads), 8 * L::BYTES, st, A);
+    if (!crowded<T>(DB) && split_keys(A, tiles))
+      hipLaunchKernelGGL((k_attn_dq<T, (crowded<T>(DB) ? 1 : DB), 2>), dim3((unsigned)(tiles * A.kv)), dim3(2 * kThreads), 8 * L::BYTES, st, A);
     else
       hipLaunchKernelGGL((k_attn_dq<T, DB, 1>), dim3((unsigned)(tiles * A.kv)), dim3(kThreads), 4 * L::BYTES, st, A);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
   if (A.rk > 0) {
-    constexpr int KEYS = keys_of(sizeof(T) == 2, DB);
-    const KeyPlan p = key_plan(A.rq, A.rk, A.n, A.kv, A.per, A.d, sizeof(T) == 2);
+    constexpr int KEYS = keys_of(sizeof(E) == 2, DB);
+    const KeyPlan p = key_plan(A.rq, A.rk, A.n, A.kv, A.per, A.d, sizeof(E) == 2);
     Args B = A;
     B.waves = p.parts;
     B.slots = p.slots;
-    hipLaunchKernelGGL((k_attn_dkv<T, DB>), dim3((unsigned)(p.parts ? p.parts : p.items)), dim3(4 * KEYS), 2 * (KEYS + kQRows) * L::PITCH + 2 * kQRows * 4, st, B);
+    hipLaunchKernelGGL((k_attn_dkv<T, DB>), dim3((unsigned)(p.parts ? p.parts : p.items)), dim3(4 * KEYS),
+                       2 * ((crowded<T>(DB) ? 0 : KEYS) + kQRows) * L::PITCH * L::PL + 2 * kQRows * 4, st, B);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    if (p.parts) hipLaunchKernelGGL((k_attn_dkv_join<T, DB>), dim3((unsigned)p.items), dim3(4 * KEYS), 0, st, B);
+    if (p.parts) hipLaunchKernelGGL((k_attn_dkv_join<E, DB>), dim3((unsigned)p.items), dim3(4 * KEYS), 0, st, B);
   }
   return hipGetLastError();
 }

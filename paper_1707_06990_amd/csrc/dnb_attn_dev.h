@@ -14,6 +14,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "../../include/dnb.h"
 
 namespace dnb {
@@ -67,21 +69,76 @@ __device__ __forceinline__ float half_sum(float v) {
   return __uint_as_float(s[0]) + __uint_as_float(s[1]);
 }
 
+// fp32 on the matrix cores' bf16 rate: x is the sum of three bf16 (8 bits of its 24 each, every remainder
+// exact), and of the nine products of two such sums the six that are not below 2^-23 of the whole are
+// made, at 32 cycles each where the fp32 instruction takes 512 for the same: six passes of a sixteenth.  Sums are
+// fp32 either way, and so is the error.  What has no such sum, infinities and values above the largest bf16
+// (3.39e38), counts as that value; NaN stays NaN.
+struct Split {};
+template <typename T>
+struct Elem {
+  using type = T;
+};
+template <>
+struct Elem<Split> {
+  using type = float;
+};
+template <typename T>
+using elem_t = typename Elem<T>::type;  // of the tensors
+
+__device__ __forceinline__ unsigned pack_bf16(float a, float b) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  return __builtin_bit_cast(unsigned, (bf16x2){(__bf16)a, (__bf16)b});
+}
+__device__ __forceinline__ void split8(const float (&x)[8], Piece (&p)[3]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    const float a = x[2 * j], b = x[2 * j + 1];
+    const unsigned hi = pack_bf16(a, b);
+    const float a1 = a - __uint_as_float(hi << 16), b1 = b - __uint_as_float(hi & 0xffff0000u);
+    const unsigned mid = pack_bf16(a1, b1);
+    p[0].q[j] = hi;
+    p[1].q[j] = mid;
+    p[2].q[j] = pack_bf16(a1 - __uint_as_float(mid << 16), b1 - __uint_as_float(mid & 0xffff0000u));
+  }
+}
+// ... of 8 floats as loaded.  The largest magnitude decides for the whole wave whether any needs cutting.
+__device__ __forceinline__ void split8(const u32x4& lo, const u32x4& hi, Piece (&p)[3]) {
+  constexpr float kMost = 3.3895313892515355e38f;
+  float x[8], top = 0.f;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    x[j] = __uint_as_float(lo[j]);
+    x[4 + j] = __uint_as_float(hi[j]);
+  }
+#pragma unroll
+  for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(x[j]));
+  if (__any(top > kMost)) {
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (fabsf(x[j]) > kMost) x[j] = copysignf(kMost, x[j]);
+  }
+  split8(x, p);
+}
+
 // A tile in LDS: rows of PC pieces of 16 bytes, of which CH hold the row (head_dim padded with zeros to
 // DB blocks of 32).  Piece c of row r lies at c ^ swz(r): sixteen rows read at one c (row_mul), and four
 // rows read 64 bytes wide (col_mul in bf16) or rows r and r + 4 read 128 bytes wide (in fp32), each meet
-// all the banks.
+// all the banks.  Each bit of swz is one of r's, so swz(r + s) is swz(r) ^ swz(s) where r and s share no bit.
+// Split: PL tiles, of the first, second and third parts.
 template <typename T, int DB>
 struct Tile {
-  static constexpr bool BF = sizeof(T) == 2;
-  static constexpr int EP = 16 / sizeof(T);            // elements of a piece
+  static constexpr bool BF = !std::is_same<T, float>::value;
+  static constexpr int PL = std::is_same<T, Split>::value ? 3 : 1;
+  static constexpr int EP = BF ? 8 : 4;                // elements of a piece
+  static constexpr int LD = EP * sizeof(elem_t<T>) / 16;  // loads of a piece from memory
   static constexpr int CH = DB * 32 / EP;
   static constexpr int PC = BF ? (DB == 1 ? 4 : DB == 2 ? 8 : 16) : (DB == 1 ? 8 : DB == 2 ? 16 : 32);
   static constexpr int PITCH = PC * 16;                // bytes
   static constexpr int NS = CH / 2;                    // steps of row_mul: a lane's half of the wave takes piece 2s + half
-  static constexpr int ROWS = BF ? 64 : 32;            // rows of a shared tile
-  static constexpr int BYTES = ROWS * PITCH;
-  static __device__ __forceinline__ int swz(int r) {
+  static constexpr int ROWS = std::is_same<T, __bf16>::value ? 64 : 32;  // rows of a shared tile
+  static constexpr int BYTES = ROWS * PITCH * PL;
+  static __device__ __forceinline__ constexpr int swz(int r) {
     if constexpr (BF) {
       if constexpr (PC == 4) return (r >> 2) & 3;
       else if constexpr (PC == 8) return (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
@@ -94,22 +151,38 @@ struct Tile {
   static __device__ __forceinline__ int at(int r, int c) { return r * PITCH + ((c ^ swz(r)) << 4); }
 };
 
-// a wave's 32 columns: of each step, this lane's half
 // Whether the waves of a workgroup of k_attn and k_attn_dq share the keys out in halves.  Eight waves at one
 // barrier are slower than two workgroups of four (12597 packed queries of 32 heads: 471 us for 393), but
 // with fewer tiles than compute units a workgroup's time is the launch's (1500 rows of 4 heads, a step: 152 us
 // for 170), unless the keys are one step anyway (a step of 33 tokens: 27 us for 24).
 inline bool split_keys(const Args& A, int64_t tiles) { return tiles * A.kv <= 256 && A.rk >= 256 * (int64_t)A.n; }
 
-template <typename T, int DB>
-using Columns = Piece[Tile<T, DB>::NS];
+// Copies of a step's tiles in LDS: the next one is written while one is read, unless the tiles are so large
+// that a second workgroup on the compute unit does more (Split above head_dim 64: 48 KB a copy).
+template <typename T>
+constexpr int buffers(int blocks) { return std::is_same<T, Split>::value && blocks > 2 ? 1 : 2; }
 
-__device__ __forceinline__ void mma(f32x16& acc, const Piece& a, const Piece& b, __bf16*) {
-  acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a.h, b.h, acc, 0, 0, 0);
+// 16 bytes of a tile, or of each of its three
+template <typename T, int DB>
+using Pieces = Piece[Tile<T, DB>::PL];
+// a wave's 32 columns: of each step, this lane's half
+template <typename T, int DB>
+using Columns = Pieces<T, DB>[Tile<T, DB>::NS];
+
+__device__ __forceinline__ void mma(f32x16& acc, const Piece (&a)[1], const Piece (&b)[1], __bf16*) {
+  acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[0].h, b[0].h, acc, 0, 0, 0);
 }
-__device__ __forceinline__ void mma(f32x16& acc, const Piece& a, const Piece& b, float*) {
+__device__ __forceinline__ void mma(f32x16& acc, const Piece (&a)[1], const Piece (&b)[1], float*) {
 #pragma unroll
-  for (int j = 0; j < 4; ++j) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a.f[j], b.f[j], acc, 0, 0, 0);
+  for (int j = 0; j < 4; ++j) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a[0].f[j], b[0].f[j], acc, 0, 0, 0);
+}
+__device__ __forceinline__ void mma(f32x16& acc, const Piece (&a)[3], const Piece (&b)[3], Split*) {
+  acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[0].h, b[2].h, acc, 0, 0, 0);
+  acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[2].h, b[0].h, acc, 0, 0, 0);
+  acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[1].h, b[1].h, acc, 0, 0, 0);
+  acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[0].h, b[1].h, acc, 0, 0, 0);
+  acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[1].h, b[0].h, acc, 0, 0, 0);
+  acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[0].h, b[0].h, acc, 0, 0, 0);
 }
 
 // Addresses in LDS as bytes from its start: what differs between a wave's reads of a tile is then a
@@ -142,16 +215,17 @@ __device__ __forceinline__ lds_t row_address(int row0) {
   return at_hand<HOLD>(Tile<T, DB>::at(row0 + (lane_id() & 31), lane_id() >> 5));
 }
 
-// rows row0 .. row0 + 31 of the tile times this wave's columns
-template <typename T, int DB, bool HOLD = false>
+// rows row0 .. row0 + 31 of the tile times this wave's columns; TR: rows of the whole tile
+template <typename T, int DB, bool HOLD = false, int TR = 32>
 __device__ __forceinline__ f32x16 row_mul(lds_t tile, int row0, const Columns<T, DB>& b) {
   using L = Tile<T, DB>;
   const lds_t at = row_address<T, DB, HOLD>(row0);
   f32x16 s = {};
 #pragma unroll
   for (int k = 0; k < L::NS; ++k) {
-    Piece a;
-    a.q = lds_read<u32x4>((at ^ (k << 5)) + tile);
+    Pieces<T, DB> a;
+#pragma unroll
+    for (int p = 0; p < L::PL; ++p) a[p].q = lds_read<u32x4>((at ^ (k << 5)) + (tile + p * TR * L::PITCH));
     mma(s, a, b[k], (T*)nullptr);
   }
   return s;
@@ -159,7 +233,7 @@ __device__ __forceinline__ f32x16 row_mul(lds_t tile, int row0, const Columns<T,
 
 // bf16: rounding s to 8 bits of mantissa is what feeding the matrix cores at their bf16 rate costs;
 // the sums stay in fp32.
-template <typename T, int DB, bool HOLD = false>
+template <typename T, int DB, bool HOLD = false, int TR = 32>
 __device__ __forceinline__ void col_mul(lds_t tile, int row0, const f32x16& s, f32x16 (&acc)[DB]) {
   using L = Tile<T, DB>;
   const int l = lane_id();
@@ -168,22 +242,33 @@ __device__ __forceinline__ void col_mul(lds_t tile, int row0, const f32x16& s, f
     const lds_t at = at_hand<HOLD>(L::at(row0 + 4 * (l >> 5) + ((l >> 2) & 3), 2 * ((l >> 4) & 1) + ((l >> 1) & 1)) + (l & 1) * 8);
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      Piece p;
+      Pieces<T, DB> y;
+      if constexpr (L::PL == 1) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) p.b[j] = (__bf16)s[8 * t + j];
+        for (int j = 0; j < 8; ++j) y[0].b[j] = (__bf16)s[8 * t + j];
+      } else {
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = s[8 * t + j];
+        split8(v, y);
+      }
 #pragma unroll
       for (int db = 0; db < DB; ++db) {
-        using lds4 = __attribute__((address_space(3))) s16x4;
-        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(uintptr_t)((at ^ (db << 6)) + (tile + 16 * t * L::PITCH)));
-        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(uintptr_t)((at ^ (db << 6) ^ 32) + (tile + (16 * t + 8) * L::PITCH)));
-        const uint2 a = __builtin_bit_cast(uint2, lo), b = __builtin_bit_cast(uint2, hi);
-        Piece x;
-        x.q = (u32x4){a.x, a.y, b.x, b.y};
-        mma(acc[db], x, p, (T*)nullptr);
+        Pieces<T, DB> x;
+#pragma unroll
+        for (int p = 0; p < L::PL; ++p) {
+          using lds4 = __attribute__((address_space(3))) s16x4;
+          const lds_t from = tile + p * TR * L::PITCH + 16 * t * L::PITCH;
+          const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(uintptr_t)((at ^ (db << 6)) + from));
+          const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(uintptr_t)((at ^ (db << 6) ^ 32) + (from + 8 * L::PITCH)));
+          const uint2 a = __builtin_bit_cast(uint2, lo), b = __builtin_bit_cast(uint2, hi);
+          x[p].q = (u32x4){a.x, a.y, b.x, b.y};
+        }
+        mma(acc[db], x, y, (T*)nullptr);
       }
     }
   } else {
-const lds_t at = at_hand<HOLD>(L::at(row0 + 4 * (l >> 5), (l & 31) >> 2) + (l & 3) * 4);
+    const lds_t at = at_hand<HOLD>(L::at(row0 + 4 * (l >> 5), (l & 31) >> 2) + (l & 3) * 4);
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
       const int r = 8 * (i >> 2) + (i & 3);
@@ -196,20 +281,35 @@ const lds_t at = at_hand<HOLD>(L::at(row0 + 4 * (l >> 5), (l & 31) >> 2) + (l & 
   }
 }
 
-// Pieces tid, tid + NT, ... of a tile's rows
-template <typename T, int DB, int U, int NT>
-__device__ __forceinline__ void store_pieces(lds_t tile, int tid, const u32x4 (&r)[U]) {
+// A loaded piece to its place in a tile of TR rows
+template <typename T, int DB, int TR>
+__device__ __forceinline__ void write_piece(lds_t to, const u32x4* r) {
+  using L = Tile<T, DB>;
+  if constexpr (L::PL == 1) {
+    lds_write(to, r[0]);
+  } else {
+    Piece p[3];
+    split8(r[0], r[1], p);
+#pragma unroll
+    for (int i = 0; i < 3; ++i) lds_write(to + i * TR * L::PITCH, p[i].q);
+  }
+}
+// Pieces tid, tid + NT, ... of a tile's TR rows
+template <typename T, int DB, int U, int NT, int TR>
+__device__ __forceinline__ void store_pieces(lds_t tile, int tid, const u32x4 (&r)[U * Tile<T, DB>::LD]) {
   using L = Tile<T, DB>;
   if constexpr (NT % L::CH == 0) {
     constexpr int STEP = NT / L::CH;  // a power of two, above the thread's first row
     const lds_t at = at_hand(L::at(tid / L::CH, tid % L::CH));
 #pragma unroll
-    for (int u = 0; u < U; ++u) lds_write((at ^ (L::swz(u * STEP) << 4)) + (tile + u * STEP * L::PITCH), r[u]);
+    for (int u = 0; u < U; ++u)
+      if (TR * L::CH % NT == 0 || tid + u * NT < TR * L::CH)
+        write_piece<T, DB, TR>((at ^ (L::swz(u * STEP) << 4)) + (tile + u * STEP * L::PITCH), r + u * L::LD);
   } else {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int i = tid + u * NT, row = i / L::CH, c = i - row * L::CH;
-      lds_write(tile + L::at(row, c), r[u]);
+      if (TR * L::CH % NT == 0 || i < TR * L::CH) write_piece<T, DB, TR>(tile + L::at(row, c), r + u * L::LD);
     }
   }
 }
@@ -219,41 +319,69 @@ __device__ __forceinline__ void store_pieces(lds_t tile, int tid, const u32x4 (&
 template <typename T, int DB, int ROWS, int NT>
 struct Stage {
   using L = Tile<T, DB>;
-  static constexpr int U = ROWS * L::CH / NT;
-  static_assert(ROWS * L::CH % NT == 0, "whole pieces a thread");
-  u32x4 r[U];
+  using E = elem_t<T>;
+  static constexpr int U = (ROWS * L::CH + NT - 1) / NT;
+  u32x4 r[U * L::LD];
   uint32_t off[U];
   __device__ __forceinline__ void init(int tid, int64_t stride, int d) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int i = tid + u * NT, row = i / L::CH, c = i - row * L::CH;
-      off[u] = c * L::EP < d ? (uint32_t)(row * (int)stride + c * L::EP) * (uint32_t)sizeof(T) : 0x80000000u;
+      off[u] = c * L::EP < d && row < ROWS ? (uint32_t)(row * (int)stride + c * L::EP) * (uint32_t)sizeof(E) : 0x80000000u;
     }
   }
   // base: the first row; rows: how many there are from it on (uniform in the wave; 0 or less: none)
-  __device__ __forceinline__ void load(const T* base, int64_t stride, int rows, int d) {
+  __device__ __forceinline__ void load(const E* base, int64_t stride, int rows, int d) {
     const int n = rows > ROWS ? ROWS : rows;
-    const int bytes = n > 0 ? (int)(((n - 1) * (int)stride + d) * (int)sizeof(T)) : 0;
+    const int bytes = n > 0 ? (int)(((n - 1) * (int)stride + d) * (int)sizeof(E)) : 0;
     const auto rsrc = __builtin_amdgcn_make_buffer_rsrc((void*)base, 0, bytes, 0x00027000);
 #pragma unroll
-    for (int u = 0; u < U; ++u) r[u] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, off[u], 0, 0);
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int p = 0; p < L::LD; ++p) r[u * L::LD + p] = __builtin_amdgcn_raw_buffer_load_b128(rsrc, off[u] + 16 * p, 0, 0);
   }
-  __device__ __forceinline__ void store(lds_t tile, int tid) {
-store_pieces<T, DB, U, NT>(tile, tid, r);
-  }
+  __device__ __forceinline__ void store(lds_t tile, int tid) { store_pieces<T, DB, U, NT, ROWS>(tile, tid, r); }
 };
 
 // This lane's column (its half of each step's two pieces) of a row of d elements; zeros if !valid.
 template <typename T, int DB>
-__device__ __forceinline__ void load_cols(Columns<T, DB>& f, const T* row, bool valid, int d) {
+__device__ __forceinline__ void load_cols(Columns<T, DB>& f, const elem_t<T>* row, bool valid, int d) {
   using L = Tile<T, DB>;
   const int h = lane_id() >> 5;
 #pragma unroll
   for (int k = 0; k < L::NS; ++k) {
     const int e = (2 * k + h) * L::EP;
-    f[k].q = (u32x4){0u, 0u, 0u, 0u};
-    if (valid && e < d) f[k].q = *reinterpret_cast<const u32x4*>(row + e);
+    u32x4 x[L::LD];
+#pragma unroll
+    for (int p = 0; p < L::LD; ++p) {
+      x[p] = (u32x4){0u, 0u, 0u, 0u};
+      if (valid && e < d) x[p] = *reinterpret_cast<const u32x4*>(row + e + p * (L::EP / L::LD));
+    }
+    if constexpr (L::PL == 1) f[k][0].q = x[0];
+    else split8(x[0], x[1], f[k]);
   }
+}
+// The product of two rows of d elements, half of it in each half of the wave
+template <typename T, int DB>
+__device__ __forceinline__ float dot_rows(const elem_t<T>* a, const elem_t<T>* b, bool valid, int d) {
+  constexpr int EP = 16 / sizeof(elem_t<T>);
+  float s = 0.f;
+#pragma unroll
+  for (int k = 0; k < 32 * DB / EP; k += 2) {
+    const int e = (k + (lane_id() >> 5)) * EP;
+    Piece x, y;
+    x.q = y.q = (u32x4){0u, 0u, 0u, 0u};
+    if (valid && e < d) {
+      x.q = *reinterpret_cast<const u32x4*>(a + e);
+      y.q = *reinterpret_cast<const u32x4*>(b + e);
+    }
+#pragma unroll
+    for (int j = 0; j < EP; ++j) {
+      if constexpr (sizeof(elem_t<T>) == 2) s = fmaf((float)x.b[j], (float)y.b[j], s);
+      else s = fmaf(x.f[j], y.f[j], s);
+    }
+  }
+  return half_sum(s);
 }
 
 // Y[d][c] of a wave (col_mul's result) times f into row c
