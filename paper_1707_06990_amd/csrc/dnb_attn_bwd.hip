@@ -18,6 +18,12 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kRows = 128;  // packed rows of a workgroup of k_attn_dq, 32 a wave
 
+// Rounding ds to bf16 is off by as much as rounding dq and dk themselves is; where a row sees few keys, D adds
+// the rounding of out, which is large there, and so is ds.  Rows that see up to this many keys multiply what
+// the rounding of ds left as well: dq and dk of packed documents are then 1.3 times as far from the exact
+// gradient as its rounding to bf16 is, without it 1.5 times.
+constexpr int kFineKeys = 128;
+
 // Two rows of registers for q and dout: above head_dim 64 Split takes those of two waves.
 template <typename T>
 constexpr bool crowded(int blocks) { return std::is_same<T, Split>::value && blocks > 2; }
@@ -59,10 +65,7 @@ __global__ __launch_bounds__(kThreads * KH, crowded<T>(DB) ? 1 : 2) void k_attn_
     if (v != -INFINITY) lse2 = v * kLog2e;
     if (l < 32 && kh == 0) A.rowdot[(int64_t)head * A.rq + qrow] = D;
   }
-  // Rounding ds to bf16 is off by as much as rounding dq itself is; where a row sees few keys, D adds the
-  // rounding of out, which is large there, and so is dq.  Waves that see up to 128 keys multiply what the
-  // rounding left as well.
-  const bool fine = most <= 128;
+  const bool fine = sizeof(E) == 2 && most <= kFineKeys;
   f32x16 acc[DB];
 #pragma unroll
   for (int i = 0; i < DB; ++i) acc[i] = (f32x16){};
@@ -101,7 +104,7 @@ __global__ __launch_bounds__(kThreads * KH, crowded<T>(DB) ? 1 : 2) void k_attn_
           for (int i = 0; i < 16; ++i) s[i] = k0 + 32 * b + row_of(i) >= sees ? 0.f : s[i];
         }
         col_mul<T, DB, HOLD, STEP>(kt, 32 * b, s, acc);
-        if (sizeof(E) == 2 && fine) {
+        if (fine) {
 #pragma unroll
           for (int i = 0; i < 16; ++i) s[i] -= (float)(__bf16)s[i];
           col_mul<T, DB, HOLD, STEP>(kt, 32 * b, s, acc);
@@ -377,6 +380,8 @@ __global__ __launch_bounds__(4 * keys_of(sizeof(elem_t<T>) == 2, DB), crowded<T>
         store_pieces<T, DB, U, NT, kQRows>(dt, threadIdx.x, rd);
         if ((int)threadIdx.x < 2 * kQRows) lds_write(rows + 4 * threadIdx.x, st);
         __syncthreads();
+        // of this wave's rows of the step, the last
+        const bool fine = BF && (A.causal ? q0 + over(s0 + qb + 31) + shift + 1 : S.nk) <= kFineKeys;
         s0 += kQRows % per;
         q0 += kQRows / per;
         if (s0 >= per) {
@@ -415,6 +420,11 @@ __global__ __launch_bounds__(4 * keys_of(sizeof(elem_t<T>) == 2, DB), crowded<T>
           }
           col_mul<T, DB, false, kQRows>(dt, qb, s, dv);
           col_mul<T, DB, false, kQRows>(qt, qb, dp, dk);
+          if (fine) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) dp[i] -= (float)(__bf16)dp[i];
+            col_mul<T, DB, false, kQRows>(qt, qb, dp, dk);
+          }
         }
       }
       // The first half of the waves finishes dk, the second dv: each gives the other sum to its partner.
