@@ -182,10 +182,20 @@ def _ptr(t):
     return t.data_ptr()
 
 
+_current = None
+
+
 def _stream(stream):
+    """Handle of a stream; None: torch's current one on the current device, asked for by its handle, which
+    takes 0.2 us where torch.cuda.current_stream() makes an object in 3 (a launch takes 3 in all)."""
+    global _current
     if stream is None:
-        import torch
-        return torch.cuda.current_stream().cuda_stream
+        if _current is None:
+            import torch
+            torch.cuda.current_stream()   # the device is set up
+            handle, device = getattr(torch._C, "_cuda_getCurrentRawStream", None), getattr(torch._C, "_cuda_getDevice", None)
+            _current = (lambda: handle(device())) if handle and device else (lambda: torch.cuda.current_stream().cuda_stream)
+        return _current()
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 

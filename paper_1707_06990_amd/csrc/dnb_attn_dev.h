@@ -421,13 +421,21 @@ __device__ __forceinline__ Seq seq_at(const Args& A, int i) {
   return s;
 }
 
-__device__ __forceinline__ int64_t wave_scan(int64_t v) {  // inclusive
-  const int l = lane_id();
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) {
-    const int64_t t = __shfl_up(v, o);
-    if (l >= o) v += t;
-  }
+// v of the lane that CTRL names, 0 where there is none or ROWS (of 16 lanes, a bit each) leaves this one out
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int64_t from_lane(int64_t v) {
+  const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)v, CTRL, ROWS, 0xf, false);
+  const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(v >> 32), CTRL, ROWS, 0xf, false);
+  return (int64_t)(((uint64_t)hi << 32) | lo);
+}
+// Inclusive sum over the lanes, within the registers: through LDS it took 0.7 us of every kernel here.
+__device__ __forceinline__ int64_t wave_scan(int64_t v) {
+  v += from_lane<0x111, 0xf>(v);  // 1, 2, 4 and 8 lanes down inside a row
+  v += from_lane<0x112, 0xf>(v);
+  v += from_lane<0x114, 0xf>(v);
+  v += from_lane<0x118, 0xf>(v);
+  v += from_lane<0x142, 0xa>(v);  // lane 15 to row 1, lane 47 to row 3
+  v += from_lane<0x143, 0xc>(v);  // lane 31 to rows 2 and 3
   return v;
 }
 __device__ __forceinline__ int bcast(int v, int lane) { return __builtin_amdgcn_readlane(v, lane); }

@@ -103,7 +103,11 @@ __global__ __launch_bounds__(kThreads) void k_clip_squares(const Chunk* table, i
 
 __global__ __launch_bounds__(kThreads) void k_clip_scale(const Chunk* table, int chunks, const double* part, int parts, float max_norm,
                                                          float* norm) {
+  int at = chunks - 1 - (int)blockIdx.x;
+  Chunk k = {};
+  if (at >= 0) k = table[at];  // on its way while the norm is made
   double s = 0.0;
+#pragma unroll 4
   for (int i = threadIdx.x; i < parts; i += kThreads) s += part[i];
   s = block_sum(s);
   const float n = (float)sqrt(s);
@@ -113,11 +117,12 @@ __global__ __launch_bounds__(kThreads) void k_clip_scale(const Chunk* table, int
     norm[0] = n;
     norm[1] = f;
   }
-  for (int i = chunks - 1 - (int)blockIdx.x; i >= 0; i -= gridDim.x) {
-    const Chunk k = table[i];
-    if (k.src == k.dst && f == 1.f) continue;  // in place and nothing to do
-    if (k.flags & 1) scale_chunk<__bf16>(k, f);
+  while (at >= 0) {
+    if (k.src == k.dst && f == 1.f) {  // in place and nothing to do
+    } else if (k.flags & 1) scale_chunk<__bf16>(k, f);
     else scale_chunk<float>(k, f);
+    at -= gridDim.x;
+    if (at >= 0) k = table[at];
   }
 }
 
