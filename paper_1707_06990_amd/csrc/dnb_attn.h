@@ -5,7 +5,8 @@
 
 namespace dnb {
 namespace attn {
-hipError_t launch_backward(const Args& A, bool bf16, hipStream_t st);
+// token: with the work of dq split over the keys
+hipError_t launch_backward(const Args& A, bool bf16, bool token, hipStream_t st);
 // bytes at Args::part that it takes
 size_t backward_part_bytes(int64_t rq, int64_t rk, int n, int kv, int per, int d, bool bf16);
 }

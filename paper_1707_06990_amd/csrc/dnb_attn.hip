@@ -8,8 +8,8 @@
 // log 2).  The sum so far and its weights are only rescaled when the maximum has grown by more than
 // 8 (a factor of 256, far from anything that fp32 sums lose), which after the first tiles it hardly does.
 //
-// k_attn_token / k_attn_join: for few rows a sequence (answering: one query a request) the work is split
-// over the keys instead, and is bound by reading them.
+// k_attn_token / k_attn_join: where few rows would leave most compute units idle (answering: one query a
+// request) the work is split over the keys instead.  With one query a request it is bound by reading them.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -98,17 +98,11 @@ __global__ __launch_bounds__(kThreads * KH, 2) void k_attn(Args A) {
   if (!find_tile(A, blockIdx.x / A.kv, [&](const Seq& s) { return (int)(((int64_t)s.nq * A.per + kRows - 1) / kRows); }, &S, &t, &count))
     return;
   if (A.causal) t = count - 1 - t;  // the rows that see most keys go first
-  const int M = S.nq * A.per, m0 = t * kRows, shift = S.nk - S.nq;
-  const int m = m0 + wave * 32 + (l & 31), row = m / A.per, sub = m - row * A.per;
-  const bool valid = m < M;
-  const int head = g * A.per + sub;
-  const int64_t qrow = (int64_t)S.q0 + row;
-  // keys that this lane's query sees, and at most / at least of the wave's; of the workgroup's
-  const int sees = A.causal ? min(max(row + shift + 1, 0), S.nk) : S.nk;
-  const int w0 = m0 + wave * 32, w1 = min(w0 + 31, M - 1);
-  const int most = w0 >= M ? 0 : A.causal ? min(max(w1 / A.per + shift + 1, 0), S.nk) : S.nk;
-  const int least = A.causal ? min(max(w0 / A.per + shift + 1, 0), S.nk) : S.nk;
-  const int all = A.causal ? min(max(min(m0 + kRows - 1, M - 1) / A.per + shift + 1, 0), S.nk) : S.nk;
+  const RowTile R0(A, S, g, t * kRows + wave * 32);
+  const int all = RowTile::seen(A, S, min((t + 1) * kRows, S.nq * A.per) - 1);  // keys that the workgroup's last row sees
+  const bool valid = R0.valid;
+  const int head = R0.head, sees = R0.sees, most = R0.most, least = R0.least;
+  const int64_t qrow = R0.qrow;
 
   Columns<T, DB> qf;
   load_cols<T, DB>(qf, (const E*)A.q + qrow * A.qs + (int64_t)head * A.d, valid, A.d);
@@ -188,27 +182,7 @@ __global__ __launch_bounds__(kThreads * KH, 2) void k_attn(Args A) {
   if (valid && l < 32) A.lse[(int64_t)head * A.rq + qrow] = sum == 0.f ? -INFINITY : (R.m + log2f(sum)) * kLn2;
 }
 
-// ---------------------------------------------------------------- few rows a sequence
-
-// Items are (sequence, tile of 32 packed rows, key/value head), in that order, a unit is 32 keys of an
-// item, and all units of all items lie on one line, which is cut into equal parts, one a wave: whatever
-// the lengths, no wave has more than one unit more than another.  A part of an item leaves O, m and l
-// in slot (wave + item): walking along the line, each next part has a next wave or a next item.
-constexpr int kItemRows = 32, kUnit = 32;
-
-struct Line {
-  int64_t units, items;  // of this lane's sequence
-};
-__device__ __forceinline__ Line line_of(const Args& A, const Seq& s) {
-  const int64_t items = ((int64_t)s.nq * A.per + kItemRows - 1) / kItemRows * A.kv;
-  return {items * ((s.nk + kUnit - 1) / kUnit), items};
-}
-__device__ __forceinline__ int64_t line_total(const Args& A) {
-  int64_t u = 0;
-  for (int i = lane_id(); i < A.n; i += 64) u += line_of(A, seq_at(A, i)).units;
-  return bcast64(wave_scan(u), 63);
-}
-constexpr int64_t slot_floats(int dp) { return (int64_t)kItemRows * dp + 2 * kItemRows; }
+// ---------------------------------------------------------------- work split over the keys
 
 template <typename T, int DB>
 __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void k_attn_token(Args A) {
@@ -217,72 +191,42 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void k_attn_token
   const lds_t lds = lds_start(shared);
   const int l = lane_id(), wave = threadIdx.x >> 6;
   const lds_t kt = lds + wave * 2 * kUnit * L::PITCH, vt = kt + kUnit * L::PITCH;
-  const int64_t total = line_total(A), W = min((int64_t)A.waves, total), w = (int64_t)blockIdx.x * 4 + wave;
-  if (w >= W) return;
-  int64_t a = w * total / W;
-  const int64_t b = (w + 1) * total / W;
   Stage<T, DB, kUnit, 64> sk, sv;
   sk.init(l, A.ks, A.d);
   sv.init(l, A.vs, A.d);
-  int64_t u0 = 0, i0 = 0;  // units and items before the 64 sequences at hand
-  for (int base = 0; base < A.n && a < b; base += 64) {
-    Seq mine = {};
-    Line ln = {};
-    if (base + l < A.n) {
-      mine = seq_at(A, base + l);
-      ln = line_of(A, mine);
+  each_part(A, (int64_t)blockIdx.x * 4 + wave, [&](const Seq& S, int g, int m0, int first, int last, int64_t slot) {
+    const RowTile R0(A, S, g, m0);
+    Columns<T, DB> qf;
+    load_cols<T, DB>(qf, (const T*)A.q + R0.qrow * A.qs + (int64_t)R0.head * A.d, R0.valid, A.d);
+    Online<DB> R;
+    R.init();
+    const T* kb = (const T*)A.k + (int64_t)S.k0 * A.ks + (int64_t)g * A.d;
+    const T* vb = (const T*)A.v + (int64_t)S.k0 * A.vs + (int64_t)g * A.d;
+    auto fetch = [&](int u) {
+      sk.load(kb + (int64_t)u * kUnit * A.ks, A.ks, S.nk - u * kUnit, A.d);
+      sv.load(vb + (int64_t)u * kUnit * A.vs, A.vs, S.nk - u * kUnit, A.d);
+    };
+    const int end = min(last, (R0.most + kUnit - 1) / kUnit);  // no row of the tile sees what follows
+    if (first < end) fetch(first);
+    for (int u = first; u < end; ++u) {
+      // the tiles are this wave's own, and LDS serves a wave's accesses in their order
+      sk.store(kt, l);
+      sv.store(vt, l);
+      if (u + 1 < end) fetch(u + 1);
+      __builtin_amdgcn_wave_barrier();
+      f32x16 s[1] = {row_mul<T, DB, false, kUnit>(kt, 0, qf)};
+      if ((u + 1) * kUnit > R0.least) hide(s[0], u * kUnit, R0.sees);
+      online_step<T, DB, 1, false, kUnit>(R, s, A.c, vt, 0);
+      __builtin_amdgcn_wave_barrier();
     }
-    const int64_t ue = wave_scan(ln.units), ie = wave_scan(ln.items);
-    const int64_t u1 = u0 + bcast64(ue, 63);
-    while (a < b && a < u1) {
-      const int at = __builtin_ctzll(__ballot(u0 + ue > a));
-      const Seq S = bcast(mine, at);
-      const int64_t su = u0 + bcast64(ue, at) - bcast64(ln.units, at), si = i0 + bcast64(ie, at) - bcast64(ln.items, at);
-      const int len = (S.nk + kUnit - 1) / kUnit;
-      const int64_t j = (a - su) / len;
-      const int first = (int)(a - su - j * len), last = (int)min((int64_t)len, first + b - a);
-      const int g = (int)(j % A.kv), m0 = (int)(j / A.kv) * kItemRows, M = S.nq * A.per;
-      const int m = m0 + (l & 31), row = m / A.per, head = g * A.per + m - row * A.per;
-      const bool valid = m < M;
-      const int sees = A.causal ? min(max(row + S.nk - S.nq + 1, 0), S.nk) : S.nk;
-      const int least = A.causal ? min(max(m0 / A.per + S.nk - S.nq + 1, 0), S.nk) : S.nk;
-      Columns<T, DB> qf;
-      load_cols<T, DB>(qf, (const T*)A.q + ((int64_t)S.q0 + row) * A.qs + (int64_t)head * A.d, valid, A.d);
-      Online<DB> R;
-      R.init();
-      const T* kb = (const T*)A.k + (int64_t)S.k0 * A.ks + (int64_t)g * A.d;
-      const T* vb = (const T*)A.v + (int64_t)S.k0 * A.vs + (int64_t)g * A.d;
-      auto fetch = [&](int u) {
-        sk.load(kb + (int64_t)u * kUnit * A.ks, A.ks, S.nk - u * kUnit, A.d);
-        sv.load(vb + (int64_t)u * kUnit * A.vs, A.vs, S.nk - u * kUnit, A.d);
-      };
-      fetch(first);
-      for (int u = first; u < last; ++u) {
-        // the tiles are this wave's own, and LDS serves a wave's accesses in their order
-        sk.store(kt, l);
-        sv.store(vt, l);
-        if (u + 1 < last) fetch(u + 1);
-        __builtin_amdgcn_wave_barrier();
-        f32x16 s[1] = {row_mul<T, DB, false, kUnit>(kt, 0, qf)};
-        if ((u + 1) * kUnit > least) hide(s[0], u * kUnit, sees);
-        online_step<T, DB, 1, false, kUnit>(R, s, A.c, vt, 0);
-        __builtin_amdgcn_wave_barrier();
-      }
-      const int64_t slot = w + si + j;
-      if (slot < A.slots) {
-        float* p = A.part + slot * slot_floats(32 * DB);
-        store_cols<float, DB>(p + (l & 31) * 32 * DB, valid, 32 * DB, R.o, 1.f);
-        const float sum = half_sum(R.l);
-        if (valid && l < 32) {
-          p[kItemRows * 32 * DB + l] = R.m;
-          p[kItemRows * 32 * DB + kItemRows + l] = sum;
-        }
-      }
-      a += last - first;
+    float* p = A.part + slot * slot_floats(32 * DB);
+    store_cols<float, DB>(p + (l & 31) * 32 * DB, R0.valid, 32 * DB, R.o, 1.f);
+    const float sum = half_sum(R.l);
+    if (R0.valid && l < 32) {
+      p[kItemRows * 32 * DB + l] = R.m;
+      p[kItemRows * 32 * DB + kItemRows + l] = sum;
     }
-    u0 = u1;
-    i0 += bcast64(ie, 63);
-  }
+  });
 }
 
 // Joins an item's parts: a workgroup for each (query row, head).  32 lanes (at head_dim 128) hold a row and
@@ -293,62 +237,25 @@ template <typename T, int DB>
 __global__ __launch_bounds__(kThreads) void k_attn_join(Args A) {
   constexpr int DP = 32 * DB, LANES = DP / 4, G = kThreads / LANES;
   __shared__ float red[G][DP + 2];
-  const int l = lane_id();
-  const int64_t id = blockIdx.x, qrow = id / A.heads;
-  const int head = (int)(id - qrow * A.heads);
-  int64_t u0 = 0, i0 = 0, su = 0, si = 0;
-  Seq S = {};
-  bool found = false;
-  for (int base = 0; base < A.n; base += 64) {
-    Seq mine = {};
-    Line ln = {};
-    if (base + l < A.n) {
-      mine = seq_at(A, base + l);
-      ln = line_of(A, mine);
-    }
-    const int64_t ue = wave_scan(ln.units), ie = wave_scan(ln.items);
-    const uint64_t holds = __ballot(mine.q0 <= qrow && qrow < (int64_t)mine.q0 + mine.nq);
-    if (holds) {
-      const int at = __builtin_ctzll(holds);
-      S = bcast(mine, at);
-      su = u0 + bcast64(ue - ln.units, at);
-      si = i0 + bcast64(ie - ln.items, at);
-      found = true;
-    }
-    u0 += bcast64(ue, 63);
-    i0 += bcast64(ie, 63);
-  }
-  if (!found) return;  // a row of no sequence
-  const int64_t total = u0, W = min((int64_t)A.waves, total);
-  const int g = head / A.per, m = (int)(qrow - S.q0) * A.per + head - g * A.per, r = m % kItemRows;
-  const int len = (S.nk + kUnit - 1) / kUnit;
-  const int64_t j = (int64_t)(m / kItemRows) * A.kv + g;
+  const RowParts P = row_parts(A, blockIdx.x);
+  if (!P.found) return;  // a row of no sequence
   const int grp = threadIdx.x / LANES, c = threadIdx.x - grp * LANES;
   float M = -INFINITY, sum = 0.f;
   f32x4 o = {};
-  if (len > 0) {
-    // unit u is wave ((u + 1) W - 1) / total's
-    const int64_t first = su + j * len;
-    const int64_t w0 = ((first + 1) * W - 1) / total, w1 = ((first + len) * W - 1) / total;
-    if (si + j + w1 >= A.slots) return;  // offsets that are not sorted
-    const float* p = A.part + (si + j + w0) * slot_floats(DP);
-    const int n = (int)(w1 - w0 + 1);
-    if (grp < G) {
-#pragma unroll 8
-      for (int i = grp; i < n; i += G) {
-        const float* q = p + i * slot_floats(DP);
-        const f32x4 v = *reinterpret_cast<const f32x4*>(q + r * DP + 4 * c);
-        const float mi = q[kItemRows * DP + r], li = q[kItemRows * DP + kItemRows + r];
-        const float top = fmaxf(M, mi), t = top == -INFINITY ? 0.f : top;
-        const float a = __builtin_amdgcn_exp2f(M - t), b = __builtin_amdgcn_exp2f(mi - t);
-        M = top;
-        sum = sum * a + li * b;
-#pragma unroll
-        for (int k = 0; k < 4; ++k) o[k] = o[k] * a + v[k] * b;
-      }
-    }
-  }
   if (grp < G) {
+    const float* p = A.part + P.slot * slot_floats(DP);
+#pragma unroll 8
+    for (int i = grp; i < P.n; i += G) {
+      const float* q = p + i * slot_floats(DP);
+      const f32x4 v = *reinterpret_cast<const f32x4*>(q + P.r * DP + 4 * c);
+      const float mi = q[kItemRows * DP + P.r], li = q[kItemRows * DP + kItemRows + P.r];
+      const float top = fmaxf(M, mi), t = top == -INFINITY ? 0.f : top;
+      const float a = __builtin_amdgcn_exp2f(M - t), b = __builtin_amdgcn_exp2f(mi - t);
+      M = top;
+      sum = sum * a + li * b;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) o[k] = o[k] * a + v[k] * b;
+    }
 #pragma unroll
     for (int k = 0; k < 4; ++k) red[grp][4 * c + k] = o[k];
     if (c == 0) {
@@ -370,8 +277,8 @@ __global__ __launch_bounds__(kThreads) void k_attn_join(Args A) {
     sum = fmaf(red[i][DP + 1], f, sum);
     y = fmaf(red[i][threadIdx.x], f, y);
   }
-  if ((int)threadIdx.x < A.d) ((T*)A.o)[qrow * A.os + (int64_t)head * A.d + threadIdx.x] = (T)(sum == 0.f ? 0.f : y / sum);
-  if (threadIdx.x == 0) A.lse[(int64_t)head * A.rq + qrow] = sum == 0.f ? -INFINITY : (M + log2f(sum)) * kLn2;
+  if ((int)threadIdx.x < A.d) ((T*)A.o)[P.qrow * A.os + (int64_t)P.head * A.d + threadIdx.x] = (T)(sum == 0.f ? 0.f : y / sum);
+  if (threadIdx.x == 0) A.lse[(int64_t)P.head * A.rq + P.qrow] = sum == 0.f ? -INFINITY : (M + log2f(sum)) * kLn2;
 }
 
 template <typename T, int DB>
@@ -464,8 +371,7 @@ int dnb_attn_create(const dnb_attn_desc* desc, dnb_attn** out) {
   dnb_attn* p = new (std::nothrow) dnb_attn();
   if (!p) return DNB_E_NOMEM;
   p->d = d;
-  // the token form takes a sequence's rows in tiles of 32: as long as they fit one on average
-  p->token = d.rows_q * per <= (int64_t)kItemRows * d.sequences;
+  p->token = split_rows(d.rows_q, d.rows_k, d.sequences, d.kv_heads, per, d.dtype == DNB_BF16);
   const int dp = (d.head_dim + 31) / 32 * 32;
   p->waves = d.dtype == DNB_BF16 ? 2048 : 1024;  // 256 compute units, two workgroups of four waves each, fp32 one
   p->slots = p->token ? p->waves + ((d.rows_q * per + kItemRows - 1) / kItemRows + d.sequences) * d.kv_heads : 0;
@@ -515,7 +421,7 @@ int dnb_attn_backward(const dnb_attn* p, const void* q, const void* k, const voi
   A.qo = q_offsets; A.ko = k_offsets; A.kl = k_lengths;
   A.rowdot = (float*)((char*)workspace + p->ws_rowdot);
   A.part = (float*)((char*)workspace + p->ws_part);
-  const hipError_t e = launch_backward(A, p->d.dtype == DNB_BF16, (hipStream_t)stream);
+  const hipError_t e = launch_backward(A, p->d.dtype == DNB_BF16, p->token, (hipStream_t)stream);
   return e == hipSuccess ? DNB_OK : DNB_E_LAUNCH;
 }
 

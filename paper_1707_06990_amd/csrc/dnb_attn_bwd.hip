@@ -43,16 +43,11 @@ __global__ __launch_bounds__(kThreads * KH, crowded<T>(DB) ? 1 : 2) void k_attn_
   if (!find_tile(A, blockIdx.x / A.kv, [&](const Seq& s) { return (int)(((int64_t)s.nq * A.per + kRows - 1) / kRows); }, &S, &t, &count))
     return;
   if (A.causal) t = count - 1 - t;
-  const int M = S.nq * A.per, m0 = t * kRows, shift = S.nk - S.nq;
-  const int m = m0 + wave * 32 + (l & 31), row = m / A.per, sub = m - row * A.per;
-  const bool valid = m < M;
-  const int head = g * A.per + sub;
-  const int64_t qrow = (int64_t)S.q0 + row;
-  const int sees = A.causal ? min(max(row + shift + 1, 0), S.nk) : S.nk;
-  const int w0 = m0 + wave * 32, w1 = min(w0 + 31, M - 1);
-  const int most = w0 >= M ? 0 : A.causal ? min(max(w1 / A.per + shift + 1, 0), S.nk) : S.nk;
-  const int least = A.causal ? min(max(w0 / A.per + shift + 1, 0), S.nk) : S.nk;
-  const int all = A.causal ? min(max(min(m0 + kRows - 1, M - 1) / A.per + shift + 1, 0), S.nk) : S.nk;
+  const RowTile R0(A, S, g, t * kRows + wave * 32);
+  const int all = RowTile::seen(A, S, min((t + 1) * kRows, S.nq * A.per) - 1);  // keys that the workgroup's last row sees
+  const bool valid = R0.valid;
+  const int head = R0.head, sees = R0.sees, most = R0.most, least = R0.least;
+  const int64_t qrow = R0.qrow;
 
   Columns<T, DB> qf, df;
   load_cols<T, DB>(qf, (const E*)A.q + qrow * A.qs + (int64_t)head * A.d, valid, A.d);
@@ -138,6 +133,90 @@ __global__ __launch_bounds__(kThreads * KH, crowded<T>(DB) ? 1 : 2) void k_attn_
       }
   }
   store_cols<E, DB>((E*)A.dq + qrow * A.qs + (int64_t)head * A.d, valid, A.d, acc, A.scale);
+}
+
+// k_attn_dq with the work split over the keys (see each_part): a wave's own tiles of 32 keys, and sums of parts
+// that k_attn_dq_join adds.
+template <typename T, int DB>
+__global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DB <= 2 ? 2 : 1) void k_attn_dq_token(Args A) {
+  using L = Tile<T, DB>;
+  const int l = lane_id(), wave = threadIdx.x >> 6;
+  const lds_t kt = wave * 2 * kUnit * L::PITCH, vt = kt + kUnit * L::PITCH;
+  Stage<T, DB, kUnit, 64> sk, sv;
+  sk.init(l, A.ks, A.d);
+  sv.init(l, A.vs, A.d);
+  each_part(A, (int64_t)blockIdx.x * 4 + wave, [&](const Seq& S, int g, int m0, int first, int last, int64_t slot) {
+    const RowTile R(A, S, g, m0);
+    const int64_t at = R.qrow * A.os + (int64_t)R.head * A.d;
+    Columns<T, DB> qf, df;
+    load_cols<T, DB>(qf, (const T*)A.q + R.qrow * A.qs + (int64_t)R.head * A.d, R.valid, A.d);
+    load_cols<T, DB>(df, (const T*)A.dout + at, R.valid, A.d);
+    const float D = dot_rows<T, DB>((const T*)A.out + at, (const T*)A.dout + at, R.valid, A.d);
+    float lse2 = INFINITY;
+    if (R.valid) {
+      const float v = A.lse[(int64_t)R.head * A.rq + R.qrow];
+      if (v != -INFINITY) lse2 = v * kLog2e;
+      if (l < 32 && first == 0) A.rowdot[(int64_t)R.head * A.rq + R.qrow] = D;
+    }
+    const bool fine = L::BF && R.most <= kFineKeys;
+    f32x16 acc[DB];
+#pragma unroll
+    for (int i = 0; i < DB; ++i) acc[i] = (f32x16){};
+    const T* kb = (const T*)A.k + (int64_t)S.k0 * A.ks + (int64_t)g * A.d;
+    const T* vb = (const T*)A.v + (int64_t)S.k0 * A.vs + (int64_t)g * A.d;
+    auto fetch = [&](int u) {
+      sk.load(kb + (int64_t)u * kUnit * A.ks, A.ks, S.nk - u * kUnit, A.d);
+      sv.load(vb + (int64_t)u * kUnit * A.vs, A.vs, S.nk - u * kUnit, A.d);
+    };
+    const int end = min(last, (R.most + kUnit - 1) / kUnit);
+    if (first < end) fetch(first);
+    for (int u = first; u < end; ++u) {
+      sk.store(kt, l);
+      sv.store(vt, l);
+      if (u + 1 < end) fetch(u + 1);
+      __builtin_amdgcn_wave_barrier();
+      f32x16 s = row_mul<T, DB, false, kUnit>(kt, 0, qf);
+      const f32x16 dp = row_mul<T, DB, false, kUnit>(vt, 0, df);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], A.c, -lse2)) * (dp[i] - D);
+      if ((u + 1) * kUnit > R.least) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] = u * kUnit + row_of(i) >= R.sees ? 0.f : s[i];
+      }
+      col_mul<T, DB, false, kUnit>(kt, 0, s, acc);
+      if (fine) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) s[i] -= (float)(__bf16)s[i];
+        col_mul<T, DB, false, kUnit>(kt, 0, s, acc);
+      }
+      __builtin_amdgcn_wave_barrier();
+    }
+    store_cols<float, DB>(A.part + slot * slot_floats(32 * DB) + (l & 31) * 32 * DB, R.valid, 32 * DB, acc, A.scale);
+  });
+}
+
+// As k_attn_join: groups of lanes with a row's parts in turn, then their sums in LDS.
+template <typename T, int DB>
+__global__ __launch_bounds__(kThreads) void k_attn_dq_join(Args A) {
+  constexpr int DP = 32 * DB, LANES = DP / 4, G = kThreads / LANES;
+  __shared__ float red[G][DP];
+  const RowParts P = row_parts(A, blockIdx.x);
+  if (!P.found) return;
+  const int grp = threadIdx.x / LANES, c = threadIdx.x - grp * LANES;
+  if (grp < G) {
+    f32x4 sum = {};
+    const float* p = A.part + P.slot * slot_floats(DP) + P.r * DP + 4 * c;
+#pragma unroll 8
+    for (int i = grp; i < P.n; i += G) sum += *reinterpret_cast<const f32x4*>(p + i * slot_floats(DP));
+#pragma unroll
+    for (int k = 0; k < 4; ++k) red[grp][4 * c + k] = sum[k];
+  }
+  __syncthreads();
+  if ((int)threadIdx.x >= A.d) return;
+  float y = 0.f;
+#pragma unroll
+  for (int i = 0; i < G; ++i) y += red[i][threadIdx.x];
+  ((T*)A.dq)[P.qrow * A.qs + (int64_t)P.head * A.d + threadIdx.x] = (T)y;
 }
 
 // row_mul with the columns in LDS too: rows brow0 .. brow0 + 31 of tile bt, of BR rows
@@ -474,7 +553,8 @@ __global__ __launch_bounds__(4 * keys_of(sizeof(elem_t<T>) == 2, DB), crowded<T>
   }
 }
 
-// Adds the parts of an item that several workgroups share, in the line's order; a workgroup an item.
+// Adds the parts of an item that several workgroups share, in the line's order; a workgroup for an item and 32
+// of head_dim, so that a long chain of parts (each some 2 us away) is read four at a time.
 template <typename T, int DB>
 __global__ __launch_bounds__(4 * keys_of(sizeof(T) == 2, DB)) void k_attn_dkv_join(Args A) {
   constexpr bool BF = sizeof(T) == 2;
@@ -513,26 +593,22 @@ __global__ __launch_bounds__(4 * keys_of(sizeof(T) == 2, DB)) void k_attn_dkv_jo
   // unit u of the line is workgroup ((u + 1) W - 1) / total's
   const int64_t w0 = ((from + 1) * W - 1) / total, w1 = (to * W - 1) / total;
   if (w0 == w1 || w1 + item >= A.slots) return;
-  f32x16 sum[DB];
-#pragma unroll
-  for (int i = 0; i < DB; ++i) sum[i] = (f32x16){};
+  const int db = blockIdx.y;
+  f32x16 sum[1] = {};
+#pragma unroll 4
   for (int64_t w = w0; w <= w1; ++w) {
-    const float4* part = reinterpret_cast<const float4*>(A.part) + ((w + item) * 2 * KB + wave) * DB * 4 * 64;
+    const f32x4* part = reinterpret_cast<const f32x4*>(A.part) + (((w + item) * 2 * KB + wave) * DB + db) * 4 * 64;
 #pragma unroll
-    for (int db = 0; db < DB; ++db)
+    for (int q = 0; q < 4; ++q) {
+      const f32x4 x = part[q * 64 + l];
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        const float4 x = part[(db * 4 + q) * 64 + l];
-        sum[db][4 * q] += x.x;
-        sum[db][4 * q + 1] += x.y;
-        sum[db][4 * q + 2] += x.z;
-        sum[db][4 * q + 3] += x.w;
-      }
+      for (int k = 0; k < 4; ++k) sum[0][4 * q + k] += x[k];
+    }
   }
   const bool second = wave >= KB;
   const int key = (int)t * KEYS + 32 * (wave & (KB - 1)) + (l & 31);
-  const int64_t krow = (int64_t)S.k0 + key, at = krow * (second ? A.vs : A.ks) + (int64_t)g * A.d;
-  store_cols<T, DB>((T*)(second ? A.dv : A.dk) + at, key < S.span, A.d, sum, second ? 1.f : A.scale);
+  const int64_t krow = (int64_t)S.k0 + key, at = krow * (second ? A.vs : A.ks) + (int64_t)g * A.d + 32 * db;
+  store_cols<T, 1>((T*)(second ? A.dv : A.dk) + at, key < S.span, A.d - 32 * db, sum, second ? 1.f : A.scale);
 }
 
 // How k_attn_dkv is launched.  Up to 512 packed rows (8 steps an item) a workgroup takes an item: a launch
@@ -553,10 +629,18 @@ KeyPlan key_plan(int64_t rq, int64_t rk, int n, int kv, int per, int d, bool bf1
 }
 
 template <typename E, int DB>
-hipError_t run(const Args& A, hipStream_t st) {
+hipError_t run(const Args& A, bool token, hipStream_t st) {
   using T = typename std::conditional<std::is_same<E, float>::value, Split, E>::type;
   using L = Tile<T, DB>;
-  if (A.rq > 0) {
+  if (A.rq > 0 && token) {
+    constexpr int PITCH = Tile<E, DB>::PITCH;
+    hipLaunchKernelGGL((k_attn_dq_token<E, DB>), dim3(A.waves / 4), dim3(kThreads), 8 * kUnit * PITCH, st, A);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((k_attn_dq_join<E, DB>), dim3((unsigned)(A.rq * A.heads)), dim3(kThreads), 0, st, A);
+    const hipError_t f = hipGetLastError();
+    if (f != hipSuccess) return f;
+  } else if (A.rq > 0) {
     const int64_t tiles = (A.rq * A.per + kRows - 1) / kRows + A.n;
     if (!crowded<T>(DB) && split_keys(A, tiles))
       hipLaunchKernelGGL((k_attn_dq<T, (crowded<T>(DB) ? 1 : DB), 2>), dim3((unsigned)(tiles * A.kv)), dim3(2 * kThreads), 8 * L::BYTES, st, A);
@@ -575,18 +659,18 @@ hipError_t run(const Args& A, hipStream_t st) {
                        2 * ((crowded<T>(DB) ? 0 : KEYS) + kQRows) * L::PITCH * L::PL + 2 * kQRows * 4, st, B);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    if (p.parts) hipLaunchKernelGGL((k_attn_dkv_join<E, DB>), dim3((unsigned)p.items), dim3(4 * KEYS), 0, st, B);
+    if (p.parts) hipLaunchKernelGGL((k_attn_dkv_join<E, DB>), dim3((unsigned)p.items, DB), dim3(4 * KEYS), 0, st, B);
   }
   return hipGetLastError();
 }
 
 template <typename T>
-hipError_t run_db(const Args& A, hipStream_t st) {
+hipError_t run_db(const Args& A, bool token, hipStream_t st) {
   switch ((A.d + 31) / 32) {
-    case 1: return run<T, 1>(A, st);
-    case 2: return run<T, 2>(A, st);
-    case 3: return run<T, 3>(A, st);
-    default: return run<T, 4>(A, st);
+    case 1: return run<T, 1>(A, token, st);
+    case 2: return run<T, 2>(A, token, st);
+    case 3: return run<T, 3>(A, token, st);
+    default: return run<T, 4>(A, token, st);
   }
 }
 
@@ -597,7 +681,9 @@ size_t backward_part_bytes(int64_t rq, int64_t rk, int n, int kv, int per, int d
   return rk > 0 ? (size_t)key_plan(rq, rk, n, kv, per, d, bf16).slots * 2 * keys_of(bf16, blocks) * blocks * 32 * sizeof(float) : 0;
 }
 
-hipError_t launch_backward(const Args& A, bool bf16, hipStream_t st) { return bf16 ? run_db<__bf16>(A, st) : run_db<float>(A, st); }
+hipError_t launch_backward(const Args& A, bool bf16, bool token, hipStream_t st) {
+  return bf16 ? run_db<__bf16>(A, token, st) : run_db<float>(A, token, st);
+}
 
 }  // namespace attn
 }  // namespace dnb

@@ -474,6 +474,144 @@ __device__ __forceinline__ bool find_tile(const Args& A, int64_t tile, F tiles_o
   return false;
 }
 
+// 32 packed rows of a wave, a lane's own being m0 + (lane & 31)
+struct RowTile {
+  bool valid;
+  int head, sees, most, least;  // keys that the lane's row sees; that the wave's last row, its first row see
+  int64_t qrow;
+  static __device__ __forceinline__ int seen(const Args& A, const Seq& S, int m) {
+    return A.causal ? min(max(m / A.per + S.nk - S.nq + 1, 0), S.nk) : S.nk;
+  }
+  __device__ __forceinline__ RowTile(const Args& A, const Seq& S, int g, int m0) {
+    const int M = S.nq * A.per, m = m0 + (lane_id() & 31), row = m / A.per;
+    valid = m < M;
+    head = g * A.per + m - row * A.per;
+    qrow = (int64_t)S.q0 + row;
+    sees = seen(A, S, m);
+    most = m0 >= M ? 0 : seen(A, S, min(m0 + 31, M - 1));
+    least = seen(A, S, m0);
+  }
+};
+
+// ---- work split over the keys.  Items are (sequence, tile of 32 packed rows, key/value head), in that order,
+// a unit is 32 keys of an item, and all units of all items lie on one line, which is cut into equal parts,
+// one a wave: whatever the lengths, no wave has more than one unit more than another.  A part of an item
+// leaves its result in slot (wave + item): walking along the line, each next part has a next wave or a next
+// item.
+constexpr int kItemRows = 32, kUnit = 32;
+
+// The rule: where tiles of 128 rows are so few that most of the chip would be idle, or mostly empty, and the
+// keys are long enough to be worth the second launch.  Lengths are on the device; the longest sequence is
+// taken to have about twice the average's keys.  (Measured with the tiles: 188 queries of 6 heads over up to
+// 3289 keys, fp32, 183 us; 523 of one head over up to 2853, bf16, 44 us.)
+inline bool split_rows(int64_t rq, int64_t rk, int64_t n, int64_t kv, int64_t per, bool bf16) {
+  const int64_t tiles = (rq * per / 128 + n) * kv;
+  return (rq * per <= kItemRows * n || tiles <= (bf16 ? 40 : 96)) && 2 * rk >= (n + 1) * (bf16 ? 400 : 256);
+}
+
+struct Line {
+  int64_t units, items;  // of this lane's sequence
+};
+__device__ __forceinline__ Line line_of(const Args& A, const Seq& s) {
+  const int64_t items = ((int64_t)s.nq * A.per + kItemRows - 1) / kItemRows * A.kv;
+  return {items * ((s.nk + kUnit - 1) / kUnit), items};
+}
+__device__ __forceinline__ int64_t line_total(const Args& A) {
+  int64_t u = 0;
+  for (int i = lane_id(); i < A.n; i += 64) u += line_of(A, seq_at(A, i)).units;
+  return bcast64(wave_scan(u), 63);
+}
+constexpr int64_t slot_floats(int dp) { return (int64_t)kItemRows * dp + 2 * kItemRows; }
+
+// f(sequence, key/value head, first packed row, first unit, unit after the last, slot) for every part of wave w.
+// Where on the line it is is looked up again for every part: what the search needs would not fit the registers
+// beside what f keeps.
+template <typename F>
+__device__ __forceinline__ void each_part(const Args& A, int64_t w, F f) {
+  const int l = lane_id();
+  const int64_t total = line_total(A), W = min((int64_t)A.waves, total);
+  if (w >= W) return;
+  int64_t a = w * total / W;
+  const int64_t b = (w + 1) * total / W;
+  while (a < b) {
+    int64_t u0 = 0, i0 = 0, j = 0, slot = -1;  // units and items before the 64 sequences at hand
+    Seq S = {};
+    int first = 0, last = 0;
+    for (int base = 0; base < A.n; base += 64) {
+      Seq mine = {};
+      Line ln = {};
+      if (base + l < A.n) {
+        mine = seq_at(A, base + l);
+        ln = line_of(A, mine);
+      }
+      const int64_t ue = wave_scan(ln.units), ie = wave_scan(ln.items);
+      const uint64_t past = __ballot(u0 + ue > a);
+      if (past) {
+        const int at = __builtin_ctzll(past);
+        S = bcast(mine, at);
+        const int64_t in = a - u0 - bcast64(ue - ln.units, at);
+        const int len = (S.nk + kUnit - 1) / kUnit;
+        j = in / len;
+        first = (int)(in - j * len);
+        last = (int)min((int64_t)len, first + b - a);
+        slot = w + i0 + bcast64(ie - ln.items, at) + j;
+        break;
+      }
+      u0 += bcast64(ue, 63);
+      i0 += bcast64(ie, 63);
+    }
+    if (slot < 0 || slot >= A.slots) return;  // offsets that decrease
+    f(S, (int)(j % A.kv), (int)(j / A.kv) * kItemRows, first, last, slot);
+    a += last - first;
+  }
+}
+
+// The parts of row id of (query rows, heads): n of them from `slot` on, in each of which it is row r.
+struct RowParts {
+  bool found;
+  int head, r, n;
+  int64_t qrow, slot;
+};
+__device__ __forceinline__ RowParts row_parts(const Args& A, int64_t id) {
+  const int l = lane_id();
+  RowParts P = {};
+  P.qrow = id / A.heads;
+  P.head = (int)(id - P.qrow * A.heads);
+  int64_t u0 = 0, i0 = 0, su = 0, si = 0;
+  Seq S = {};
+  for (int base = 0; base < A.n; base += 64) {
+    Seq mine = {};
+    Line ln = {};
+    if (base + l < A.n) {
+      mine = seq_at(A, base + l);
+      ln = line_of(A, mine);
+    }
+    const int64_t ue = wave_scan(ln.units), ie = wave_scan(ln.items);
+    const uint64_t holds = __ballot(mine.q0 <= P.qrow && P.qrow < (int64_t)mine.q0 + mine.nq);
+    if (holds) {
+      const int at = __builtin_ctzll(holds);
+      S = bcast(mine, at);
+      su = u0 + bcast64(ue - ln.units, at);
+      si = i0 + bcast64(ie - ln.items, at);
+      P.found = true;
+    }
+    u0 += bcast64(ue, 63);
+    i0 += bcast64(ie, 63);
+  }
+  const int len = (S.nk + kUnit - 1) / kUnit;
+  if (!P.found || len == 0) return P;
+  const int64_t total = u0, W = min((int64_t)A.waves, total);
+  const int g = P.head / A.per, m = (int)(P.qrow - S.q0) * A.per + P.head - g * A.per;
+  const int64_t j = (int64_t)(m / kItemRows) * A.kv + g, first = su + j * len;
+  // unit u is wave ((u + 1) W - 1) / total's
+  const int64_t w0 = ((first + 1) * W - 1) / total, w1 = ((first + len) * W - 1) / total;
+  P.r = m % kItemRows;
+  P.n = (int)(w1 - w0 + 1);
+  P.slot = si + j + w0;
+  if (P.slot + P.n > A.slots) P.found = false;  // offsets that decrease
+  return P;
+}
+
 }  // namespace
 }  // namespace attn
 }  // namespace dnb

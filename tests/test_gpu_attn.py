@@ -306,3 +306,39 @@ def test_in_a_graph_and_on_another_stream(dnb, token):
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, (out, lse, dq, dk, dv)))
     p.close()
+
+
+# few rows and long keys: the work is split over the keys, forward and for dq
+SPLIT = {"one": ([1], [3000]), "prompt": ([700], [700]), "chunks": ([40, 3, 100, 0, 1], [900, 1200, 700, 50, 2000]),
+         "more_queries": ([90, 700], [30, 690]), "empty": ([5, 0, 33, 2], [0, 900, 3000, 1])}
+
+
+@pytest.mark.parametrize("causal", [True, False], ids=["causal", "full"])
+@pytest.mark.parametrize("lengths", SPLIT, ids=list(SPLIT))
+@pytest.mark.parametrize("heads,kv_heads,dim", [(1, 1, 128), (6, 2, 64), (7, 1, 40)])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_few_rows_over_long_keys(dnb, dtype, heads, kv_heads, dim, lengths, causal):
+    q, k = SPLIT[lengths]
+    p = Problem(dnb, dtype, q, k, heads, kv_heads, dim, causal, capacity=[x + 9 for x in k])
+    p.check_forward()
+    p.check_backward()
+    p.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_few_rows_over_long_keys_repeat_and_offsets_are_cut(dnb, dtype):
+    p = Problem(dnb, dtype, [20, 60, 5], [700, 1500, 900], 4, 2, 96, True)
+    out, lse = p.forward()
+    grads = p.backward(out, lse)
+    for _ in range(3):
+        p.ws.fill_(255)
+        o, l = p.forward()
+        assert torch.equal(o, out) and torch.equal(l, lse)
+        assert all(torch.equal(a, b) for a, b in zip(p.backward(o, l), grads))
+    big = 2 ** 31 - 1
+    p.o_ = (torch.cat([ints([-5]), p.o_[0][1:-1], ints([big])]), torch.cat([ints([-big]), p.o_[1][1:-1], ints([big])]), None)
+    o, l = p.forward()
+    assert torch.equal(o, out) and all(torch.equal(a, b) for a, b in zip(p.backward(o, l), grads))
+    p.o_ = (ints([9, 2, big, -7]), ints([100, -3, 50, 7]), ints([big, 5, -1]))   # what comes out is undefined
+    p.backward(*p.forward())
+    p.close()
