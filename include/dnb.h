@@ -478,7 +478,8 @@ int dnb_op_maxpool3s2_backward(const void* dout, const void* pos, void* din, int
  *   written; dk and dv of rows that are not in use yet are zero.  Offsets that leave the tensors are cut
  *   to them, and offsets that decrease give undefined values in the outputs, but no access outside.
  * A value that is infinite or NaN in a key or value reaches the queries that see it, and may reach those
- * of the same sequence that a causal mask keeps from it. */
+ * of the same sequence that a causal mask keeps from it.  DNB_F32: where many rows share keys, infinities
+ * and magnitudes above 3.39e38 in q, k, v and dout count as 3.39e38 (the largest bf16). */
 typedef struct dnb_attn dnb_attn; /* opaque, host side only */
 typedef struct {
   int32_t heads, kv_heads;  /* heads a multiple of kv_heads                                      */
@@ -498,7 +499,8 @@ void dnb_attn_destroy(dnb_attn* plan);
 size_t dnb_attn_workspace_bytes(const dnb_attn* plan);
 int dnb_attn_forward(const dnb_attn* plan, const void* q, const void* k, const void* v, const int32_t* q_offsets,
                      const int32_t* k_offsets, const int32_t* k_lengths, void* out, float* lse, void* workspace, void* stream);
-/* out and lse are the forward's. */
+/* out and lse are the forward's.  (DNB_BF16: sum_d dout out, which the gradients contain, is taken from
+ * q, k, v, dout and lse for rows that see few keys, where out's rounding would show.) */
 int dnb_attn_backward(const dnb_attn* plan, const void* q, const void* k, const void* v, const void* out, const float* lse,
                       const void* dout, const int32_t* q_offsets, const int32_t* k_offsets, const int32_t* k_lengths, void* dq,
                       void* dk, void* dv, void* workspace, void* stream);

@@ -18,10 +18,13 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kRows = 128;  // packed rows of a workgroup of k_attn_dq, 32 a wave
 
-// Rounding ds to bf16 is off by as much as rounding dq and dk themselves is; where a row sees few keys, D adds
-// the rounding of out, which is large there, and so is ds.  Rows that see up to this many keys multiply what
-// the rounding of ds left as well: dq and dk of packed documents are then 1.3 times as far from the exact
-// gradient as its rounding to bf16 is, without it 1.5 times.
+// bf16: where a row sees few keys its ds is large, and two roundings show in it.  Rows that see up to this many
+// keys therefore
+//  - multiply what rounding ds to bf16 left as well, in dq and dk;
+//  - take D from sum_j p_j (dout v^T)_j, which it equals, and not from out, whose rounding is then as large as
+//    ds: one more pass over their few keys (k_attn_dq, where a whole workgroup's rows are such rows).
+// dq and dk of some ten tokens are 1.1 times as far from the exact gradient as its rounding to bf16 alone, of 33
+// tokens 1.4 times, where both were 1.6 times without; a step of 7185 packed tokens takes 3% longer.
 constexpr int kFineKeys = 128;
 
 // Two rows of registers for q and dout: above head_dim 64 Split takes those of two waves.
@@ -52,13 +55,12 @@ __global__ __launch_bounds__(kThreads * KH, crowded<T>(DB) ? 1 : 2) void k_attn_
   Columns<T, DB> qf, df;
   load_cols<T, DB>(qf, (const E*)A.q + qrow * A.qs + (int64_t)head * A.d, valid, A.d);
   load_cols<T, DB>(df, (const E*)A.dout + qrow * A.os + (int64_t)head * A.d, valid, A.d);
-  const float D = dot_rows<T, DB>((const E*)A.out + qrow * A.os + (int64_t)head * A.d, (const E*)A.dout + qrow * A.os + (int64_t)head * A.d, valid, A.d);
+  float D = dot_rows<T, DB>((const E*)A.out + qrow * A.os + (int64_t)head * A.d, (const E*)A.dout + qrow * A.os + (int64_t)head * A.d, valid, A.d);
   // lse = -inf: the row sees no key, and none of its p may be anything but 0
   float lse2 = INFINITY;
   if (valid) {
     const float v = A.lse[(int64_t)head * A.rq + qrow];
     if (v != -INFINITY) lse2 = v * kLog2e;
-    if (l < 32 && kh == 0) A.rowdot[(int64_t)head * A.rq + qrow] = D;
   }
   const bool fine = sizeof(E) == 2 && most <= kFineKeys;
   f32x16 acc[DB];
@@ -77,6 +79,33 @@ __global__ __launch_bounds__(kThreads * KH, crowded<T>(DB) ? 1 : 2) void k_attn_
     sk.store(lds + buf * 2 * KH * L::BYTES, threadIdx.x);
     sv.store(lds + (buf * 2 + 1) * KH * L::BYTES, threadIdx.x);
   };
+  if (sizeof(E) == 2 && all <= kFineKeys) {  // uniform in the workgroup: D from p and dout v^T
+    float d = 0.f;
+    for (int at = 0; at < all; at += STEP) {
+      fetch(at);
+      put(0);
+      __syncthreads();
+      const int k0 = at + kh * KT;
+      const lds_t kt = lds + kh * KT * L::PITCH;
+#pragma unroll 1
+      for (int b = 0; b < NB && k0 < most; ++b) {
+        const f32x16 s = row_mul<T, DB, false, STEP>(kt, 32 * b, qf);
+        const f32x16 dp = row_mul<T, DB, false, STEP>(kt + KH * L::BYTES, 32 * b, df);
+#pragma unroll
+        for (int i = 0; i < 16; ++i)
+          d += k0 + 32 * b + row_of(i) >= sees ? 0.f : __builtin_amdgcn_exp2f(fmaf(s[i], A.c, -lse2)) * dp[i];
+      }
+      __syncthreads();
+    }
+    D = half_sum(d);
+    if constexpr (KH == 2) {  // the other half of the waves has the other tiles
+      lds_write(lds + 4 * threadIdx.x, D);
+      __syncthreads();
+      D += lds_read<float>(lds + 4 * (threadIdx.x ^ 256));
+      __syncthreads();
+    }
+  }
+  if (valid && l < 32 && kh == 0) A.rowdot[(int64_t)head * A.rq + qrow] = D;
   if (all > 0) {
     fetch(0);
     put(0);
@@ -151,12 +180,11 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DB <= 2 ? 2 : 1) void k
     Columns<T, DB> qf, df;
     load_cols<T, DB>(qf, (const T*)A.q + R.qrow * A.qs + (int64_t)R.head * A.d, R.valid, A.d);
     load_cols<T, DB>(df, (const T*)A.dout + at, R.valid, A.d);
-    const float D = dot_rows<T, DB>((const T*)A.out + at, (const T*)A.dout + at, R.valid, A.d);
+    float D = dot_rows<T, DB>((const T*)A.out + at, (const T*)A.dout + at, R.valid, A.d);
     float lse2 = INFINITY;
     if (R.valid) {
       const float v = A.lse[(int64_t)R.head * A.rq + R.qrow];
       if (v != -INFINITY) lse2 = v * kLog2e;
-      if (l < 32 && first == 0) A.rowdot[(int64_t)R.head * A.rq + R.qrow] = D;
     }
     const bool fine = L::BF && R.most <= kFineKeys;
     f32x16 acc[DB];
@@ -168,7 +196,23 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DB <= 2 ? 2 : 1) void k
       sk.load(kb + (int64_t)u * kUnit * A.ks, A.ks, S.nk - u * kUnit, A.d);
       sv.load(vb + (int64_t)u * kUnit * A.vs, A.vs, S.nk - u * kUnit, A.d);
     };
-    const int end = min(last, (R.most + kUnit - 1) / kUnit);
+    const int units = (R.most + kUnit - 1) / kUnit, end = min(last, units);
+    if (fine && first == 0 && last >= units) {  // all of the keys that the tile sees: D from p and dout v^T
+      float d = 0.f;
+      for (int u = 0; u < end; ++u) {
+        fetch(u);
+        sk.store(kt, l);
+        sv.store(vt, l);
+        __builtin_amdgcn_wave_barrier();
+        const f32x16 s = row_mul<T, DB, false, kUnit>(kt, 0, qf);
+        const f32x16 dp = row_mul<T, DB, false, kUnit>(vt, 0, df);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) d += u * kUnit + row_of(i) >= R.sees ? 0.f : __builtin_amdgcn_exp2f(fmaf(s[i], A.c, -lse2)) * dp[i];
+        __builtin_amdgcn_wave_barrier();
+      }
+      D = half_sum(d);
+    }
+    if (R.valid && l < 32 && first == 0) A.rowdot[(int64_t)R.head * A.rq + R.qrow] = D;
     if (first < end) fetch(first);
     for (int u = first; u < end; ++u) {
       sk.store(kt, l);

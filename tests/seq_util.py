@@ -81,6 +81,10 @@ def attn_backward(q, k, v, out, lse, dout, q_offsets, k_offsets, k_lengths, caus
             e = f * ((d + 8) * size + 4 * torch.nan_to_num(lse[h, qs][:, None], neginf=0).abs() + 16)
             ep = (r_p + e + f * n) * p
             es = (r_p + e + f * n) * ds.abs() + p * f * (d + 4) * (big + bigD)
+            # bf16: sum_d dout out of rows that see few keys may be taken from p and dout v^T instead; the given out
+            # is off by its rounding, half a step, and so is the sum from it
+            few = seen.sum(1, keepdim=True) <= 160
+            es = es + few * r_p * p * (do.abs() * o.abs()).sum(1, keepdim=True)
             dq[qs, h] = scale * ds @ b
             tq[qs, h] = scale * es @ b.abs()
             dk[ks, g] += scale * ds.T @ a
