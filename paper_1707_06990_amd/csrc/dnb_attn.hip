@@ -128,13 +128,17 @@ __global__ __launch_bounds__(kThreads * KH, 2) void k_attn(Args A) {
   __syncthreads();
   auto step = [&](int at, auto which) {
     constexpr int BUF = which;
-    if (at + STEP < all) fetch(at + STEP);
     const int k0 = at + kh * KT;
+    if (k0 >= most && at + STEP < all) fetch(at + STEP);
     if (k0 < most) {
       const lds_t kt = lds + (BUFS == 1 ? 0 : BUF * 2 * KH * L::BYTES) + kh * KT * L::PITCH;
       f32x16 s[NB];
 #pragma unroll
       for (int b = 0; b < NB; ++b) s[b] = row_mul<T, DB, HOLD, STEP>(kt, 32 * b, qf);
+      // four reads of LDS ahead of their products, and the next tile's registers not taken before: 381 -> 367 us
+      // for 12597 packed queries of 32 heads
+      if constexpr (L::PL == 1) read_ahead<KH == 1 ? 4 : 2, NB * L::NS>();
+      if (at + STEP < all) fetch(at + STEP);
       if (k0 + KT > least) {
 #pragma unroll
         for (int b = 0; b < NB; ++b) hide(s[b], k0 + 32 * b, sees);

@@ -113,14 +113,16 @@ __global__ __launch_bounds__(kThreads * KH, crowded<T>(DB) ? 1 : 2) void k_attn_
   __syncthreads();
   auto step = [&](int at, auto which) {
     constexpr int BUF = which;
-    if (at + STEP < all) fetch(at + STEP);
     const int k0 = at + kh * KT;
+    if (k0 >= most && at + STEP < all) fetch(at + STEP);
     if (k0 < most) {
       const lds_t kt = lds + BUF * 2 * KH * L::BYTES + kh * KT * L::PITCH;
 #pragma unroll
       for (int b = 0; b < NB; ++b) {
         f32x16 s = row_mul<T, DB, HOLD, STEP>(kt, 32 * b, qf);
         const f32x16 dp = row_mul<T, DB, HOLD, STEP>(kt + KH * L::BYTES, 32 * b, df);
+        if constexpr (L::PL == 1) read_ahead<4, 2 * L::NS>();  // (as in k_attn)
+        if (b == 0 && at + STEP < all) fetch(at + STEP);
 #pragma unroll
         for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], A.c, -lse2)) * (dp[i] - D);
         if (k0 + 32 * b + 32 > least) {

@@ -281,6 +281,18 @@ __device__ __forceinline__ void col_mul(lds_t tile, int row0, const f32x16& s, f
   }
 }
 
+// An order for the compiler's scheduler: N products, each with a read of LDS, AHEAD reads before the first.
+template <int AHEAD, int N>
+__device__ __forceinline__ void read_ahead() {
+  __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+  }
+  __builtin_amdgcn_sched_barrier(0);
+}
+
 // A loaded piece to its place in a tile of TR rows
 template <typename T, int DB, int TR>
 __device__ __forceinline__ void write_piece(lds_t to, const u32x4* r) {
