@@ -7,9 +7,12 @@
 // One pass over the keys, with the running maximum and sum of the softmax (both fp32, in units of
 // log 2).  The sum so far and its weights are only rescaled when the maximum has grown by more than
 // 8 (a factor of 256, far from anything that fp32 sums lose), which after the first tiles it hardly does.
+// 12597 packed tokens of 32 heads of 128 on 8 key/value heads, causal: 362 us, 885 TFLOP/s; matrix cores
+// 41% busy and vector units 39%: a wave is at either, and registers allow two waves a SIMD.
 //
 // k_attn_token / k_attn_join: where few rows would leave most compute units idle (answering: one query a
-// request) the work is split over the keys instead.  With one query a request it is bound by reading them.
+// request) the work is split over the keys instead.  With one query a request it is bound by reading them: 165 MB
+// of keys and values in 35 us (4.7 TB/s), and 6 us for the join.
 #include <hip/hip_runtime.h>
 
 #include <cmath>

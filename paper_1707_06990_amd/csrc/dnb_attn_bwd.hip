@@ -5,6 +5,8 @@
 // in fp32 in memory, results that repeat bit for bit.  That costs seven matrix products where five would
 // do.  k_attn_dq walks over the keys for 32 packed rows a wave and leaves D for k_attn_dkv, which walks
 // over the rows of all heads of a group for 32 keys a wave (the sum over shared heads is part of it).
+// 7185 packed tokens of 16 heads of 128 on 4 key/value heads, causal: 105 us for dq, 159 us for dk and dv and 16
+// for their join.  Both are bound by the chain products - exponentials - products of the two waves that fit a SIMD.
 #include <hip/hip_runtime.h>
 
 #include <type_traits>

