@@ -541,8 +541,9 @@ int dnb_op_norm_residual_backward(const void* b, const void* h_new, const float*
 
 /* Clipping by the global norm of many tensors: with norm = sqrt(sum of all squares) and
  * coef = min(1, max_norm / (norm + 1e-6)), dst[i] = coef * src[i] (the same memory is allowed) and
- * norm[0] = norm, norm[1] = coef (two floats on the device).  The squares are summed in 64 bits across
- * a tensor's parts, in an order that does not change.  A plan is made of the tensors' addresses, counts
+ * norm[0] = norm, norm[1] = coef (two floats on the device).  Squares, their sums (in an order that does
+ * not change), norm and coef are 64 bits, so that finite values of any magnitude are scaled by the right
+ * coef; norm[0] is infinite where norm is beyond fp32.  A plan is made of the tensors' addresses, counts
  * and types; its table is copied to the device by the caller (dnb_clip_table writes it to host memory)
  * and given to every run, with a workspace (both 16-byte aligned). */
 typedef struct dnb_clip dnb_clip; /* opaque, host side only */

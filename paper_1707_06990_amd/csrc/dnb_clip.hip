@@ -2,7 +2,8 @@
 //   norm = sqrt(sum over all tensors of g^2)   coef = min(1, max_norm / (norm + 1e-6))   dst = coef * src
 // Two launches whatever the number of tensors.  Tensors are cut into chunks, which are listed in a table
 // that the caller keeps on the device; a workgroup takes every G-th chunk, so the sums have one order.
-// Squares are summed in fp32 over a chunk's share of a thread (64 values) and in fp64 from there on.
+// Squares and their sums are fp64, and so are norm and coef until they are rounded for the caller: the squares of fp32
+// values leave fp32's range from 1.9e19 on (an exploding gradient, which is what clipping is for) and below 1e-23.
 // Bound by memory: src is read twice, since nothing may be written before the whole norm is known.  The
 // second launch goes through the chunks backwards: what was read last is in the 256 MB of the last cache,
 // and it writes past that cache, so as not to push out what it has still to read (677 -> 642 us for 612
@@ -32,11 +33,13 @@ struct Chunk {
 
 typedef unsigned u4 __attribute__((ext_vector_type(4)));
 
+__device__ __forceinline__ double square_add(float v, double s) { return fma((double)v, (double)v, s); }
+
 template <typename T>
-__device__ __forceinline__ float square_sum(const Chunk& c) {
+__device__ __forceinline__ double square_sum(const Chunk& c) {
   constexpr int V = 16 / sizeof(T);
   const T* p = (const T*)c.src;
-  float s = 0.f;
+  double s = 0.0;
   int tail = 0;
   if (!(c.flags & 2)) {
     const int vecs = c.count / V;
@@ -46,16 +49,16 @@ __device__ __forceinline__ float square_sum(const Chunk& c) {
       T v[V];
       __builtin_memcpy(v, &q, 16);
 #pragma unroll
-      for (int j = 0; j < V; ++j) s = fmaf((float)v[j], (float)v[j], s);
+      for (int j = 0; j < V; ++j) s = square_add((float)v[j], s);
     }
     tail = vecs * V;
   }
-  for (int i = tail + threadIdx.x; i < c.count; i += kThreads) s = fmaf((float)p[i], (float)p[i], s);
+  for (int i = tail + threadIdx.x; i < c.count; i += kThreads) s = square_add((float)p[i], s);
   return s;
 }
 
 template <typename T>
-__device__ __forceinline__ void scale_chunk(const Chunk& c, float f) {
+__device__ __forceinline__ void scale_chunk(const Chunk& c, float f, float f2) {
   constexpr int V = 16 / sizeof(T);
   const T* p = (const T*)c.src;
   T* y = (T*)c.dst;
@@ -68,14 +71,14 @@ __device__ __forceinline__ void scale_chunk(const Chunk& c, float f) {
       T v[V];
       __builtin_memcpy(v, &q, 16);
 #pragma unroll
-      for (int j = 0; j < V; ++j) v[j] = (T)((float)v[j] * f);
+      for (int j = 0; j < V; ++j) v[j] = (T)((float)v[j] * f * f2);
       uint4 o;
       __builtin_memcpy(&o, v, 16);
       __builtin_nontemporal_store(__builtin_bit_cast(u4, o), reinterpret_cast<u4*>(y) + i);
     }
     tail = vecs * V;
   }
-  for (int i = tail + threadIdx.x; i < c.count; i += kThreads) y[i] = (T)((float)p[i] * f);
+  for (int i = tail + threadIdx.x; i < c.count; i += kThreads) y[i] = (T)((float)p[i] * f * f2);
 }
 
 // the sum of a value of every thread of the workgroup, in every thread
@@ -95,7 +98,7 @@ __global__ __launch_bounds__(kThreads) void k_clip_squares(const Chunk* table, i
   double s = 0.0;
   for (int i = blockIdx.x; i < chunks; i += gridDim.x) {
     const Chunk c = table[i];
-    s += (double)(c.flags & 1 ? square_sum<__bf16>(c) : square_sum<float>(c));
+    s += c.flags & 1 ? square_sum<__bf16>(c) : square_sum<float>(c);
   }
   s = block_sum(s);
   if (threadIdx.x == 0) part[blockIdx.x] = s;
@@ -110,17 +113,19 @@ __global__ __launch_bounds__(kThreads) void k_clip_scale(const Chunk* table, int
 #pragma unroll 4
   for (int i = threadIdx.x; i < parts; i += kThreads) s += part[i];
   s = block_sum(s);
-  const float n = (float)sqrt(s);
-  const float c = max_norm / (n + 1e-6f);
-  const float f = c > 1.f ? 1.f : c;  // NaN stays
+  const double n = sqrt(s), c = max_norm / (n + 1e-6);
+  const float coef = (float)(c > 1.0 ? 1.0 : c);  // NaN stays
   if (blockIdx.x == 0 && threadIdx.x == 0) {
-    norm[0] = n;
-    norm[1] = f;
+    norm[0] = (float)n;
+    norm[1] = coef;
   }
+  // a coef that fp32 does not hold to its last bit is applied in two factors, the second a power of two
+  const bool tiny = c < 0x1p-120;
+  const float f = tiny ? (float)(c * 0x1p100) : coef, f2 = tiny ? 0x1p-100f : 1.f;
   while (at >= 0) {
     if (k.src == k.dst && f == 1.f) {  // in place and nothing to do
-    } else if (k.flags & 1) scale_chunk<__bf16>(k, f);
-    else scale_chunk<float>(k, f);
+    } else if (k.flags & 1) scale_chunk<__bf16>(k, f, f2);
+    else scale_chunk<float>(k, f, f2);
     at -= gridDim.x;
     if (at >= 0) k = table[at];
   }
