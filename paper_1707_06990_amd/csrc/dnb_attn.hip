@@ -95,10 +95,11 @@ __global__ __launch_bounds__(kThreads * KH, 2) void k_attn(Args A) {
   constexpr int BUFS = buffers<T>(DB);
   extern __shared__ __attribute__((aligned(512))) char shared[];  // [BUFS][K tiles, V tiles]
   const lds_t lds = lds_start(shared);
-  const int g = blockIdx.x % A.kv, l = lane_id(), wave = (threadIdx.x >> 6) & 3, kh = KH == 1 ? 0 : (int)(threadIdx.x >> 8);
+  const unsigned id = flat_block();
+  const int g = id % A.kv, l = lane_id(), wave = (threadIdx.x >> 6) & 3, kh = KH == 1 ? 0 : (int)(threadIdx.x >> 8);
   Seq S;
   int t, count;
-  if (!find_tile(A, blockIdx.x / A.kv, [&](const Seq& s) { return (int)(((int64_t)s.nq * A.per + kRows - 1) / kRows); }, &S, &t, &count))
+  if (!find_tile(A, id / A.kv, [&](const Seq& s) { return (int)(((int64_t)s.nq * A.per + kRows - 1) / kRows); }, &S, &t, &count))
     return;
   if (A.causal) t = count - 1 - t;  // the rows that see most keys go first
   const RowTile R0(A, S, g, t * kRows + wave * 32);
@@ -244,7 +245,7 @@ template <typename T, int DB>
 __global__ __launch_bounds__(kThreads) void k_attn_join(Args A) {
   constexpr int DP = 32 * DB, LANES = DP / 4, G = kThreads / LANES;
   __shared__ float red[G][DP + 2];
-  const RowParts P = row_parts(A, blockIdx.x);
+  const RowParts P = row_parts(A, flat_block());
   if (!P.found) return;  // a row of no sequence
   const int grp = threadIdx.x / LANES, c = threadIdx.x - grp * LANES;
   float M = -INFINITY, sum = 0.f;
@@ -295,16 +296,16 @@ hipError_t run_forward(const Args& A, bool token, hipStream_t st) {
     hipLaunchKernelGGL((k_attn_token<T, DB>), dim3(A.waves / 4), dim3(kThreads), 8 * kUnit * PITCH, st, A);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((k_attn_join<T, DB>), dim3((unsigned)(A.rq * A.heads)), dim3(kThreads), 0, st, A);
+    hipLaunchKernelGGL((k_attn_join<T, DB>), flat_grid(A.rq * A.heads), dim3(kThreads), 0, st, A);
     return hipGetLastError();
   }
   using M = typename std::conditional<std::is_same<T, float>::value, Split, T>::type;
   constexpr int BYTES = Tile<M, DB>::BYTES;
   const int64_t tiles = (A.rq * A.per + kRows - 1) / kRows + A.n;
   if (split_keys(A, tiles))
-    hipLaunchKernelGGL((k_attn<M, DB, 2>), dim3((unsigned)(tiles * A.kv)), dim3(2 * kThreads), 4 * buffers<M>(DB) * BYTES, st, A);
+    hipLaunchKernelGGL((k_attn<M, DB, 2>), flat_grid(tiles * A.kv), dim3(2 * kThreads), 4 * buffers<M>(DB) * BYTES, st, A);
   else
-    hipLaunchKernelGGL((k_attn<M, DB, 1>), dim3((unsigned)(tiles * A.kv)), dim3(kThreads), 2 * buffers<M>(DB) * BYTES, st, A);
+    hipLaunchKernelGGL((k_attn<M, DB, 1>), flat_grid(tiles * A.kv), dim3(kThreads), 2 * buffers<M>(DB) * BYTES, st, A);
   return hipGetLastError();
 }
 

@@ -42,10 +42,11 @@ __global__ __launch_bounds__(kThreads * KH, crowded<T>(DB) ? 1 : 2) void k_attn_
   constexpr bool HOLD = DB <= (L::PL == 1 && KH == 1 ? 3 : 2);
   extern __shared__ __attribute__((aligned(512))) char shared[];  // [2][K tiles, V tiles]
   const lds_t lds = lds_start(shared);
-  const int g = blockIdx.x % A.kv, l = lane_id(), wave = (threadIdx.x >> 6) & 3, kh = KH == 1 ? 0 : (int)(threadIdx.x >> 8);
+  const unsigned id = flat_block();
+  const int g = id % A.kv, l = lane_id(), wave = (threadIdx.x >> 6) & 3, kh = KH == 1 ? 0 : (int)(threadIdx.x >> 8);
   Seq S;
   int t, count;
-  if (!find_tile(A, blockIdx.x / A.kv, [&](const Seq& s) { return (int)(((int64_t)s.nq * A.per + kRows - 1) / kRows); }, &S, &t, &count))
+  if (!find_tile(A, id / A.kv, [&](const Seq& s) { return (int)(((int64_t)s.nq * A.per + kRows - 1) / kRows); }, &S, &t, &count))
     return;
   if (A.causal) t = count - 1 - t;
   const RowTile R0(A, S, g, t * kRows + wave * 32);
@@ -248,7 +249,7 @@ template <typename T, int DB>
 __global__ __launch_bounds__(kThreads) void k_attn_dq_join(Args A) {
   constexpr int DP = 32 * DB, LANES = DP / 4, G = kThreads / LANES;
   __shared__ float red[G][DP];
-  const RowParts P = row_parts(A, blockIdx.x);
+  const RowParts P = row_parts(A, flat_block());
   if (!P.found) return;
   const int grp = threadIdx.x / LANES, c = threadIdx.x - grp * LANES;
   if (grp < G) {
@@ -420,7 +421,7 @@ __global__ __launch_bounds__(4 * keys_of(sizeof(elem_t<T>) == 2, DB), crowded<T>
   auto over = [&](int x) { return (int)(((float)x + 0.5f) * inv); };
 
   const bool whole = A.waves == 0;  // a workgroup an item, not a part of the line
-  int64_t w = blockIdx.x, a = 0, b = 1;
+  int64_t w = flat_block(), a = 0, b = 1;
   if (!whole) {
     const int64_t total = key_total<KEYS, BF>(A), W = key_parts(total, A.waves, BF);
     if (w >= W) return;
@@ -608,6 +609,7 @@ __global__ __launch_bounds__(4 * keys_of(sizeof(T) == 2, DB)) void k_attn_dkv_jo
   constexpr bool BF = sizeof(T) == 2;
   constexpr int KEYS = keys_of(BF, DB), KB = KEYS / 32;
   const int l = lane_id(), wave = threadIdx.x >> 6;
+  const int64_t item = flat_block();
   int64_t u0 = 0, i0 = 0, su = 0, si = 0;
   Seq S = {};
   bool found = false;
@@ -621,7 +623,7 @@ __global__ __launch_bounds__(4 * keys_of(sizeof(T) == 2, DB)) void k_attn_dkv_jo
       items = k.tiles * A.kv;
     }
     const int64_t ue = wave_scan(cost), ie = wave_scan(items);
-    const uint64_t past = __ballot(i0 + ie > (int64_t)blockIdx.x);
+    const uint64_t past = __ballot(i0 + ie > item);
     if (past && !found) {
       const int at = __builtin_ctzll(past);
       S = bcast(mine, at);
@@ -634,14 +636,14 @@ __global__ __launch_bounds__(4 * keys_of(sizeof(T) == 2, DB)) void k_attn_dkv_jo
   }
   if (!found) return;
   const KeyLine<KEYS, BF> line(A, S);
-  const int64_t total = u0, W = key_parts(total, A.waves, BF), item = blockIdx.x;
+  const int64_t total = u0, W = key_parts(total, A.waves, BF);
   const int g = (int)((item - si) / line.tiles);
   const int64_t t = (item - si) - g * line.tiles;
   const int64_t from = su + g * line.before(line.tiles) + line.before(t), to = from + line.before(t + 1) - line.before(t);
   // unit u of the line is workgroup ((u + 1) W - 1) / total's
   const int64_t w0 = ((from + 1) * W - 1) / total, w1 = (to * W - 1) / total;
   if (w0 == w1 || w1 + item >= A.slots) return;
-  const int db = blockIdx.y;
+  const int db = blockIdx.z;
   f32x16 sum[1] = {};
 #pragma unroll 4
   for (int64_t w = w0; w <= w1; ++w) {
@@ -685,15 +687,15 @@ hipError_t run(const Args& A, bool token, hipStream_t st) {
     hipLaunchKernelGGL((k_attn_dq_token<E, DB>), dim3(A.waves / 4), dim3(kThreads), 8 * kUnit * PITCH, st, A);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((k_attn_dq_join<E, DB>), dim3((unsigned)(A.rq * A.heads)), dim3(kThreads), 0, st, A);
+    hipLaunchKernelGGL((k_attn_dq_join<E, DB>), flat_grid(A.rq * A.heads), dim3(kThreads), 0, st, A);
     const hipError_t f = hipGetLastError();
     if (f != hipSuccess) return f;
   } else if (A.rq > 0) {
     const int64_t tiles = (A.rq * A.per + kRows - 1) / kRows + A.n;
     if (!crowded<T>(DB) && split_keys(A, tiles))
-      hipLaunchKernelGGL((k_attn_dq<T, (crowded<T>(DB) ? 1 : DB), 2>), dim3((unsigned)(tiles * A.kv)), dim3(2 * kThreads), 8 * L::BYTES, st, A);
+      hipLaunchKernelGGL((k_attn_dq<T, (crowded<T>(DB) ? 1 : DB), 2>), flat_grid(tiles * A.kv), dim3(2 * kThreads), 8 * L::BYTES, st, A);
     else
-      hipLaunchKernelGGL((k_attn_dq<T, DB, 1>), dim3((unsigned)(tiles * A.kv)), dim3(kThreads), 4 * L::BYTES, st, A);
+      hipLaunchKernelGGL((k_attn_dq<T, DB, 1>), flat_grid(tiles * A.kv), dim3(kThreads), 4 * L::BYTES, st, A);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -703,11 +705,11 @@ hipError_t run(const Args& A, bool token, hipStream_t st) {
     Args B = A;
     B.waves = p.parts;
     B.slots = p.slots;
-    hipLaunchKernelGGL((k_attn_dkv<T, DB>), dim3((unsigned)(p.parts ? p.parts : p.items)), dim3(4 * KEYS),
+    hipLaunchKernelGGL((k_attn_dkv<T, DB>), flat_grid(p.parts ? p.parts : p.items), dim3(4 * KEYS),
                        2 * ((crowded<T>(DB) ? 0 : KEYS) + kQRows) * L::PITCH * L::PL + 2 * kQRows * 4, st, B);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    if (p.parts) hipLaunchKernelGGL((k_attn_dkv_join<E, DB>), dim3((unsigned)p.items, DB), dim3(4 * KEYS), 0, st, B);
+    if (p.parts) hipLaunchKernelGGL((k_attn_dkv_join<E, DB>), flat_grid(p.items, DB), dim3(4 * KEYS), 0, st, B);
   }
   return hipGetLastError();
 }

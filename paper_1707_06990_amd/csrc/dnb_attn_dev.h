@@ -39,6 +39,14 @@ struct Args {
 
 namespace {
 
+// A launch has less than 2^32 threads in one dimension, and there may be more tiles, items or rows of heads than
+// that takes: workgroups are counted over x, then y.
+constexpr unsigned kAcross = 1u << 22;
+inline dim3 flat_grid(int64_t count, unsigned z = 1) {
+  return count <= (int64_t)kAcross ? dim3((unsigned)count, 1, z) : dim3(kAcross, (unsigned)((count + kAcross - 1) / kAcross), z);
+}
+__device__ __forceinline__ unsigned flat_block() { return blockIdx.y * kAcross + blockIdx.x; }
+
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));

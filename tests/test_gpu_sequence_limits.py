@@ -1,0 +1,70 @@
+"""Sequence operators at the sizes where a launch has 2^24 workgroups and more."""
+import math
+
+import pytest
+import torch
+
+import attn_forms
+from seq_util import assert_within, attn_backward, attn_forward
+from test_gpu_attn import ints
+
+pytestmark = pytest.mark.gpu
+
+
+def room(gb):
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < gb * 2 ** 30:
+        pytest.skip(f"needs {gb} GiB of device memory")
+
+
+def test_split_form_with_2_24_rows_of_heads(dnb):
+    """A workgroup joins a (row, head) of the split form: forward and dq, of requests of which few have keys."""
+    n, heads, kv, dim = 4097, 4096, 128, 8
+    rk = 200 * (n + 1)
+    lengths = [40 if i % 997 == 0 else 300 if i == n - 1 else 0 for i in range(n)]
+    assert attn_forms.form("bf16", [1] * n, rk, heads, kv) == "split" and n * heads >= 1 << 24
+    room(20)
+    gen = torch.Generator().manual_seed(1)
+    rand = lambda *s: torch.randn(s, generator=gen).to(torch.bfloat16)
+    mine = [i for i, x in enumerate(lengths) if x]
+    q_few, do_few = rand(len(mine), heads, dim), rand(len(mine), heads, dim)
+    k_few, v_few = rand(sum(lengths), kv, dim), rand(sum(lengths), kv, dim)
+    q, dout = (torch.ones((n, heads, dim), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    q[mine], dout[mine] = q_few.cuda(), do_few.cuda()
+    k, v = (torch.empty((rk, kv, dim), dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    k[:sum(lengths)], v[:sum(lengths)] = k_few.cuda(), v_few.cuda()
+    ko = [0]
+    for x in lengths:
+        ko.append(ko[-1] + x)
+    qo, ko_ = torch.arange(n + 1, dtype=torch.int32, device="cuda"), ints(ko)
+    plan = dnb.dnb_attn_create(heads, kv, dim, n, n, rk, causal=True)
+    ws = torch.empty(dnb.dnb_attn_workspace_bytes(plan), dtype=torch.uint8, device="cuda")
+    out, lse = torch.full_like(q, float("nan")), torch.full((heads, n), float("nan"), device="cuda")
+    dnb.dnb_attn_forward(plan, q, k, v, qo, ko_, None, out, lse, ws)
+    torch.cuda.synchronize()
+    few_o = list(range(len(mine) + 1))
+    few_k = [0] + [ko[i + 1] for i in mine]
+    # heads of some groups only, so that the definition stays small
+    pick = [0, 1, 31, 32, 2048, 4064, 4095]
+    groups = sorted({h // (heads // kv) for h in pick})
+    none = [i for i, x in enumerate(lengths) if not x]
+    assert bool((out[none] == 0).all()) and bool((lse[:, none] == -math.inf).all())
+    assert not bool(torch.isnan(out.float()).any()) and not bool(torch.isnan(lse).any())
+    for h in pick:
+        g = h // (heads // kv)
+        o, l, to, tl = attn_forward(q_few[:, h:h + 1], k_few[:, g:g + 1], v_few[:, g:g + 1], few_o, few_k, None, True)
+        assert_within(out[mine, h:h + 1], o, to, f"out of head {h}")
+        assert_within(lse[h:h + 1, mine], l, tl, f"lse of head {h}")
+    dq, dk, dv = torch.full_like(q, float("nan")), torch.full_like(k, float("nan")), torch.full_like(v, float("nan"))
+    dnb.dnb_attn_backward(plan, q, k, v, out, lse, dout, qo, ko_, None, dq, dk, dv, ws)
+    torch.cuda.synchronize()
+    assert bool((dq[none] == 0).all()) and not bool(torch.isnan(dq.float()).any())
+    used = sum(lengths)
+    for g in groups:
+        hs = slice(g * (heads // kv), (g + 1) * (heads // kv))
+        o, l = out[mine][:, hs].cpu(), lse[hs][:, mine].cpu()
+        want, tol = attn_backward(q_few[:, hs], k_few[:, g:g + 1], v_few[:, g:g + 1], o, l, do_few[:, hs], few_o, few_k, None, True)
+        for got, w, t, name in zip((dq[mine][:, hs], dk[:used, g:g + 1], dv[:used, g:g + 1]), want, tol, ("dq", "dk", "dv")):
+            assert_within(got, w, t, f"{name} of group {g}")
+    assert bool(torch.isnan(dk[used:].float()).all()) and bool(torch.isnan(dv[used:].float()).all())   # rows of no sequence
+    dnb.dnb_attn_destroy(plan)
