@@ -16,6 +16,7 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kMaxAngles = 1024;  // (row, pair) angles of a workgroup in LDS
+constexpr unsigned kAcross = 1u << 22;  // workgroups along x, then z: less than 2^32 threads in one dimension
 
 struct RopeArgs {
   const void* x;
@@ -38,7 +39,8 @@ struct __attribute__((aligned(sizeof(T) * V))) Vec {
 template <typename T, int V, bool HALF>
 __global__ __launch_bounds__(kThreads) void k_rope(RopeArgs A) {
   __shared__ float2 cs[kMaxAngles];
-  const int64_t r0 = (int64_t)blockIdx.x * A.rpw;
+  const int64_t r0 = ((int64_t)blockIdx.z * kAcross + blockIdx.x) * A.rpw;
+  if (r0 >= A.rows) return;
   const int nr = (int)min((int64_t)A.rpw, A.rows - r0);
   const int h0 = blockIdx.y * A.hpw, nh = min(A.hpw, A.heads - h0);
   for (int i = threadIdx.x; i < nr * A.half; i += kThreads) {
@@ -101,7 +103,8 @@ hipError_t launch(RopeArgs A, bool half_order, hipStream_t st) {
   const int64_t want = units >= 4ll * kThreads * 1024 ? 4 * kThreads : kThreads;
   A.rpw = (int)min(max(want / per_row, (int64_t)1), (int64_t)max(1, kMaxAngles / A.half));
   A.hpw = (int)min(max(want / A.uph, (int64_t)1), (int64_t)A.heads);
-  const dim3 grid((unsigned)((A.rows + A.rpw - 1) / A.rpw), (unsigned)((A.heads + A.hpw - 1) / A.hpw));
+  const int64_t across = (A.rows + A.rpw - 1) / A.rpw;
+  const dim3 grid((unsigned)min(across, (int64_t)kAcross), (unsigned)((A.heads + A.hpw - 1) / A.hpw), (unsigned)((across + kAcross - 1) / kAcross));
   if (half_order) hipLaunchKernelGGL((k_rope<T, V, true>), grid, dim3(kThreads), 0, st, A);
   else hipLaunchKernelGGL((k_rope<T, (V < 2 ? 2 : V), false>), grid, dim3(kThreads), 0, st, A);
   return hipGetLastError();

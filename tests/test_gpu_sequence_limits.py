@@ -5,7 +5,7 @@ import pytest
 import torch
 
 import attn_forms
-from seq_util import assert_within, attn_backward, attn_forward
+from seq_util import assert_within, attn_backward, attn_forward, half_step
 from test_gpu_attn import ints
 
 pytestmark = pytest.mark.gpu
@@ -15,6 +15,25 @@ def room(gb):
     torch.cuda.empty_cache()
     if torch.cuda.mem_get_info()[0] < gb * 2 ** 30:
         pytest.skip(f"needs {gb} GiB of device memory")
+
+
+def test_rotary_rows_beyond_2_24_workgroups(dnb):
+    """Rows of 1024 pairs, a workgroup each: in place, since they take 64 GiB."""
+    rows, heads, dim = (1 << 24) + 3, 1024, 2
+    room(75)
+    x = torch.full((rows, heads, dim), 1.0, dtype=torch.bfloat16, device="cuda")
+    pos = torch.arange(rows, dtype=torch.int32, device="cuda")
+    turns = torch.tensor([0.37 / (2 * math.pi)], dtype=torch.float64, device="cuda")
+    dnb.dnb_op_rope_forward(x, pos, turns, x, rows, heads, dim, dim, dnb.DNB_ROPE_HALF, 1.0, dnb.DNB_BF16)
+    angle = pos.double() * 0.37
+    want = torch.stack((torch.cos(angle) - torch.sin(angle), torch.cos(angle) + torch.sin(angle)), 1)
+    # as in test_gpu_rope.py: 8 steps of 2^-24 of |a| + |b| = 2, one rounding, and the product's in 64 bits
+    tol = half_step(torch.bfloat16) * want.abs() + 16 * 2.0 ** -24 + 2 * rows * 2.0 ** -52
+    assert bool(((x[:, 0].double() - want).abs() <= tol).all())
+    for a in range(0, rows, 1 << 19):
+        part = x[a:a + (1 << 19)]
+        assert bool((part == part[:, :1]).all()), a
+    del x, part
 
 
 def test_split_form_with_2_24_rows_of_heads(dnb):
