@@ -78,7 +78,7 @@ __device__ __forceinline__ void online_step(Online<DB>& S, f32x16 (&s)[N], float
 }
 
 // Scores of keys key0 + row_of(i) that a query which sees keys below `sees` does not see
-__device__ __forceinline__ void hide(f32x16& s, int key0, int sees) {
+__device__ __forceinline__ void hide(f32x16& s, unsigned key0, unsigned sees) {
 #pragma unroll
   for (int i = 0; i < 16; ++i)
     s[i] = key0 + row_of(i) >= sees ? -INFINITY : s[i];
@@ -103,9 +103,10 @@ __global__ __launch_bounds__(kThreads * KH, 2) void k_attn(Args A) {
     return;
   if (A.causal) t = count - 1 - t;  // the rows that see most keys go first
   const RowTile R0(A, S, g, t * kRows + wave * 32);
-  const int all = RowTile::seen(A, S, min((t + 1) * kRows, S.nq * A.per) - 1);  // keys that the workgroup's last row sees
+  const unsigned all = RowTile::seen(A, S, min((t + 1) * kRows, S.nq * A.per) - 1);  // keys that the workgroup's last row sees
   const bool valid = R0.valid;
-  const int head = R0.head, sees = R0.sees, most = R0.most, least = R0.least;
+  const int head = R0.head;
+  const unsigned sees = R0.sees, most = R0.most, least = R0.least;
   const int64_t qrow = R0.qrow;
 
   Columns<T, DB> qf;
@@ -117,7 +118,7 @@ __global__ __launch_bounds__(kThreads * KH, 2) void k_attn(Args A) {
   Stage<T, DB, STEP, NT> sk, sv;
   sk.init(threadIdx.x, A.ks, A.d);
   sv.init(threadIdx.x, A.vs, A.d);
-  auto fetch = [&](int k0) {
+  auto fetch = [&](unsigned k0) {
     sk.load(kb + (int64_t)k0 * A.ks, A.ks, S.nk - k0, A.d);
     sv.load(vb + (int64_t)k0 * A.vs, A.vs, S.nk - k0, A.d);
   };
@@ -130,9 +131,9 @@ __global__ __launch_bounds__(kThreads * KH, 2) void k_attn(Args A) {
     put(0);
   }
   __syncthreads();
-  auto step = [&](int at, auto which) {
+  auto step = [&](unsigned at, auto which) {
     constexpr int BUF = which;
-    const int k0 = at + kh * KT;
+    const unsigned k0 = at + kh * KT;
     if (k0 >= most && at + STEP < all) fetch(at + STEP);
     if (k0 < most) {
       const lds_t kt = lds + (BUFS == 1 ? 0 : BUF * 2 * KH * L::BYTES) + kh * KT * L::PITCH;
@@ -155,7 +156,7 @@ __global__ __launch_bounds__(kThreads * KH, 2) void k_attn(Args A) {
     }
     __syncthreads();
   };
-  for (int at = 0; at < all; at += 2 * STEP) {
+  for (unsigned at = 0; at < all; at += 2 * STEP) {
     step(at, std::integral_constant<int, 0>());
     if (at + STEP < all) step(at + STEP, std::integral_constant<int, 1>());
   }
@@ -214,7 +215,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void k_attn_token
       sk.load(kb + (int64_t)u * kUnit * A.ks, A.ks, S.nk - u * kUnit, A.d);
       sv.load(vb + (int64_t)u * kUnit * A.vs, A.vs, S.nk - u * kUnit, A.d);
     };
-    const int end = min(last, (R0.most + kUnit - 1) / kUnit);  // no row of the tile sees what follows
+    const int end = min(last, units_of(R0.most));  // no row of the tile sees what follows
     if (first < end) fetch(first);
     for (int u = first; u < end; ++u) {
       // the tiles are this wave's own, and LDS serves a wave's accesses in their order
@@ -223,7 +224,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 ? 2 : 1) void k_attn_token
       if (u + 1 < end) fetch(u + 1);
       __builtin_amdgcn_wave_barrier();
       f32x16 s[1] = {row_mul<T, DB, false, kUnit>(kt, 0, qf)};
-      if ((u + 1) * kUnit > R0.least) hide(s[0], u * kUnit, R0.sees);
+      if ((u + 1u) * kUnit > R0.least) hide(s[0], u * kUnit, R0.sees);
       online_step<T, DB, 1, false, kUnit>(R, s, A.c, vt, 0);
       __builtin_amdgcn_wave_barrier();
     }

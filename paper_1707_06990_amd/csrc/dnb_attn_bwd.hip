@@ -50,9 +50,10 @@ __global__ __launch_bounds__(kThreads * KH, crowded<T>(DB) ? 1 : 2) void k_attn_
     return;
   if (A.causal) t = count - 1 - t;
   const RowTile R0(A, S, g, t * kRows + wave * 32);
-  const int all = RowTile::seen(A, S, min((t + 1) * kRows, S.nq * A.per) - 1);  // keys that the workgroup's last row sees
+  const unsigned all = RowTile::seen(A, S, min((t + 1) * kRows, S.nq * A.per) - 1);  // keys that the workgroup's last row sees
   const bool valid = R0.valid;
-  const int head = R0.head, sees = R0.sees, most = R0.most, least = R0.least;
+  const int head = R0.head;
+  const unsigned sees = R0.sees, most = R0.most, least = R0.least;
   const int64_t qrow = R0.qrow;
 
   Columns<T, DB> qf, df;
@@ -74,7 +75,7 @@ __global__ __launch_bounds__(kThreads * KH, crowded<T>(DB) ? 1 : 2) void k_attn_
   Stage<T, DB, STEP, NT> sk, sv;
   sk.init(threadIdx.x, A.ks, A.d);
   sv.init(threadIdx.x, A.vs, A.d);
-  auto fetch = [&](int k0) {
+  auto fetch = [&](unsigned k0) {
     sk.load(kb + (int64_t)k0 * A.ks, A.ks, S.nk - k0, A.d);
     sv.load(vb + (int64_t)k0 * A.vs, A.vs, S.nk - k0, A.d);
   };
@@ -84,11 +85,11 @@ __global__ __launch_bounds__(kThreads * KH, crowded<T>(DB) ? 1 : 2) void k_attn_
   };
   if (sizeof(E) == 2 && all <= kFineKeys) {  // uniform in the workgroup: D from p and dout v^T
     float d = 0.f;
-    for (int at = 0; at < all; at += STEP) {
+    for (unsigned at = 0; at < all; at += STEP) {
       fetch(at);
       put(0);
       __syncthreads();
-      const int k0 = at + kh * KT;
+      const unsigned k0 = at + kh * KT;
       const lds_t kt = lds + kh * KT * L::PITCH;
 #pragma unroll 1
       for (int b = 0; b < NB && k0 < most; ++b) {
@@ -114,9 +115,9 @@ __global__ __launch_bounds__(kThreads * KH, crowded<T>(DB) ? 1 : 2) void k_attn_
     put(0);
   }
   __syncthreads();
-  auto step = [&](int at, auto which) {
+  auto step = [&](unsigned at, auto which) {
     constexpr int BUF = which;
-    const int k0 = at + kh * KT;
+    const unsigned k0 = at + kh * KT;
     if (k0 >= most && at + STEP < all) fetch(at + STEP);
     if (k0 < most) {
       const lds_t kt = lds + BUF * 2 * KH * L::BYTES + kh * KT * L::PITCH;
@@ -143,7 +144,7 @@ __global__ __launch_bounds__(kThreads * KH, crowded<T>(DB) ? 1 : 2) void k_attn_
     if (at + STEP < all) put(BUF ^ 1);
     __syncthreads();
   };
-  for (int at = 0; at < all; at += 2 * STEP) {
+  for (unsigned at = 0; at < all; at += 2 * STEP) {
     step(at, std::integral_constant<int, 0>());
     if (at + STEP < all) step(at + STEP, std::integral_constant<int, 1>());
   }
@@ -201,7 +202,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DB <= 2 ? 2 : 1) void k
       sk.load(kb + (int64_t)u * kUnit * A.ks, A.ks, S.nk - u * kUnit, A.d);
       sv.load(vb + (int64_t)u * kUnit * A.vs, A.vs, S.nk - u * kUnit, A.d);
     };
-    const int units = (R.most + kUnit - 1) / kUnit, end = min(last, units);
+    const int units = units_of(R.most), end = min(last, units);
     if (fine && first == 0 && last >= units) {  // all of the keys that the tile sees: D from p and dout v^T
       float d = 0.f;
       for (int u = 0; u < end; ++u) {
@@ -212,7 +213,7 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DB <= 2 ? 2 : 1) void k
         const f32x16 s = row_mul<T, DB, false, kUnit>(kt, 0, qf);
         const f32x16 dp = row_mul<T, DB, false, kUnit>(vt, 0, df);
 #pragma unroll
-        for (int i = 0; i < 16; ++i) d += u * kUnit + row_of(i) >= R.sees ? 0.f : __builtin_amdgcn_exp2f(fmaf(s[i], A.c, -lse2)) * dp[i];
+        for (int i = 0; i < 16; ++i) d += (unsigned)(u * kUnit) + row_of(i) >= R.sees ? 0.f : __builtin_amdgcn_exp2f(fmaf(s[i], A.c, -lse2)) * dp[i];
         __builtin_amdgcn_wave_barrier();
       }
       D = half_sum(d);
@@ -228,9 +229,9 @@ __global__ __launch_bounds__(kThreads, sizeof(T) == 2 && DB <= 2 ? 2 : 1) void k
       const f32x16 dp = row_mul<T, DB, false, kUnit>(vt, 0, df);
 #pragma unroll
       for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], A.c, -lse2)) * (dp[i] - D);
-      if ((u + 1) * kUnit > R.least) {
+      if ((u + 1u) * kUnit > R.least) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] = u * kUnit + row_of(i) >= R.sees ? 0.f : s[i];
+        for (int i = 0; i < 16; ++i) s[i] = (unsigned)(u * kUnit) + row_of(i) >= R.sees ? 0.f : s[i];
       }
       col_mul<T, DB, false, kUnit>(kt, 0, s, acc);
       if (fine) {
@@ -312,7 +313,7 @@ struct KeyLine {
   bool causal;
   __device__ __forceinline__ KeyLine(const Args& A, const Seq& s) {
     nq = s.nq; nk = s.nk; per = A.per; causal = A.causal;
-    tiles = (s.span + KEYS - 1) / KEYS;
+    tiles = ((int64_t)s.span + KEYS - 1) / KEYS;
     used = (nk + KEYS - 1) / KEYS;
     const int64_t shift = nk - nq;
     full = !causal ? used : shift < 0 ? 0 : min(used, shift / KEYS + 1);
@@ -441,10 +442,11 @@ __global__ __launch_bounds__(4 * keys_of(sizeof(elem_t<T>) == 2, DB), crowded<T>
       const int64_t t = at.t, lo = at.lo, full = line.before(t + 1) - line.before(t), hi = whole ? full : min(full, lo + b - a), item = at.item;
       a += hi - lo;
 
-      const int c0 = (int)t * KEYS, w0 = c0 + kb, key = w0 + (l & 31), shift = S.nk - S.nq;
-      const bool valid = key < S.nk;
+      const unsigned c0 = (unsigned)t * KEYS, w0 = c0 + kb, key = w0 + (l & 31), nk = S.nk;
+      const int64_t shift = (int64_t)S.nk - S.nq;
+      const bool valid = key < nk;
       // query i sees key j if j <= i + shift: rows from `first` on see some key of the item
-      const int first = A.causal ? min(max(c0 - shift, 0), S.nq) : 0;
+      const int first = A.causal ? (int)min(max((int64_t)c0 - shift, (int64_t)0), (int64_t)S.nq) : 0;
       const int left = (int)line.cut(t, hi);  // packed rows m0 .. left - 1, counted from query `first` on
       int m0 = (int)line.cut(t, lo);
       f32x16 dk[DB], dv[DB];
@@ -467,8 +469,8 @@ __global__ __launch_bounds__(4 * keys_of(sizeof(elem_t<T>) == 2, DB), crowded<T>
         sk.store(vt, threadIdx.x);
       }
       // the first packed row that sees this lane's key; the wave's first key, its last
-      auto first_for = [&](int k) { return A.causal ? (int)min(max(((int64_t)k - shift - first) * per, (int64_t)0), (int64_t)left) : 0; };
-      const int need = valid ? first_for(key) : left, need0 = first_for(w0), need1 = w0 + 32 > S.nk ? left : first_for(w0 + 31);
+      auto first_for = [&](unsigned k) { return A.causal ? (int)min(max(((int64_t)k - shift - first) * per, (int64_t)0), (int64_t)left) : 0; };
+      const int need = valid ? first_for(key) : left, need0 = first_for(w0), need1 = w0 + 32 > nk ? left : first_for(w0 + 31);
       // the step at hand starts at packed row m0: query q0 of the sequence, head s0 of the group
       int q0 = first + m0 / per, s0 = m0 % per;
       constexpr int U = (kQRows * L::CH + NT - 1) / NT;
@@ -518,7 +520,7 @@ __global__ __launch_bounds__(4 * keys_of(sizeof(elem_t<T>) == 2, DB), crowded<T>
         }
         if (m0 + kQRows < left) fetch(m0 + kQRows, q0, s0);
         // uniform in the wave: some row of the block sees some key of the wave
-        if (w0 < S.nk && m0 + qb < left && m0 + qb + 31 >= need0) {
+        if (w0 < nk && m0 + qb < left && m0 + qb + 31 >= need0) {
           f32x16 s, dp;
           if constexpr (COLS) {
             s = row_mul<T, DB, false, kQRows>(qt, qb, kf);
@@ -589,7 +591,7 @@ __global__ __launch_bounds__(4 * keys_of(sizeof(elem_t<T>) == 2, DB), crowded<T>
       }
       if (lo == 0 && hi == full) {  // rows of the sequence's span that are not in use get zeros
         const int64_t krow = (int64_t)S.k0 + key, to = krow * (second ? A.vs : A.ks) + (int64_t)g * A.d;
-        store_cols<E, DB>((E*)(second ? A.dv : A.dk) + to, key < S.span, A.d, dk, second ? 1.f : A.scale);
+        store_cols<E, DB>((E*)(second ? A.dv : A.dk) + to, key < (unsigned)S.span, A.d, dk, second ? 1.f : A.scale);
       } else if (w + item < A.slots) {
         float4* part = reinterpret_cast<float4*>(A.part) + ((w + item) * 2 * KB + wave) * DB * 4 * 64;
 #pragma unroll
@@ -656,9 +658,9 @@ __global__ __launch_bounds__(4 * keys_of(sizeof(T) == 2, DB)) void k_attn_dkv_jo
     }
   }
   const bool second = wave >= KB;
-  const int key = (int)t * KEYS + 32 * (wave & (KB - 1)) + (l & 31);
+  const unsigned key = (unsigned)t * KEYS + 32 * (wave & (KB - 1)) + (l & 31);
   const int64_t krow = (int64_t)S.k0 + key, at = krow * (second ? A.vs : A.ks) + (int64_t)g * A.d + 32 * db;
-  store_cols<T, 1>((T*)(second ? A.dv : A.dk) + at, key < S.span, A.d - 32 * db, sum, second ? 1.f : A.scale);
+  store_cols<T, 1>((T*)(second ? A.dv : A.dk) + at, key < (unsigned)S.span, A.d - 32 * db, sum, second ? 1.f : A.scale);
 }
 
 // How k_attn_dkv is launched.  Up to 512 packed rows (8 steps an item) a workgroup takes an item: a launch

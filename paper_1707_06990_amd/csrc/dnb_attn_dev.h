@@ -428,7 +428,8 @@ __device__ __forceinline__ void store_cols(T* row, bool valid, int d, const f32x
     }
 }
 
-// One sequence, as its offsets say; whatever they hold, the rows stay inside the tensors.
+// One sequence, as its offsets say; whatever they hold, the rows stay inside the tensors.  nk may be 2^31 - 1:
+// positions of keys, which go up to a tile further, are unsigned.
 struct Seq {
   int q0, nq, k0, nk, span;  // span: rows of k up to the next sequence's, of which nk are in use
 };
@@ -497,10 +498,11 @@ __device__ __forceinline__ bool find_tile(const Args& A, int64_t tile, F tiles_o
 // 32 packed rows of a wave, a lane's own being m0 + (lane & 31)
 struct RowTile {
   bool valid;
-  int head, sees, most, least;  // keys that the lane's row sees; that the wave's last row, its first row see
+  int head;
+  unsigned sees, most, least;  // keys that the lane's row sees; that the wave's last row, its first row see
   int64_t qrow;
-  static __device__ __forceinline__ int seen(const Args& A, const Seq& S, int m) {
-    return A.causal ? min(max(m / A.per + S.nk - S.nq + 1, 0), S.nk) : S.nk;
+  static __device__ __forceinline__ unsigned seen(const Args& A, const Seq& S, int m) {
+    return A.causal ? max(S.nk + min(m / A.per + 1 - S.nq, 0), 0) : S.nk;
   }
   __device__ __forceinline__ RowTile(const Args& A, const Seq& S, int g, int m0) {
     const int M = S.nq * A.per, m = m0 + (lane_id() & 31), row = m / A.per;
@@ -519,6 +521,7 @@ struct RowTile {
 // leaves its result in slot (wave + item): walking along the line, each next part has a next wave or a next
 // item.
 constexpr int kItemRows = 32, kUnit = 32;
+__device__ __forceinline__ int units_of(unsigned keys) { return (int)((keys + kUnit - 1) / kUnit); }
 
 // The rule: where tiles of 128 rows are so few that most of the chip would be idle, or mostly empty, and the
 // keys are long enough to be worth the second launch.  Lengths are on the device; the longest sequence is
@@ -534,7 +537,7 @@ struct Line {
 };
 __device__ __forceinline__ Line line_of(const Args& A, const Seq& s) {
   const int64_t items = ((int64_t)s.nq * A.per + kItemRows - 1) / kItemRows * A.kv;
-  return {items * ((s.nk + kUnit - 1) / kUnit), items};
+  return {items * units_of(s.nk), items};
 }
 __device__ __forceinline__ int64_t line_total(const Args& A) {
   int64_t u = 0;
@@ -570,7 +573,7 @@ __device__ __forceinline__ void each_part(const Args& A, int64_t w, F f) {
         const int at = __builtin_ctzll(past);
         S = bcast(mine, at);
         const int64_t in = a - u0 - bcast64(ue - ln.units, at);
-        const int len = (S.nk + kUnit - 1) / kUnit;
+        const int len = units_of(S.nk);
         j = in / len;
         first = (int)(in - j * len);
         last = (int)min((int64_t)len, first + b - a);
@@ -618,7 +621,7 @@ __device__ __forceinline__ RowParts row_parts(const Args& A, int64_t id) {
     u0 += bcast64(ue, 63);
     i0 += bcast64(ie, 63);
   }
-  const int len = (S.nk + kUnit - 1) / kUnit;
+  const int len = units_of(S.nk);
   if (!P.found || len == 0) return P;
   const int64_t total = u0, W = min((int64_t)A.waves, total);
   const int g = P.head / A.per, m = (int)(P.qrow - S.q0) * A.per + P.head - g * A.per;

@@ -1,4 +1,4 @@
-"""Sequence operators at the sizes where a launch has 2^24 workgroups and more."""
+"""Sequence operators at the sizes where a launch has 2^24 workgroups and more, and where key positions reach 2^31."""
 import math
 
 import pytest
@@ -86,4 +86,44 @@ def test_split_form_with_2_24_rows_of_heads(dnb):
         for got, w, t, name in zip((dq[mine][:, hs], dk[:used, g:g + 1], dv[:used, g:g + 1]), want, tol, ("dq", "dk", "dv")):
             assert_within(got, w, t, f"{name} of group {g}")
     assert bool(torch.isnan(dk[used:].float()).all()) and bool(torch.isnan(dv[used:].float()).all())   # rows of no sequence
+    dnb.dnb_attn_destroy(plan)
+
+
+def test_key_positions_up_to_2_31(dnb):
+    """One query over 2^31 - 1 keys, all zero but the last two: one takes the weight, one is as the others."""
+    nk, dim = 2 ** 31 - 1, 8
+    room(165)
+    k, v, dk, dv = (torch.zeros((nk, 1, dim), dtype=torch.bfloat16, device="cuda") for _ in range(4))
+    q = torch.full((1, 1, dim), 2.0, dtype=torch.bfloat16, device="cuda")
+    k[-2] = 8.0                                  # score 2 * 8 * 8 / sqrt(8) = 45.25
+    v[-2] = torch.arange(dim).to(torch.bfloat16).cuda()
+    v[-1] = 2.0 ** 60                            # weight 2.2e-20: adds 0.0255 to every value
+    score = 128 / math.sqrt(8)
+    plan = dnb.dnb_attn_create(1, 1, dim, 1, 1, nk, causal=True)
+    ws = torch.empty(dnb.dnb_attn_workspace_bytes(plan), dtype=torch.uint8, device="cuda")
+    out, lse = torch.full_like(q, float("nan")), torch.full((1, 1), float("nan"), device="cuda")
+    off, ends = ints([0, 1]), ints([0, nk])
+    dnb.dnb_attn_forward(plan, q, k, v, off, ends, None, out, lse, ws)
+    torch.cuda.synchronize()
+    r, f = half_step(torch.bfloat16), 2.0 ** -24
+    want_lse = score + math.log1p((nk - 1) * math.exp(-score))
+    # the score's products are exact, the scaled score is rounded some times: e, which a weight takes over
+    e = f * (8 * score + 16)
+    assert abs(float(lse) - want_lse) <= e
+    small = math.exp(-want_lse)
+    want = torch.arange(dim, dtype=torch.float64) * math.exp(score - want_lse) + small * 2.0 ** 60
+    assert_within(out[0, 0], want, (2 * r + 2 * e) * want, "out")
+    dout = torch.ones_like(q)
+    dnb.dnb_attn_backward(plan, q, k, v, out, lse, dout, off, ends, None, q.clone(), dk, dv, ws)
+    torch.cuda.synchronize()
+    # dv: the weight of each key, once rounded to bf16 for its product and once at the end
+    assert bool((dv[:-2] == dv[0]).all()) and bool((dv[-1] == dv[0]).all())
+    assert abs(float(dv[0, 0, 0]) - small) <= (2 * r + 2 * e) * small and abs(float(dv[-2, 0, 0]) - 1) <= 2 * r + 2 * e
+    # dk of a key of value 0: weight times (0 - sum dout out) times the query, over sqrt(8); sum dout out as out gives it
+    D = float(out.double().sum())
+    one = -small * D * 2 / math.sqrt(8)
+    assert bool((dk[:-2] == dk[0]).all())
+    assert abs(float(dk[0, 0, 0]) - one) <= (2 * r + 2 * e + 16 * f) * abs(one)
+    last = small * (8 * 2.0 ** 60 - D) * 2 / math.sqrt(8)
+    assert abs(float(dk[-1, 0, 0]) - last) <= (2 * r + 2 * e + 32 * f) * abs(last)
     dnb.dnb_attn_destroy(plan)
