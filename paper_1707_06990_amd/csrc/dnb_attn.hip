@@ -109,56 +109,70 @@ __global__ __launch_bounds__(kThreads * KH, 2) void k_attn(Args A) {
   const unsigned sees = R0.sees, most = R0.most, least = R0.least;
   const int64_t qrow = R0.qrow;
 
-  Columns<T, DB> qf;
-  load_cols<T, DB>(qf, (const E*)A.q + qrow * A.qs + (int64_t)head * A.d, valid, A.d);
   Online<DB> R;
-  R.init();
-  const E* kb = (const E*)A.k + (int64_t)S.k0 * A.ks + (int64_t)g * A.d;
-  const E* vb = (const E*)A.v + (int64_t)S.k0 * A.vs + (int64_t)g * A.d;
-  Stage<T, DB, STEP, NT> sk, sv;
-  sk.init(threadIdx.x, A.ks, A.d);
-  sv.init(threadIdx.x, A.vs, A.d);
-  auto fetch = [&](unsigned k0) {
-    sk.load(kb + (int64_t)k0 * A.ks, A.ks, S.nk - k0, A.d);
-    sv.load(vb + (int64_t)k0 * A.vs, A.vs, S.nk - k0, A.d);
-  };
-  auto put = [&](int buf) {
-    sk.store(lds + buf * 2 * KH * L::BYTES, threadIdx.x);
-    sv.store(lds + (buf * 2 + 1) * KH * L::BYTES, threadIdx.x);
-  };
-  if (all > 0) {
-    fetch(0);
-    put(0);
-  }
-  __syncthreads();
-  auto step = [&](unsigned at, auto which) {
-    constexpr int BUF = which;
-    const unsigned k0 = at + kh * KT;
-    if (k0 >= most && at + STEP < all) fetch(at + STEP);
-    if (k0 < most) {
-      const lds_t kt = lds + (BUFS == 1 ? 0 : BUF * 2 * KH * L::BYTES) + kh * KT * L::PITCH;
-      f32x16 s[NB];
-#pragma unroll
-      for (int b = 0; b < NB; ++b) s[b] = row_mul<T, DB, HOLD, STEP>(kt, 32 * b, qf);
-      // four reads of LDS ahead of their products, and the next tile's registers not taken before: 381 -> 367 us
-      // for 12597 packed queries of 32 heads
-      if constexpr (L::PL == 1) read_ahead<KH == 1 ? 4 : 2, NB * L::NS>();
-      if (at + STEP < all) fetch(at + STEP);
-      if (k0 + KT > least) {
-#pragma unroll
-        for (int b = 0; b < NB; ++b) hide(s[b], k0 + 32 * b, sees);
-      }
-      online_step<T, DB, NB, HOLD, STEP>(R, s, A.c, kt + KH * L::BYTES, 0);
-    }
-    if (at + STEP < all) {
-      if (BUFS == 1) __syncthreads();
-      put(BUFS == 1 ? 0 : BUF ^ 1);
+  auto walk = [&](auto form) {
+    using F = decltype(form);
+    const int tid = apart<F>((int)threadIdx.x);
+    Columns<F, DB> qf;
+    load_cols<F, DB>(qf, (const E*)A.q + apart<F>(qrow) * A.qs + (int64_t)apart<F>(head) * A.d, valid, A.d);
+    R.init();
+    const E* kb = (const E*)A.k + (int64_t)S.k0 * A.ks + (int64_t)g * A.d;
+    const E* vb = (const E*)A.v + (int64_t)S.k0 * A.vs + (int64_t)g * A.d;
+    Stage<F, DB, STEP, NT> sk, sv;
+    sk.init(tid, A.ks, A.d);
+    sv.init(tid, A.vs, A.d);
+    auto fetch = [&](unsigned k0) {
+      sk.load(kb + (int64_t)k0 * A.ks, A.ks, S.nk - k0, A.d);
+      sv.load(vb + (int64_t)k0 * A.vs, A.vs, S.nk - k0, A.d);
+    };
+    auto put = [&](int buf) {
+      sk.store(lds + buf * 2 * KH * L::BYTES, tid);
+      sv.store(lds + (buf * 2 + 1) * KH * L::BYTES, tid);
+    };
+    if (!is_whole<F> && all > 0) {
+      fetch(0);
+      put(0);
     }
     __syncthreads();
+    auto step = [&](unsigned at, auto which) {
+      constexpr int BUF = which;
+      const unsigned k0 = at + kh * KT;
+      const bool ahead = !is_whole<F> && at + STEP < all;  // Whole holds no tile over its products
+      if (is_whole<F>) {
+        fetch(at);
+        put(BUFS == 1 ? 0 : BUF);
+        __syncthreads();
+      }
+      if (k0 >= most && ahead) fetch(at + STEP);
+      if (k0 < most) {
+        const lds_t kt = lds + (BUFS == 1 ? 0 : BUF * 2 * KH * L::BYTES) + kh * KT * L::PITCH;
+        f32x16 s[NB];
+#pragma unroll
+        for (int b = 0; b < NB; ++b) s[b] = row_mul<F, DB, HOLD, STEP>(kt, 32 * b, qf);
+        // four reads of LDS ahead of their products, and the next tile's registers not taken before: 381 -> 367 us
+        // for 12597 packed queries of 32 heads
+        if constexpr (L::PL == 1) read_ahead<KH == 1 ? 4 : 2, NB * L::NS>();
+        if (ahead) fetch(at + STEP);
+        if (k0 + KT > least) {
+#pragma unroll
+          for (int b = 0; b < NB; ++b) hide(s[b], k0 + 32 * b, sees);
+        }
+        online_step<F, DB, NB, HOLD, STEP>(R, s, A.c, kt + KH * L::BYTES, 0);
+      }
+      if (ahead) {
+        if (BUFS == 1) __syncthreads();
+        put(BUFS == 1 ? 0 : BUF ^ 1);
+      }
+      __syncthreads();
+    };
+    for (unsigned at = 0; at < all; at += 2 * STEP) {
+      step(at, std::integral_constant<int, 0>());
+      if (at + STEP < all) step(at + STEP, std::integral_constant<int, 1>());
+    }
   };
-  for (unsigned at = 0; at < all; at += 2 * STEP) {
-    step(at, std::integral_constant<int, 0>());
-    if (at + STEP < all) step(at + STEP, std::integral_constant<int, 1>());
+  walk(T());
+  if constexpr (L::PL == 3) {  // (the last step ended with a barrier)
+    if (any_wave<4 * KH>(lds + BUFS * 2 * KH * L::BYTES, not_finite(R.o))) walk(Whole());
   }
   if constexpr (KH == 2) {
     // the second half's O in 16-byte pieces, then its m and l; the last step ended with a barrier
@@ -301,12 +315,12 @@ hipError_t run_forward(const Args& A, bool token, hipStream_t st) {
     return hipGetLastError();
   }
   using M = typename std::conditional<std::is_same<T, float>::value, Split, T>::type;
-  constexpr int BYTES = Tile<M, DB>::BYTES;
+  constexpr int BYTES = Tile<M, DB>::BYTES, FLAGS = in_parts<M> ? kFlags : 0;
   const int64_t tiles = (A.rq * A.per + kRows - 1) / kRows + A.n;
   if (split_keys(A, tiles))
-    hipLaunchKernelGGL((k_attn<M, DB, 2>), flat_grid(tiles * A.kv), dim3(2 * kThreads), 4 * buffers<M>(DB) * BYTES, st, A);
+    hipLaunchKernelGGL((k_attn<M, DB, 2>), flat_grid(tiles * A.kv), dim3(2 * kThreads), 4 * buffers<M>(DB) * BYTES + FLAGS, st, A);
   else
-    hipLaunchKernelGGL((k_attn<M, DB, 1>), flat_grid(tiles * A.kv), dim3(kThreads), 2 * buffers<M>(DB) * BYTES, st, A);
+    hipLaunchKernelGGL((k_attn<M, DB, 1>), flat_grid(tiles * A.kv), dim3(kThreads), 2 * buffers<M>(DB) * BYTES + FLAGS, st, A);
   return hipGetLastError();
 }
 

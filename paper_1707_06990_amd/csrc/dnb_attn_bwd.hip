@@ -31,7 +31,7 @@ constexpr int kFineKeys = 128;
 
 // Two rows of registers for q and dout: above head_dim 64 Split takes those of two waves.
 template <typename T>
-constexpr bool crowded(int blocks) { return std::is_same<T, Split>::value && blocks > 2; }
+constexpr bool crowded(int blocks) { return in_parts<T> && blocks > 2; }
 
 // KH 2: eight waves, of which the second four take the second of every two tiles of keys (see k_attn).
 template <typename T, int DB, int KH>
@@ -56,97 +56,112 @@ __global__ __launch_bounds__(kThreads * KH, crowded<T>(DB) ? 1 : 2) void k_attn_
   const unsigned sees = R0.sees, most = R0.most, least = R0.least;
   const int64_t qrow = R0.qrow;
 
-  Columns<T, DB> qf, df;
-  load_cols<T, DB>(qf, (const E*)A.q + qrow * A.qs + (int64_t)head * A.d, valid, A.d);
-  load_cols<T, DB>(df, (const E*)A.dout + qrow * A.os + (int64_t)head * A.d, valid, A.d);
-  float D = dot_rows<T, DB>((const E*)A.out + qrow * A.os + (int64_t)head * A.d, (const E*)A.dout + qrow * A.os + (int64_t)head * A.d, valid, A.d);
-  // lse = -inf: the row sees no key, and none of its p may be anything but 0
-  float lse2 = INFINITY;
-  if (valid) {
-    const float v = A.lse[(int64_t)head * A.rq + qrow];
-    if (v != -INFINITY) lse2 = v * kLog2e;
-  }
-  const bool fine = sizeof(E) == 2 && most <= kFineKeys;
   f32x16 acc[DB];
+  auto walk = [&](auto form) {
+    using F = decltype(form);
+    const int tid = apart<F>((int)threadIdx.x), h = apart<F>(head);
+    const int64_t at = apart<F>(qrow) * A.os + (int64_t)h * A.d;
+    Columns<F, DB> qf, df;
+    load_cols<F, DB>(qf, (const E*)A.q + apart<F>(qrow) * A.qs + (int64_t)h * A.d, valid, A.d);
+    load_cols<F, DB>(df, (const E*)A.dout + at, valid, A.d);
+    float D = dot_rows<T, DB>((const E*)A.out + at, (const E*)A.dout + at, valid, A.d);
+    // lse = -inf: the row sees no key, and none of its p may be anything but 0
+    float lse2 = INFINITY;
+    if (valid) {
+      const float v = A.lse[(int64_t)h * A.rq + apart<F>(qrow)];
+      if (v != -INFINITY) lse2 = v * kLog2e;
+    }
+    const bool fine = sizeof(E) == 2 && most <= kFineKeys;
 #pragma unroll
-  for (int i = 0; i < DB; ++i) acc[i] = (f32x16){};
-  const E* kb = (const E*)A.k + (int64_t)S.k0 * A.ks + (int64_t)g * A.d;
-  const E* vb = (const E*)A.v + (int64_t)S.k0 * A.vs + (int64_t)g * A.d;
-  Stage<T, DB, STEP, NT> sk, sv;
-  sk.init(threadIdx.x, A.ks, A.d);
-  sv.init(threadIdx.x, A.vs, A.d);
-  auto fetch = [&](unsigned k0) {
-    sk.load(kb + (int64_t)k0 * A.ks, A.ks, S.nk - k0, A.d);
-    sv.load(vb + (int64_t)k0 * A.vs, A.vs, S.nk - k0, A.d);
-  };
-  auto put = [&](int buf) {
-    sk.store(lds + buf * 2 * KH * L::BYTES, threadIdx.x);
-    sv.store(lds + (buf * 2 + 1) * KH * L::BYTES, threadIdx.x);
-  };
-  if (sizeof(E) == 2 && all <= kFineKeys) {  // uniform in the workgroup: D from p and dout v^T
-    float d = 0.f;
-    for (unsigned at = 0; at < all; at += STEP) {
-      fetch(at);
-      put(0);
-      __syncthreads();
-      const unsigned k0 = at + kh * KT;
-      const lds_t kt = lds + kh * KT * L::PITCH;
+    for (int i = 0; i < DB; ++i) acc[i] = (f32x16){};
+    const E* kb = (const E*)A.k + (int64_t)S.k0 * A.ks + (int64_t)g * A.d;
+    const E* vb = (const E*)A.v + (int64_t)S.k0 * A.vs + (int64_t)g * A.d;
+    Stage<F, DB, STEP, NT> sk, sv;
+    sk.init(tid, A.ks, A.d);
+    sv.init(tid, A.vs, A.d);
+    auto fetch = [&](unsigned k0) {
+      sk.load(kb + (int64_t)k0 * A.ks, A.ks, S.nk - k0, A.d);
+      sv.load(vb + (int64_t)k0 * A.vs, A.vs, S.nk - k0, A.d);
+    };
+    auto put = [&](int buf) {
+      sk.store(lds + buf * 2 * KH * L::BYTES, tid);
+      sv.store(lds + (buf * 2 + 1) * KH * L::BYTES, tid);
+    };
+    if (sizeof(E) == 2 && all <= kFineKeys) {  // uniform in the workgroup: D from p and dout v^T
+      float d = 0.f;
+      for (unsigned at = 0; at < all; at += STEP) {
+        fetch(at);
+        put(0);
+        __syncthreads();
+        const unsigned k0 = at + kh * KT;
+        const lds_t kt = lds + kh * KT * L::PITCH;
 #pragma unroll 1
-      for (int b = 0; b < NB && k0 < most; ++b) {
-        const f32x16 s = row_mul<T, DB, false, STEP>(kt, 32 * b, qf);
-        const f32x16 dp = row_mul<T, DB, false, STEP>(kt + KH * L::BYTES, 32 * b, df);
+        for (int b = 0; b < NB && k0 < most; ++b) {
+          const f32x16 s = row_mul<F, DB, false, STEP>(kt, 32 * b, qf);
+          const f32x16 dp = row_mul<F, DB, false, STEP>(kt + KH * L::BYTES, 32 * b, df);
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          d += k0 + 32 * b + row_of(i) >= sees ? 0.f : __builtin_amdgcn_exp2f(fmaf(s[i], A.c, -lse2)) * dp[i];
+          for (int i = 0; i < 16; ++i)
+            d += k0 + 32 * b + row_of(i) >= sees ? 0.f : __builtin_amdgcn_exp2f(fmaf(s[i], A.c, -lse2)) * dp[i];
+        }
+        __syncthreads();
       }
-      __syncthreads();
-    }
-    D = half_sum(d);
-    if constexpr (KH == 2) {  // the other half of the waves has the other tiles
-      lds_write(lds + 4 * threadIdx.x, D);
-      __syncthreads();
-      D += lds_read<float>(lds + 4 * (threadIdx.x ^ 256));
-      __syncthreads();
-    }
-  }
-  if (valid && l < 32 && kh == 0) A.rowdot[(int64_t)head * A.rq + qrow] = D;
-  if (all > 0) {
-    fetch(0);
-    put(0);
-  }
-  __syncthreads();
-  auto step = [&](unsigned at, auto which) {
-    constexpr int BUF = which;
-    const unsigned k0 = at + kh * KT;
-    if (k0 >= most && at + STEP < all) fetch(at + STEP);
-    if (k0 < most) {
-      const lds_t kt = lds + BUF * 2 * KH * L::BYTES + kh * KT * L::PITCH;
-#pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        f32x16 s = row_mul<T, DB, HOLD, STEP>(kt, 32 * b, qf);
-        const f32x16 dp = row_mul<T, DB, HOLD, STEP>(kt + KH * L::BYTES, 32 * b, df);
-        if constexpr (L::PL == 1) read_ahead<4, 2 * L::NS>();  // (as in k_attn)
-        if (b == 0 && at + STEP < all) fetch(at + STEP);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], A.c, -lse2)) * (dp[i] - D);
-        if (k0 + 32 * b + 32 > least) {
-#pragma unroll
-          for (int i = 0; i < 16; ++i) s[i] = k0 + 32 * b + row_of(i) >= sees ? 0.f : s[i];
-        }
-        col_mul<T, DB, HOLD, STEP>(kt, 32 * b, s, acc);
-        if (fine) {
-#pragma unroll
-          for (int i = 0; i < 16; ++i) s[i] -= (float)(__bf16)s[i];
-          col_mul<T, DB, HOLD, STEP>(kt, 32 * b, s, acc);
-        }
+      D = half_sum(d);
+      if constexpr (KH == 2) {  // the other half of the waves has the other tiles
+        lds_write(lds + 4 * threadIdx.x, D);
+        __syncthreads();
+        D += lds_read<float>(lds + 4 * (threadIdx.x ^ 256));
+        __syncthreads();
       }
     }
-    if (at + STEP < all) put(BUF ^ 1);
+    if (valid && l < 32 && kh == 0) A.rowdot[(int64_t)h * A.rq + apart<F>(qrow)] = D;
+    if (!is_whole<F> && all > 0) {
+      fetch(0);
+      put(0);
+    }
     __syncthreads();
+    auto step = [&](unsigned at, auto which) {
+      constexpr int BUF = which;
+      const unsigned k0 = at + kh * KT;
+      const bool ahead = !is_whole<F> && at + STEP < all;  // (as in k_attn)
+      if (is_whole<F>) {
+        fetch(at);
+        put(BUF);
+        __syncthreads();
+      }
+      if (k0 >= most && ahead) fetch(at + STEP);
+      if (k0 < most) {
+        const lds_t kt = lds + BUF * 2 * KH * L::BYTES + kh * KT * L::PITCH;
+#pragma unroll
+        for (int b = 0; b < NB; ++b) {
+          f32x16 s = row_mul<F, DB, HOLD, STEP>(kt, 32 * b, qf);
+          const f32x16 dp = row_mul<F, DB, HOLD, STEP>(kt + KH * L::BYTES, 32 * b, df);
+          if constexpr (L::PL == 1) read_ahead<4, 2 * L::NS>();  // (as in k_attn)
+          if (b == 0 && ahead) fetch(at + STEP);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) s[i] = __builtin_amdgcn_exp2f(fmaf(s[i], A.c, -lse2)) * (dp[i] - D);
+          if (k0 + 32 * b + 32 > least) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] = k0 + 32 * b + row_of(i) >= sees ? 0.f : s[i];
+          }
+          col_mul<F, DB, HOLD, STEP>(kt, 32 * b, s, acc);
+          if (fine) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) s[i] -= (float)(__bf16)s[i];
+            col_mul<F, DB, HOLD, STEP>(kt, 32 * b, s, acc);
+          }
+        }
+      }
+      if (ahead) put(BUF ^ 1);
+      __syncthreads();
+    };
+    for (unsigned at = 0; at < all; at += 2 * STEP) {
+      step(at, std::integral_constant<int, 0>());
+      if (at + STEP < all) step(at + STEP, std::integral_constant<int, 1>());
+    }
   };
-  for (unsigned at = 0; at < all; at += 2 * STEP) {
-    step(at, std::integral_constant<int, 0>());
-    if (at + STEP < all) step(at + STEP, std::integral_constant<int, 1>());
+  walk(T());
+  if constexpr (L::PL == 3) {  // (the last step ended with a barrier)
+    if (any_wave<4 * KH>(lds + 4 * KH * L::BYTES, not_finite(acc))) walk(Whole());
   }
   if constexpr (KH == 2) {
     f32x4* to = reinterpret_cast<f32x4*>(shared) + wave * DB * 4 * 64 + l;
@@ -447,115 +462,126 @@ __global__ __launch_bounds__(4 * keys_of(sizeof(elem_t<T>) == 2, DB), crowded<T>
       const bool valid = key < nk;
       // query i sees key j if j <= i + shift: rows from `first` on see some key of the item
       const int first = A.causal ? (int)min(max((int64_t)c0 - shift, (int64_t)0), (int64_t)S.nq) : 0;
+      // the last query that sees no more than kFineKeys keys
+      const int fine_to = A.causal ? (int)min(max(kFineKeys - 1 - shift, (int64_t)-1), (int64_t)INT32_MAX) : S.nk <= kFineKeys ? INT32_MAX : -1;
       const int left = (int)line.cut(t, hi);  // packed rows m0 .. left - 1, counted from query `first` on
-      int m0 = (int)line.cut(t, lo);
       f32x16 dk[DB], dv[DB];
+      auto walk = [&](auto form) {
+        using F = decltype(form);
+        const int tid = apart<F>((int)threadIdx.x);
+        int m0 = (int)line.cut(t, lo);
 #pragma unroll
-      for (int i = 0; i < DB; ++i) dk[i] = dv[i] = (f32x16){};
-
-      __syncthreads();  // the item before is done with LDS
-      Columns<T, DB> kf, vf;
-      if (COLS) {
-        const int64_t krow = (int64_t)S.k0 + key;
-        load_cols<T, DB>(kf, (const E*)A.k + krow * A.ks + (int64_t)g * A.d, valid && m0 < left, A.d);
-        load_cols<T, DB>(vf, (const E*)A.v + krow * A.vs + (int64_t)g * A.d, valid && m0 < left, A.d);
-      } else if (m0 < left) {  // uniform in the workgroup
-        Stage<T, DB, KEYS, NT> sk;
-        sk.init(threadIdx.x, A.ks, A.d);
-        sk.load((const E*)A.k + ((int64_t)S.k0 + c0) * A.ks + (int64_t)g * A.d, A.ks, S.nk - c0, A.d);
-        sk.store(kt, threadIdx.x);
-        sk.init(threadIdx.x, A.vs, A.d);
-        sk.load((const E*)A.v + ((int64_t)S.k0 + c0) * A.vs + (int64_t)g * A.d, A.vs, S.nk - c0, A.d);
-        sk.store(vt, threadIdx.x);
-      }
-      // the first packed row that sees this lane's key; the wave's first key, its last
-      auto first_for = [&](unsigned k) { return A.causal ? (int)min(max(((int64_t)k - shift - first) * per, (int64_t)0), (int64_t)left) : 0; };
-      const int need = valid ? first_for(key) : left, need0 = first_for(w0), need1 = w0 + 32 > nk ? left : first_for(w0 + 31);
-      // the step at hand starts at packed row m0: query q0 of the sequence, head s0 of the group
-      int q0 = first + m0 / per, s0 = m0 % per;
-      constexpr int U = (kQRows * L::CH + NT - 1) / NT;
-      u32x4 rq[U * L::LD], rd[U * L::LD];
-      float st = 0.f;  // threads 0 .. 63: lse of a row, 64 .. 127: D
-      auto fetch = [&](int m, int q, int s) {
-        const auto qr = __builtin_amdgcn_make_buffer_rsrc((E*)A.q + ((int64_t)S.q0 + q) * A.qs + (int64_t)g * per * A.d, 0, 0x7fffffff, 0x00027000);
-        const auto dr = __builtin_amdgcn_make_buffer_rsrc((E*)A.dout + ((int64_t)S.q0 + q) * A.os + (int64_t)g * per * A.d, 0, 0x7fffffff, 0x00027000);
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-          const int i = threadIdx.x + u * NT, row = i / L::CH, c = i - row * L::CH;
-          const int x = over(s + row), e = (s + row - x * per) * A.d + c * L::EP;
-          const bool ok = row < kQRows && m + row < left && c * L::EP < A.d;
-          const uint32_t oq = ok ? (uint32_t)(x * (int)A.qs + e) * (uint32_t)sizeof(E) : 0x80000000u;
-          const uint32_t od = ok ? (uint32_t)(x * (int)A.os + e) * (uint32_t)sizeof(E) : 0x80000000u;
-#pragma unroll
-          for (int p = 0; p < L::LD; ++p) {
-            rq[u * L::LD + p] = __builtin_amdgcn_raw_buffer_load_b128(qr, oq + 16 * p, 0, 0);
-            rd[u * L::LD + p] = __builtin_amdgcn_raw_buffer_load_b128(dr, od + 16 * p, 0, 0);
-          }
+        for (int i = 0; i < DB; ++i) dk[i] = dv[i] = (f32x16){};
+        __syncthreads();  // the item, or the walk, before is done with LDS
+        Columns<F, DB> kf, vf;
+        if (COLS) {
+          const int64_t krow = (int64_t)S.k0 + key;
+          load_cols<F, DB>(kf, (const E*)A.k + krow * A.ks + (int64_t)g * A.d, valid && m0 < left, A.d);
+          load_cols<F, DB>(vf, (const E*)A.v + krow * A.vs + (int64_t)g * A.d, valid && m0 < left, A.d);
+        } else if (m0 < left) {  // uniform in the workgroup
+          Stage<F, DB, KEYS, NT> sk;
+          sk.init(tid, A.ks, A.d);
+          sk.load((const E*)A.k + ((int64_t)S.k0 + c0) * A.ks + (int64_t)g * A.d, A.ks, S.nk - c0, A.d);
+          sk.store(kt, tid);
+          sk.init(tid, A.vs, A.d);
+          sk.load((const E*)A.v + ((int64_t)S.k0 + c0) * A.vs + (int64_t)g * A.d, A.vs, S.nk - c0, A.d);
+          sk.store(vt, tid);
         }
-        if ((int)threadIdx.x < 2 * kQRows) {
-          const int r = threadIdx.x & (kQRows - 1), x = over(s + r);
-          const bool is_lse = (int)threadIdx.x < kQRows;
-          st = is_lse ? INFINITY : 0.f;
-          if (m + r < left) {
-            const float v = (is_lse ? A.lse : A.rowdot)[(int64_t)(g * per + s + r - x * per) * A.rq + S.q0 + q + x];
-            if (!is_lse) st = v;
-            else if (v != -INFINITY) st = v * kLog2e;
+        // the first packed row that sees this lane's key; the wave's first key, its last
+        auto first_for = [&](unsigned k) { return A.causal ? (int)min(max(((int64_t)k - shift - first) * per, (int64_t)0), (int64_t)left) : 0; };
+        const int need = valid ? first_for(key) : left, need0 = first_for(w0), need1 = w0 + 32 > nk ? left : first_for(w0 + 31);
+        // the step at hand starts at packed row m0: query q0 of the sequence, head s0 of the group
+        int q0 = first + m0 / per, s0 = m0 % per;
+        constexpr int U = (kQRows * L::CH + NT - 1) / NT;
+        u32x4 rq[U * L::LD], rd[U * L::LD];
+        float st = 0.f;  // threads 0 .. 63: lse of a row, 64 .. 127: D
+        auto fetch = [&](int m, int q, int s) {
+          const auto qr = __builtin_amdgcn_make_buffer_rsrc((E*)A.q + ((int64_t)S.q0 + q) * A.qs + (int64_t)g * per * A.d, 0, 0x7fffffff, 0x00027000);
+          const auto dr = __builtin_amdgcn_make_buffer_rsrc((E*)A.dout + ((int64_t)S.q0 + q) * A.os + (int64_t)g * per * A.d, 0, 0x7fffffff, 0x00027000);
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            const int i = tid + u * NT, row = i / L::CH, c = i - row * L::CH;
+            const int x = over(s + row), e = (s + row - x * per) * A.d + c * L::EP;
+            const bool ok = row < kQRows && m + row < left && c * L::EP < A.d;
+            const uint32_t oq = ok ? (uint32_t)(x * (int)A.qs + e) * (uint32_t)sizeof(E) : 0x80000000u;
+            const uint32_t od = ok ? (uint32_t)(x * (int)A.os + e) * (uint32_t)sizeof(E) : 0x80000000u;
+#pragma unroll
+            for (int p = 0; p < L::LD; ++p) {
+              rq[u * L::LD + p] = __builtin_amdgcn_raw_buffer_load_b128(qr, oq + 16 * p, 0, 0);
+              rd[u * L::LD + p] = __builtin_amdgcn_raw_buffer_load_b128(dr, od + 16 * p, 0, 0);
+            }
+          }
+          if (tid < 2 * kQRows) {
+            const int r = tid & (kQRows - 1), x = over(s + r);
+            const bool is_lse = tid < kQRows;
+            st = is_lse ? INFINITY : 0.f;
+            if (m + r < left) {
+              const float v = (is_lse ? A.lse : A.rowdot)[(int64_t)(g * per + s + r - x * per) * A.rq + S.q0 + q + x];
+              if (!is_lse) st = v;
+              else if (v != -INFINITY) st = v * kLog2e;
+            }
+          }
+        };
+        if (!is_whole<F> && m0 < left) fetch(m0, q0, s0);
+        for (; m0 < left; m0 += kQRows) {
+          if (is_whole<F>) fetch(m0, q0, s0);
+          __syncthreads();  // the step before is done with the tiles
+          store_pieces<F, DB, U, NT, kQRows>(qt, tid, rq);
+          store_pieces<F, DB, U, NT, kQRows>(dt, tid, rd);
+          if (tid < 2 * kQRows) lds_write(rows + 4 * tid, st);
+          __syncthreads();
+          // of this wave's rows of the step, the last
+          const bool fine = BF && q0 + over(s0 + qb + 31) <= fine_to;
+          s0 += kQRows % per;
+          q0 += kQRows / per;
+          if (s0 >= per) {
+            s0 -= per;
+            ++q0;
+          }
+          if (!is_whole<F> && m0 + kQRows < left) fetch(m0 + kQRows, q0, s0);
+          // uniform in the wave: some row of the block sees some key of the wave
+          if (w0 < nk && m0 + qb < left && m0 + qb + 31 >= need0) {
+            f32x16 s, dp;
+            if constexpr (COLS) {
+              s = row_mul<F, DB, false, kQRows>(qt, qb, kf);
+              dp = row_mul<F, DB, false, kQRows>(dt, qb, vf);
+            } else {
+              s = row_mul_lds<F, DB, kQRows, KEYS>(qt, qb, kt, kb);
+              dp = row_mul_lds<F, DB, kQRows, KEYS>(dt, qb, vt, kb);
+            }
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              const f32x4 le = lds_read<f32x4>(rows + 4 * (qb + 8 * q + 4 * (l >> 5)));
+              const f32x4 Dd = lds_read<f32x4>(rows + 4 * (kQRows + qb + 8 * q + 4 * (l >> 5)));
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                const float p = __builtin_amdgcn_exp2f(fmaf(s[4 * q + j], A.c, -le[j]));
+                s[4 * q + j] = p;
+                dp[4 * q + j] = p * (dp[4 * q + j] - Dd[j]);
+              }
+            }
+            if (m0 + qb < need1) {
+#pragma unroll
+              for (int i = 0; i < 16; ++i) {
+                const bool sees = m0 + qb + row_of(i) >= need;
+                s[i] = sees ? s[i] : 0.f;
+                dp[i] = sees ? dp[i] : 0.f;
+              }
+            }
+            col_mul<F, DB, false, kQRows>(dt, qb, s, dv);
+            col_mul<F, DB, false, kQRows>(qt, qb, dp, dk);
+            if (fine) {
+#pragma unroll
+              for (int i = 0; i < 16; ++i) dp[i] -= (float)(__bf16)dp[i];
+              col_mul<F, DB, false, kQRows>(qt, qb, dp, dk);
+            }
           }
         }
       };
-      if (m0 < left) fetch(m0, q0, s0);
-      for (; m0 < left; m0 += kQRows) {
-        __syncthreads();  // the step before is done with the tiles
-        store_pieces<T, DB, U, NT, kQRows>(qt, threadIdx.x, rq);
-        store_pieces<T, DB, U, NT, kQRows>(dt, threadIdx.x, rd);
-        if ((int)threadIdx.x < 2 * kQRows) lds_write(rows + 4 * threadIdx.x, st);
-        __syncthreads();
-        // of this wave's rows of the step, the last
-        const bool fine = BF && (A.causal ? q0 + over(s0 + qb + 31) + shift + 1 : S.nk) <= kFineKeys;
-        s0 += kQRows % per;
-        q0 += kQRows / per;
-        if (s0 >= per) {
-          s0 -= per;
-          ++q0;
-        }
-        if (m0 + kQRows < left) fetch(m0 + kQRows, q0, s0);
-        // uniform in the wave: some row of the block sees some key of the wave
-        if (w0 < nk && m0 + qb < left && m0 + qb + 31 >= need0) {
-          f32x16 s, dp;
-          if constexpr (COLS) {
-            s = row_mul<T, DB, false, kQRows>(qt, qb, kf);
-            dp = row_mul<T, DB, false, kQRows>(dt, qb, vf);
-          } else {
-            s = row_mul_lds<T, DB, kQRows, KEYS>(qt, qb, kt, kb);
-            dp = row_mul_lds<T, DB, kQRows, KEYS>(dt, qb, vt, kb);
-          }
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const f32x4 le = lds_read<f32x4>(rows + 4 * (qb + 8 * q + 4 * (l >> 5)));
-            const f32x4 Dd = lds_read<f32x4>(rows + 4 * (kQRows + qb + 8 * q + 4 * (l >> 5)));
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const float p = __builtin_amdgcn_exp2f(fmaf(s[4 * q + j], A.c, -le[j]));
-              s[4 * q + j] = p;
-              dp[4 * q + j] = p * (dp[4 * q + j] - Dd[j]);
-            }
-          }
-          if (m0 + qb < need1) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-              const bool sees = m0 + qb + row_of(i) >= need;
-              s[i] = sees ? s[i] : 0.f;
-              dp[i] = sees ? dp[i] : 0.f;
-            }
-          }
-          col_mul<T, DB, false, kQRows>(dt, qb, s, dv);
-          col_mul<T, DB, false, kQRows>(qt, qb, dp, dk);
-          if (fine) {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) dp[i] -= (float)(__bf16)dp[i];
-            col_mul<T, DB, false, kQRows>(qt, qb, dp, dk);
-          }
-        }
+      walk(T());
+      if constexpr (L::PL == 3) {
+        const bool odd_k = not_finite(dk), odd_v = not_finite(dv);
+        if (any_wave<2 * KB>(rows + 2 * kQRows * 4, odd_k || odd_v)) walk(Whole());
       }
       // The first half of the waves finishes dk, the second dv: each gives the other sum to its partner.
 #pragma unroll
@@ -684,6 +710,7 @@ template <typename E, int DB>
 hipError_t run(const Args& A, bool token, hipStream_t st) {
   using T = typename std::conditional<std::is_same<E, float>::value, Split, E>::type;
   using L = Tile<T, DB>;
+  constexpr int FLAGS = in_parts<T> ? kFlags : 0;
   if (A.rq > 0 && token) {
     constexpr int PITCH = Tile<E, DB>::PITCH;
     hipLaunchKernelGGL((k_attn_dq_token<E, DB>), dim3(A.waves / 4), dim3(kThreads), 8 * kUnit * PITCH, st, A);
@@ -695,9 +722,9 @@ hipError_t run(const Args& A, bool token, hipStream_t st) {
   } else if (A.rq > 0) {
     const int64_t tiles = (A.rq * A.per + kRows - 1) / kRows + A.n;
     if (!crowded<T>(DB) && split_keys(A, tiles))
-      hipLaunchKernelGGL((k_attn_dq<T, (crowded<T>(DB) ? 1 : DB), 2>), flat_grid(tiles * A.kv), dim3(2 * kThreads), 8 * L::BYTES, st, A);
+      hipLaunchKernelGGL((k_attn_dq<T, (crowded<T>(DB) ? 1 : DB), 2>), flat_grid(tiles * A.kv), dim3(2 * kThreads), 8 * L::BYTES + FLAGS, st, A);
     else
-      hipLaunchKernelGGL((k_attn_dq<T, DB, 1>), flat_grid(tiles * A.kv), dim3(kThreads), 4 * L::BYTES, st, A);
+      hipLaunchKernelGGL((k_attn_dq<T, DB, 1>), flat_grid(tiles * A.kv), dim3(kThreads), 4 * L::BYTES + FLAGS, st, A);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -708,7 +735,7 @@ hipError_t run(const Args& A, bool token, hipStream_t st) {
     B.waves = p.parts;
     B.slots = p.slots;
     hipLaunchKernelGGL((k_attn_dkv<T, DB>), flat_grid(p.parts ? p.parts : p.items), dim3(4 * KEYS),
-                       2 * ((crowded<T>(DB) ? 0 : KEYS) + kQRows) * L::PITCH * L::PL + 2 * kQRows * 4, st, B);
+                       2 * ((crowded<T>(DB) ? 0 : KEYS) + kQRows) * L::PITCH * L::PL + 2 * kQRows * 4 + FLAGS, st, B);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
     if (p.parts) hipLaunchKernelGGL((k_attn_dkv_join<E, DB>), flat_grid(p.items, DB), dim3(4 * KEYS), 0, st, B);

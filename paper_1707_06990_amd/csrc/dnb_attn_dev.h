@@ -80,15 +80,26 @@ __device__ __forceinline__ float half_sum(float v) {
 // fp32 on the matrix cores' bf16 rate: x is the sum of three bf16 (8 bits of its 24 each, every remainder
 // exact), and of the nine products of two such sums the six that are not below 2^-23 of the whole are
 // made, at 32 cycles each where the fp32 instruction takes 512 for the same: six passes of a sixteenth.  Sums are
-// fp32 either way, and so is the error.  What has no such sum, infinities and values above the largest bf16
-// (3.39e38), counts as that value; NaN stays NaN.
+// fp32 either way, and so is the error.  Infinities and values above the largest bf16 (3.39e38) have no such sum:
+// their remainders are not finite, and every product with them is NaN.  A workgroup whose sums are not finite
+// therefore does its work once more with Whole, where the parts' sum is the value, whatever it is, and every
+// product is the fp32 instruction's: infinities are then what arithmetic makes of them, at four times the time.
 struct Split {};
+struct Whole {};
+template <typename T>
+constexpr bool is_whole = std::is_same<T, Whole>::value;
+template <typename T>
+constexpr bool in_parts = std::is_same<T, Split>::value || is_whole<T>;
 template <typename T>
 struct Elem {
   using type = T;
 };
 template <>
 struct Elem<Split> {
+  using type = float;
+};
+template <>
+struct Elem<Whole> {
   using type = float;
 };
 template <typename T>
@@ -98,7 +109,7 @@ __device__ __forceinline__ unsigned pack_bf16(float a, float b) {
   typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
   return __builtin_bit_cast(unsigned, (bf16x2){(__bf16)a, (__bf16)b});
 }
-__device__ __forceinline__ void split8(const float (&x)[8], Piece (&p)[3]) {
+__device__ __forceinline__ void split8(const float (&x)[8], Piece (&p)[3], Split*) {
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     const float a = x[2 * j], b = x[2 * j + 1];
@@ -110,34 +121,40 @@ __device__ __forceinline__ void split8(const float (&x)[8], Piece (&p)[3]) {
     p[2].q[j] = pack_bf16(a1 - __uint_as_float(mid << 16), b1 - __uint_as_float(mid & 0xffff0000u));
   }
 }
-// ... of 8 floats as loaded.  The largest magnitude decides for the whole wave whether any needs cutting.
+__device__ __forceinline__ void split8(const float (&x)[8], Piece (&p)[3], Whole*) {
+  constexpr float kMost = 3.3895313892515355e38f;  // the largest bf16
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    const bool inf = fabsf(x[j]) == INFINITY;
+    const float hi = inf || !(fabsf(x[j]) > kMost) ? (float)(__bf16)x[j] : copysignf(kMost, x[j]);
+    const float rest = inf ? 0.f : x[j] - hi;
+    const float mid = (float)(__bf16)rest;
+    p[0].b[j] = (__bf16)hi;
+    p[1].b[j] = (__bf16)mid;
+    p[2].b[j] = (__bf16)(rest - mid);
+  }
+}
+// ... of 8 floats as loaded
+template <typename T>
 __device__ __forceinline__ void split8(const u32x4& lo, const u32x4& hi, Piece (&p)[3]) {
-  constexpr float kMost = 3.3895313892515355e38f;
-  float x[8], top = 0.f;
+  float x[8];
 #pragma unroll
   for (int j = 0; j < 4; ++j) {
     x[j] = __uint_as_float(lo[j]);
     x[4 + j] = __uint_as_float(hi[j]);
   }
-#pragma unroll
-  for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(x[j]));
-  if (__any(top > kMost)) {
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (fabsf(x[j]) > kMost) x[j] = copysignf(kMost, x[j]);
-  }
-  split8(x, p);
+  split8(x, p, (T*)nullptr);
 }
 
 // A tile in LDS: rows of PC pieces of 16 bytes, of which CH hold the row (head_dim padded with zeros to
 // DB blocks of 32).  Piece c of row r lies at c ^ swz(r): sixteen rows read at one c (row_mul), and four
 // rows read 64 bytes wide (col_mul in bf16) or rows r and r + 4 read 128 bytes wide (in fp32), each meet
 // all the banks.  Each bit of swz is one of r's, so swz(r + s) is swz(r) ^ swz(s) where r and s share no bit.
-// Split: PL tiles, of the first, second and third parts.
+// In parts: PL tiles, of the first, second and third.
 template <typename T, int DB>
 struct Tile {
   static constexpr bool BF = !std::is_same<T, float>::value;
-  static constexpr int PL = std::is_same<T, Split>::value ? 3 : 1;
+  static constexpr int PL = in_parts<T> ? 3 : 1;
   static constexpr int EP = BF ? 8 : 4;                // elements of a piece
   static constexpr int LD = EP * sizeof(elem_t<T>) / 16;  // loads of a piece from memory
   static constexpr int CH = DB * 32 / EP;
@@ -166,16 +183,29 @@ struct Tile {
 inline bool split_keys(const Args& A, int64_t tiles) { return tiles * A.kv <= 256 && A.rk >= 256 * (int64_t)A.n; }
 
 // Copies of a step's tiles in LDS: the next one is written while one is read, unless the tiles are so large
-// that a second workgroup on the compute unit does more (Split above head_dim 64: 48 KB a copy).
+// that a second workgroup on the compute unit does more (in parts above head_dim 64: 48 KB a copy).
 template <typename T>
-constexpr int buffers(int blocks) { return std::is_same<T, Split>::value && blocks > 2 ? 1 : 2; }
+constexpr int buffers(int blocks) { return in_parts<T> && blocks > 2 ? 1 : 2; }
 
 // 16 bytes of a tile, or of each of its three
 template <typename T, int DB>
 using Pieces = Piece[Tile<T, DB>::PL];
 // a wave's 32 columns: of each step, this lane's half
 template <typename T, int DB>
-using Columns = Pieces<T, DB>[Tile<T, DB>::NS];
+struct ColumnsOf {
+  using type = Pieces<T, DB>[Tile<T, DB>::NS];
+};
+// Whole: where they are in memory, read at every use.  What is done so seldom must not take registers from Split.
+struct Row {
+  const float* at;
+  int d;  // 0: zeros
+};
+template <int DB>
+struct ColumnsOf<Whole, DB> {
+  using type = Row;
+};
+template <typename T, int DB>
+using Columns = typename ColumnsOf<T, DB>::type;
 
 __device__ __forceinline__ void mma(f32x16& acc, const Piece (&a)[1], const Piece (&b)[1], __bf16*) {
   acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[0].h, b[0].h, acc, 0, 0, 0);
@@ -191,6 +221,13 @@ __device__ __forceinline__ void mma(f32x16& acc, const Piece (&a)[3], const Piec
   acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[0].h, b[1].h, acc, 0, 0, 0);
   acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[1].h, b[0].h, acc, 0, 0, 0);
   acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a[0].h, b[0].h, acc, 0, 0, 0);
+}
+// (a lane's eight of the 16 steps of the bf16 instruction are eight instructions of two steps, one of each half.
+// Second and third part first: the first two of the largest values add up to 2^128.)
+__device__ __forceinline__ float whole(const Piece (&p)[3], int j) { return (float)p[0].b[j] + ((float)p[1].b[j] + (float)p[2].b[j]); }
+__device__ __forceinline__ void mma(f32x16& acc, const Piece (&a)[3], const Piece (&b)[3], Whole*) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(whole(a, j), whole(b, j), acc, 0, 0, 0);
 }
 
 // Addresses in LDS as bytes from its start: what differs between a wave's reads of a tile is then a
@@ -229,12 +266,26 @@ __device__ __forceinline__ f32x16 row_mul(lds_t tile, int row0, const Columns<T,
   using L = Tile<T, DB>;
   const lds_t at = row_address<T, DB, HOLD>(row0);
   f32x16 s = {};
-#pragma unroll
-  for (int k = 0; k < L::NS; ++k) {
-    Pieces<T, DB> a;
+  auto piece = [&](int k, Pieces<T, DB>& a) {
 #pragma unroll
     for (int p = 0; p < L::PL; ++p) a[p].q = lds_read<u32x4>((at ^ (k << 5)) + (tile + p * TR * L::PITCH));
-    mma(s, a, b[k], (T*)nullptr);
+  };
+  if constexpr (is_whole<T>) {
+#pragma unroll 1
+    for (int k = 0; k < L::NS; ++k) {
+      Pieces<T, DB> a;
+      piece(k, a);
+      const int e = (2 * k + (lane_id() >> 5)) * L::EP;
+#pragma unroll
+      for (int j = 0; j < L::EP; ++j) s = __builtin_amdgcn_mfma_f32_32x32x2f32(whole(a, j), e < b.d ? b.at[e + j] : 0.f, s, 0, 0, 0);
+    }
+  } else {
+#pragma unroll
+    for (int k = 0; k < L::NS; ++k) {
+      Pieces<T, DB> a;
+      piece(k, a);
+      mma(s, a, b[k], (T*)nullptr);
+    }
   }
   return s;
 }
@@ -251,14 +302,15 @@ __device__ __forceinline__ void col_mul(lds_t tile, int row0, const f32x16& s, f
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       Pieces<T, DB> y;
-      if constexpr (L::PL == 1) {
+      if constexpr (is_whole<T>) {
+      } else if constexpr (L::PL == 1) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) y[0].b[j] = (__bf16)s[8 * t + j];
       } else {
         float v[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = s[8 * t + j];
-        split8(v, y);
+        split8(v, y, (T*)nullptr);
       }
 #pragma unroll
       for (int db = 0; db < DB; ++db) {
@@ -272,7 +324,13 @@ __device__ __forceinline__ void col_mul(lds_t tile, int row0, const f32x16& s, f
           const uint2 a = __builtin_bit_cast(uint2, lo), b = __builtin_bit_cast(uint2, hi);
           x[p].q = (u32x4){a.x, a.y, b.x, b.y};
         }
-        mma(acc[db], x, y, (T*)nullptr);
+        if constexpr (is_whole<T>) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(whole(x, j), s[8 * t + j], acc[db], 0, 0, 0);
+          __builtin_amdgcn_sched_barrier(0);  // no reads ahead, no registers for them
+        } else {
+          mma(acc[db], x, y, (T*)nullptr);
+        }
       }
     }
   } else {
@@ -309,7 +367,7 @@ __device__ __forceinline__ void write_piece(lds_t to, const u32x4* r) {
     lds_write(to, r[0]);
   } else {
     Piece p[3];
-    split8(r[0], r[1], p);
+    split8<T>(r[0], r[1], p);
 #pragma unroll
     for (int i = 0; i < 3; ++i) lds_write(to + i * TR * L::PITCH, p[i].q);
   }
@@ -367,18 +425,22 @@ struct Stage {
 template <typename T, int DB>
 __device__ __forceinline__ void load_cols(Columns<T, DB>& f, const elem_t<T>* row, bool valid, int d) {
   using L = Tile<T, DB>;
-  const int h = lane_id() >> 5;
+  if constexpr (is_whole<T>) {
+    f = {row, valid ? d : 0};
+  } else {
+    const int h = lane_id() >> 5;
 #pragma unroll
-  for (int k = 0; k < L::NS; ++k) {
-    const int e = (2 * k + h) * L::EP;
-    u32x4 x[L::LD];
+    for (int k = 0; k < L::NS; ++k) {
+      const int e = (2 * k + h) * L::EP;
+      u32x4 x[L::LD];
 #pragma unroll
-    for (int p = 0; p < L::LD; ++p) {
-      x[p] = (u32x4){0u, 0u, 0u, 0u};
-      if (valid && e < d) x[p] = *reinterpret_cast<const u32x4*>(row + e + p * (L::EP / L::LD));
+      for (int p = 0; p < L::LD; ++p) {
+        x[p] = (u32x4){0u, 0u, 0u, 0u};
+        if (valid && e < d) x[p] = *reinterpret_cast<const u32x4*>(row + e + p * (L::EP / L::LD));
+      }
+      if constexpr (L::PL == 1) f[k][0].q = x[0];
+      else split8<T>(x[0], x[1], f[k]);
     }
-    if constexpr (L::PL == 1) f[k][0].q = x[0];
-    else split8(x[0], x[1], f[k]);
   }
 }
 // The product of two rows of d elements, half of it in each half of the wave
@@ -426,6 +488,35 @@ __device__ __forceinline__ void store_cols(T* row, bool valid, int d, const f32x
             make_float4(acc[db][4 * g] * f, acc[db][4 * g + 1] * f, acc[db][4 * g + 2] * f, acc[db][4 * g + 3] * f);
       }
     }
+}
+
+// Whether some value of the wave's is infinite or NaN
+template <int DB>
+__device__ __forceinline__ bool not_finite(const f32x16 (&acc)[DB]) {
+  float t = 0.f;
+#pragma unroll
+  for (int db = 0; db < DB; ++db)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) t = fmaf(acc[db][i], 0.f, t);
+  return __any(t != t);
+}
+// x in a form in which Whole's walk does not share it, or what is made of it, with the walk before: it would take a
+// register through all of that.
+template <typename F, typename X>
+__device__ __forceinline__ X apart(X x) {
+  if (is_whole<F>) asm volatile("" : "+v"(x));
+  return x;
+}
+// v of any of the workgroup's WAVES waves, through kFlags bytes of LDS at `at`
+constexpr int kFlags = 64;
+template <int WAVES>
+__device__ __forceinline__ bool any_wave(lds_t at, bool v) {
+  if (lane_id() == 0) lds_write(at + 4 * (threadIdx.x >> 6), (int)v);
+  __syncthreads();
+  int any = 0;
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) any |= lds_read<int>(at + 4 * w);
+  return __builtin_amdgcn_readfirstlane(any) != 0;
 }
 
 // One sequence, as its offsets say; whatever they hold, the rows stay inside the tensors.  nk may be 2^31 - 1:
