@@ -485,7 +485,7 @@ typedef struct dnb_attn dnb_attn; /* opaque, host side only */
 typedef struct {
   int32_t heads, kv_heads;  /* heads a multiple of kv_heads                                      */
   int32_t head_dim;         /* a multiple of 8 up to 128 (else DNB_E_UNSUPPORTED)                */
-  int32_t sequences;        /* >= 1                                                              */
+  int32_t sequences;        /* 1 to 2^20                                                         */
   int64_t rows_q, rows_k;   /* rows of the tensors; 0 is allowed                                 */
   int64_t q_stride;         /* elements between rows of q and dq, k and dk, v and dv; 0: dense.  */
   int64_t k_stride;         /* Multiples of 16 bytes, at most 2^22; out and dout are dense, so   */
@@ -496,7 +496,8 @@ typedef struct {
 } dnb_attn_desc;
 int dnb_attn_create(const dnb_attn_desc* desc, dnb_attn** out);
 void dnb_attn_destroy(dnb_attn* plan);
-/* Scratch of either call below (16-byte aligned).  Nothing in it lasts from one call to the next. */
+/* Scratch of either call below (16-byte aligned).  Nothing in it lasts from one call to the next.  (Of more than
+ * 128 sequences backward needs it without queries too.) */
 size_t dnb_attn_workspace_bytes(const dnb_attn* plan);
 int dnb_attn_forward(const dnb_attn* plan, const void* q, const void* k, const void* v, const int32_t* q_offsets,
                      const int32_t* k_offsets, const int32_t* k_lengths, void* out, float* lse, void* workspace, void* stream);

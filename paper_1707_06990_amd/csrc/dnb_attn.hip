@@ -27,7 +27,6 @@ namespace attn {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kRows = 128;  // packed rows of a workgroup of k_attn, 32 a wave
 
 // The state of 32 rows: O^T, running maximum (log2 units of the scaled scores) and this half's sum.
 template <int DB>
@@ -99,8 +98,7 @@ __global__ __launch_bounds__(kThreads * KH, 2) void k_attn(Args A) {
   const int g = id % A.kv, l = lane_id(), wave = (threadIdx.x >> 6) & 3, kh = KH == 1 ? 0 : (int)(threadIdx.x >> 8);
   Seq S;
   int t, count;
-  if (!find_tile(A, id / A.kv, [&](const Seq& s) { return (int)(((int64_t)s.nq * A.per + kRows - 1) / kRows); }, &S, &t, &count))
-    return;
+  if (!find_tile(A, id / A.kv, &S, &t, &count)) return;
   if (A.causal) t = count - 1 - t;  // the rows that see most keys go first
   const RowTile R0(A, S, g, t * kRows + wave * 32);
   const unsigned all = RowTile::seen(A, S, min((t + 1) * kRows, S.nq * A.per) - 1);  // keys that the workgroup's last row sees
@@ -306,6 +304,11 @@ __global__ __launch_bounds__(kThreads) void k_attn_join(Args A) {
 
 template <typename T, int DB>
 hipError_t run_forward(const Args& A, bool token, hipStream_t st) {
+  if (A.index) {
+    hipLaunchKernelGGL(k_attn_index<RowSums>, dim3(1), dim3(kIndexThreads), 0, st, A, (int64_t*)A.index);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
   if (token) {
     constexpr int PITCH = Tile<T, DB>::PITCH;
     hipLaunchKernelGGL((k_attn_token<T, DB>), dim3(A.waves / 4), dim3(kThreads), 8 * kUnit * PITCH, st, A);
@@ -347,12 +350,12 @@ struct dnb_attn {
   bool token;       // the forward's form
   int waves;        // of the token form
   int64_t slots;
-  size_t ws_part, ws_rowdot, ws_bytes;
+  size_t ws_index, ws_part, ws_rowdot, ws_bytes;
 };
 
 namespace {
 
-void fill(const dnb_attn* p, Args* A) {
+void fill(const dnb_attn* p, void* workspace, bool backward, Args* A) {
   const dnb_attn_desc& d = p->d;
   *A = Args{};
   A->n = d.sequences; A->heads = d.heads; A->kv = d.kv_heads; A->per = d.heads / d.kv_heads; A->d = d.head_dim;
@@ -363,6 +366,10 @@ void fill(const dnb_attn* p, Args* A) {
   A->c = d.scale * kLog2e;
   A->waves = p->waves;
   A->slots = p->slots;
+  char* ws = (char*)workspace;
+  A->rowdot = (float*)(ws + p->ws_rowdot);
+  A->index = d.sequences > (p->token ? kScanSplit : backward ? kScanBackward : kScanForward) ? (const int64_t*)(ws + p->ws_index) : nullptr;
+  A->part = (float*)(ws + p->ws_part);
 }
 
 }  // namespace
@@ -399,7 +406,8 @@ int dnb_attn_create(const dnb_attn_desc* desc, dnb_attn** out) {
   p->waves = d.dtype == DNB_BF16 ? 2048 : 1024;  // 256 compute units, two workgroups of four waves each, fp32 one
   p->slots = p->token ? p->waves + ((d.rows_q * per + kItemRows - 1) / kItemRows + d.sequences) * d.kv_heads : 0;
   p->ws_rowdot = 0;
-  p->ws_part = ((size_t)d.rows_q * d.heads * sizeof(float) + 255) / 256 * 256;
+  p->ws_index = ((size_t)d.rows_q * d.heads * sizeof(float) + 255) / 256 * 256;
+  p->ws_part = (p->ws_index + index_bytes(d.sequences) + 255) / 256 * 256;
   const size_t fwd = (size_t)p->slots * slot_floats(dp) * sizeof(float);
   const size_t bwd = backward_part_bytes(d.rows_q, d.rows_k, d.sequences, d.kv_heads, per, d.head_dim, d.dtype == DNB_BF16);
   p->ws_bytes = p->ws_part + (fwd > bwd ? fwd : bwd);
@@ -419,10 +427,9 @@ int dnb_attn_forward(const dnb_attn* p, const void* q, const void* k, const void
   for (const void* x : {q, k, v, (const void*)out, (const void*)workspace})
     if (!aligned16(x)) return DNB_E_ALIGN;
   Args A;
-  fill(p, &A);
+  fill(p, workspace, false, &A);
   A.q = q; A.k = k; A.v = v; A.o = out; A.lse = lse;
   A.qo = q_offsets; A.ko = k_offsets; A.kl = k_lengths;
-  A.part = (float*)((char*)workspace + p->ws_part);
   hipStream_t st = (hipStream_t)stream;
   const hipError_t e = p->d.dtype == DNB_BF16 ? run_forward_db<__bf16>(A, p->token, st) : run_forward_db<float>(A, p->token, st);
   return e == hipSuccess ? DNB_OK : DNB_E_LAUNCH;
@@ -434,16 +441,14 @@ int dnb_attn_backward(const dnb_attn* p, const void* q, const void* k, const voi
   if (!p || !q_offsets || !k_offsets) return DNB_E_NULL;
   const bool anyq = p->d.rows_q > 0, anyk = p->d.rows_k > 0;
   if (anyq && (!q || !out || !lse || !dout || !dq || !workspace)) return DNB_E_NULL;
-  if (anyk && (!k || !v || !dk || !dv)) return DNB_E_NULL;
+  if (anyk && (!k || !v || !dk || !dv || (p->d.sequences > kScanSplit && !workspace))) return DNB_E_NULL;
   for (const void* x : {q, k, v, out, dout, (const void*)dq, (const void*)dk, (const void*)dv, (const void*)workspace})
     if (!aligned16(x)) return DNB_E_ALIGN;
   Args A;
-  fill(p, &A);
+  fill(p, workspace, true, &A);
   A.q = q; A.k = k; A.v = v; A.out = out; A.lse = (float*)lse; A.dout = dout;
   A.dq = dq; A.dk = dk; A.dv = dv;
   A.qo = q_offsets; A.ko = k_offsets; A.kl = k_lengths;
-  A.rowdot = (float*)((char*)workspace + p->ws_rowdot);
-  A.part = (float*)((char*)workspace + p->ws_part);
   const hipError_t e = launch_backward(A, p->d.dtype == DNB_BF16, p->token, (hipStream_t)stream);
   return e == hipSuccess ? DNB_OK : DNB_E_LAUNCH;
 }

@@ -18,7 +18,6 @@ namespace attn {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kRows = 128;  // packed rows of a workgroup of k_attn_dq, 32 a wave
 
 // bf16: where a row sees few keys its ds is large, and two roundings show in it.  Rows that see up to this many
 // keys therefore
@@ -46,8 +45,7 @@ __global__ __launch_bounds__(kThreads * KH, crowded<T>(DB) ? 1 : 2) void k_attn_
   const int g = id % A.kv, l = lane_id(), wave = (threadIdx.x >> 6) & 3, kh = KH == 1 ? 0 : (int)(threadIdx.x >> 8);
   Seq S;
   int t, count;
-  if (!find_tile(A, id / A.kv, [&](const Seq& s) { return (int)(((int64_t)s.nq * A.per + kRows - 1) / kRows); }, &S, &t, &count))
-    return;
+  if (!find_tile(A, id / A.kv, &S, &t, &count)) return;
   if (A.causal) t = count - 1 - t;
   const RowTile R0(A, S, g, t * kRows + wave * 32);
   const unsigned all = RowTile::seen(A, S, min((t + 1) * kRows, S.nq * A.per) - 1);  // keys that the workgroup's last row sees
@@ -353,7 +351,18 @@ __device__ __forceinline__ int64_t key_parts(int64_t total, int most, bool bf16)
   return max((int64_t)1, min((int64_t)most, total / least_cost(bf16)));
 }
 template <int KEYS, bool BF>
+struct KeySums {
+  static constexpr int N = kSums;
+  static __device__ __forceinline__ void sums(const Args& A, const Seq& s, int64_t* v) {
+    RowSums::sums(A, s, v);
+    const KeyLine<KEYS, BF> k(A, s);
+    v[kCost] = k.before(k.tiles) * A.kv;
+    v[kKeyItems] = k.tiles * A.kv;
+  }
+};
+template <int KEYS, bool BF>
 __device__ __forceinline__ int64_t key_total(const Args& A) {
+  if (A.index) return index_of(A, kCost)[chunks_of(A.n)];
   int64_t u = 0;
   for (int i = lane_id(); i < A.n; i += 64) {
     const KeyLine<KEYS, BF> k(A, seq_at(A, i));
@@ -374,7 +383,14 @@ __device__ __forceinline__ KeyAt key_at(const Args& A, int64_t x, bool by_item) 
   const int l = lane_id();
   KeyAt r = {};
   int64_t u0 = 0, i0 = 0;  // cost and items before the 64 sequences at hand
-  for (int base = 0; base < A.n; base += 64) {
+  int base = 0;
+  if (A.index) {
+    const int c = index_find(index_of(A, by_item ? kKeyItems : kCost), chunks_of(A.n), x);
+    base = c * 64;
+    u0 = index_of(A, kCost)[c];
+    i0 = index_of(A, kKeyItems)[c];
+  }
+  for (; base < A.n; base += 64) {
     Seq mine = {};
     int64_t cost = 0, items = 0;
     if (base + l < A.n) {
@@ -456,6 +472,7 @@ __global__ __launch_bounds__(4 * keys_of(sizeof(elem_t<T>) == 2, DB), crowded<T>
       const int g = at.g;
       const int64_t t = at.t, lo = at.lo, full = line.before(t + 1) - line.before(t), hi = whole ? full : min(full, lo + b - a), item = at.item;
       a += hi - lo;
+      const int64_t slot = lo == 0 && hi == full ? -1 : w + item;  // of a part's sums; -1: the item is whole
 
       const unsigned c0 = (unsigned)t * KEYS, w0 = c0 + kb, key = w0 + (l & 31), nk = S.nk;
       const int64_t shift = (int64_t)S.nk - S.nq;
@@ -489,7 +506,7 @@ __global__ __launch_bounds__(4 * keys_of(sizeof(elem_t<T>) == 2, DB), crowded<T>
         }
         // the first packed row that sees this lane's key; the wave's first key, its last
         auto first_for = [&](unsigned k) { return A.causal ? (int)min(max(((int64_t)k - shift - first) * per, (int64_t)0), (int64_t)left) : 0; };
-        const int need = valid ? first_for(key) : left, need0 = first_for(w0), need1 = w0 + 32 > nk ? left : first_for(w0 + 31);
+        const int need = valid ? first_for(key) : left, need0 = w0 < nk ? first_for(w0) : INT32_MAX, need1 = w0 + 32 > nk ? left : first_for(w0 + 31);
         // the step at hand starts at packed row m0: query q0 of the sequence, head s0 of the group
         int q0 = first + m0 / per, s0 = m0 % per;
         constexpr int U = (kQRows * L::CH + NT - 1) / NT;
@@ -540,7 +557,7 @@ __global__ __launch_bounds__(4 * keys_of(sizeof(elem_t<T>) == 2, DB), crowded<T>
           }
           if (!is_whole<F> && m0 + kQRows < left) fetch(m0 + kQRows, q0, s0);
           // uniform in the wave: some row of the block sees some key of the wave
-          if (w0 < nk && m0 + qb < left && m0 + qb + 31 >= need0) {
+          if (m0 + qb < left && m0 + qb + 31 >= need0) {
             f32x16 s, dp;
             if constexpr (COLS) {
               s = row_mul<F, DB, false, kQRows>(qt, qb, kf);
@@ -615,11 +632,11 @@ __global__ __launch_bounds__(4 * keys_of(sizeof(elem_t<T>) == 2, DB), crowded<T>
             dk[db][4 * q + 3] += x.w;
           }
       }
-      if (lo == 0 && hi == full) {  // rows of the sequence's span that are not in use get zeros
+      if (slot < 0) {  // rows of the sequence's span that are not in use get zeros
         const int64_t krow = (int64_t)S.k0 + key, to = krow * (second ? A.vs : A.ks) + (int64_t)g * A.d;
         store_cols<E, DB>((E*)(second ? A.dv : A.dk) + to, key < (unsigned)S.span, A.d, dk, second ? 1.f : A.scale);
-      } else if (w + item < A.slots) {
-        float4* part = reinterpret_cast<float4*>(A.part) + ((w + item) * 2 * KB + wave) * DB * 4 * 64;
+      } else if (slot < A.slots) {
+        float4* part = reinterpret_cast<float4*>(A.part) + (slot * 2 * KB + wave) * DB * 4 * 64;
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -641,7 +658,15 @@ __global__ __launch_bounds__(4 * keys_of(sizeof(T) == 2, DB)) void k_attn_dkv_jo
   int64_t u0 = 0, i0 = 0, su = 0, si = 0;
   Seq S = {};
   bool found = false;
-  for (int base = 0; base < A.n; base += 64) {
+  int base = 0, end = A.n;
+  if (A.index) {
+    const int c = index_find(index_of(A, kKeyItems), chunks_of(A.n), item);
+    base = c * 64;
+    end = min(base + 64, A.n);
+    u0 = index_of(A, kCost)[c];
+    i0 = index_of(A, kKeyItems)[c];
+  }
+  for (; base < end; base += 64) {
     Seq mine = {};
     int64_t cost = 0, items = 0;
     if (base + l < A.n) {
@@ -664,7 +689,7 @@ __global__ __launch_bounds__(4 * keys_of(sizeof(T) == 2, DB)) void k_attn_dkv_jo
   }
   if (!found) return;
   const KeyLine<KEYS, BF> line(A, S);
-  const int64_t total = u0, W = key_parts(total, A.waves, BF);
+  const int64_t total = A.index ? key_total<KEYS, BF>(A) : u0, W = key_parts(total, A.waves, BF);
   const int g = (int)((item - si) / line.tiles);
   const int64_t t = (item - si) - g * line.tiles;
   const int64_t from = su + g * line.before(line.tiles) + line.before(t), to = from + line.before(t + 1) - line.before(t);
@@ -711,6 +736,11 @@ hipError_t run(const Args& A, bool token, hipStream_t st) {
   using T = typename std::conditional<std::is_same<E, float>::value, Split, E>::type;
   using L = Tile<T, DB>;
   constexpr int FLAGS = in_parts<T> ? kFlags : 0;
+  if (A.index && (A.rq > 0 || A.rk > 0)) {
+    hipLaunchKernelGGL((k_attn_index<KeySums<keys_of(sizeof(E) == 2, DB), sizeof(E) == 2>>), dim3(1), dim3(kIndexThreads), 0, st, A, (int64_t*)A.index);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
   if (A.rq > 0 && token) {
     constexpr int PITCH = Tile<E, DB>::PITCH;
     hipLaunchKernelGGL((k_attn_dq_token<E, DB>), dim3(A.waves / 4), dim3(kThreads), 8 * kUnit * PITCH, st, A);
