@@ -478,9 +478,10 @@ int dnb_op_maxpool3s2_backward(const void* dout, const void* pos, void* din, int
  *   written; dk and dv of rows that are not in use yet are zero.  Offsets that leave the tensors are cut
  *   to them, and offsets that decrease give undefined values in the outputs, but no access outside.
  * A value that is infinite or NaN in q, k, v or dout reaches the results that depend on it, as inf or NaN
- * as arithmetic makes it, and may reach as NaN those of the same sequence that a causal mask keeps from it
- * (a hidden weight is 0, and 0 times infinity is NaN).  DNB_F32: work with results that are not finite is
- * done twice and takes about four times as long. */
+ * as arithmetic makes it.  In DNB_BF16, and where few rows have long keys, it may also reach as NaN those
+ * of the same sequence that a causal mask keeps from it (a hidden weight is 0, and 0 times infinity is
+ * NaN); in DNB_F32 else it does not.  DNB_F32: work with results that are not finite is done twice and
+ * takes about five times as long. */
 typedef struct dnb_attn dnb_attn; /* opaque, host side only */
 typedef struct {
   int32_t heads, kv_heads;  /* heads a multiple of kv_heads                                      */

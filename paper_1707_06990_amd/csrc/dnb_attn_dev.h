@@ -84,7 +84,8 @@ __device__ __forceinline__ float half_sum(float v) {
 // fp32 either way, and so is the error.  Infinities and values above the largest bf16 (3.39e38) have no such sum:
 // their remainders are not finite, and every product with them is NaN.  A workgroup whose sums are not finite
 // therefore does its work once more with Whole, where the parts' sum is the value, whatever it is, and every
-// product is the fp32 instruction's: infinities are then what arithmetic makes of them, at four times the time.
+// product is the fp32 instruction's: infinities are then what arithmetic makes of them, at five times the time, and
+// hidden ones nothing.
 struct Split {};
 struct Whole {};
 template <typename T>
@@ -291,6 +292,39 @@ __device__ __forceinline__ f32x16 row_mul(lds_t tile, int row0, const Columns<T,
   return s;
 }
 
+// acc += X^T S over eight rows a lane, S from element s0 on, where a weight of 0 takes nothing of a value, whatever that is:
+// hidden pairs have that weight.  What is not finite is left out of the product and counted: infinities that
+// arrive with either sign, and NaN.
+__device__ __forceinline__ void whole_mul(f32x16& acc, const Piece (&x)[3], const f32x16& s, int s0) {
+  float v[8], odd = 0.f;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    v[j] = whole(x, j);
+    const bool fin = fabsf(v[j]) < INFINITY;
+    odd = fin ? odd : 1.f;
+    acc = __builtin_amdgcn_mfma_f32_32x32x2f32(fin ? v[j] : 0.f, s[s0 + j], acc, 0, 0, 0);
+  }
+  if (!__any(odd != 0.f)) return;
+  auto one = [](bool b) { return b ? 1.f : 0.f; };
+#pragma unroll
+  for (int kind = 0; kind < 3; ++kind) {
+    const float to = kind == 0 ? INFINITY : kind == 1 ? -INFINITY : NAN;
+    f32x16 count = {};
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      const float w = s[s0 + j];
+      if (kind == 2) {
+        count = __builtin_amdgcn_mfma_f32_32x32x2f32(one(v[j] != v[j]), one(w < 0.f || w > 0.f), count, 0, 0, 0);
+      } else {
+        count = __builtin_amdgcn_mfma_f32_32x32x2f32(one(v[j] == to), one(w > 0.f), count, 0, 0, 0);
+        count = __builtin_amdgcn_mfma_f32_32x32x2f32(one(v[j] == -to), one(w < 0.f), count, 0, 0, 0);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) acc[i] += count[i] > 0.f ? to : 0.f;
+  }
+}
+
 // bf16: rounding s to 8 bits of mantissa is what feeding the matrix cores at their bf16 rate costs;
 // the sums stay in fp32.
 template <typename T, int DB, bool HOLD = false, int TR = 32>
@@ -326,8 +360,7 @@ __device__ __forceinline__ void col_mul(lds_t tile, int row0, const f32x16& s, f
           x[p].q = (u32x4){a.x, a.y, b.x, b.y};
         }
         if constexpr (is_whole<T>) {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(whole(x, j), s[8 * t + j], acc[db], 0, 0, 0);
+          whole_mul(acc[db], x, s, 8 * t);
           __builtin_amdgcn_sched_barrier(0);  // no reads ahead, no registers for them
         } else {
           mma(acc[db], x, y, (T*)nullptr);

@@ -100,3 +100,45 @@ def test_infinite_gradients_stay_infinite(dnb, form):
         f = torch.isfinite(w)
         assert_within(g[f], w[f], t[f], name)
     p.close()
+
+
+MASKED = {"tile": ([70, 40], [70, 40], 4, 2, 64), "tile128": ([70, 40], [75, 40], 4, 2, 128), "eight": ([1300], [1300], 12, 12, 32),
+          "eight128": ([1300], [1310], 12, 12, 128)}
+
+
+@pytest.mark.parametrize("bad", [math.inf, -math.inf, math.nan])
+@pytest.mark.parametrize("form", MASKED, ids=list(MASKED))
+def test_what_a_causal_mask_hides_does_not_matter(dnb, form, bad):
+    """Keys, values, queries and dout from some row on: earlier queries do not see those keys, and later keys are not seen
+    by those queries, whatever they hold.  Within one tile of 32, and in its tile's neighbours."""
+    q, k, heads, kv, dim = MASKED[form]
+    p = Problem(dnb, "f32", q, k, heads, kv, dim, True)
+    shift, n = k[0] - q[0], 45
+    good = [t.clone() for t in (p.q, p.k, p.v, p.dout)]
+    o, l, to, tl = p.oracle()
+    # forward and dq: a value, and a key, that queries from n on see
+    for which in ("v", "k"):
+        p.q, p.k, p.v, p.dout = (t.clone() for t in good)
+        getattr(p, which)[n + shift, 0, 3] = bad
+        p.dk_, p.dv_ = p.k.cuda(), p.v.cuda()
+        out, lse = p.forward()
+        same(out[:n], o[:n], to[:n], f"out, {which}")
+        assert_within(lse[:, :n], l[:, :n], tl[:, :n], "lse")
+        assert not bool(torch.isfinite(out[n:q[0], 0]).all())
+        assert torch.equal(torch.isfinite(out[q[0]:]), torch.ones_like(out[q[0]:], dtype=torch.bool))
+        out_, lse_ = o.float(), l.float()
+        dq = p.backward(out_.cuda(), lse_.cuda())[0]
+        (want, _, _), (tol, _, _) = attn_backward(good[0], good[1], good[2], out_, lse_, good[3], p.qo, p.ko, None, True)
+        same(dq[:n], want[:n], tol[:n], f"dq, {which}")
+    # dk and dv: a query, and a dout, that keys up to n + shift see
+    want, tol = attn_backward(good[0], good[1], good[2], o.float(), l.float(), good[3], p.qo, p.ko, None, True)
+    later = slice(n + shift + 1, k[0])
+    for which in ("q", "dout"):
+        p.q, p.k, p.v, p.dout = (t.clone() for t in good)
+        getattr(p, which)[n, 0, 3] = bad
+        p.dq_, p.dk_, p.dv_ = p.q.cuda(), p.k.cuda(), p.v.cuda()
+        _, dk, dv = p.backward(o.float().cuda(), l.float().cuda())
+        same(dk[later], want[1][later], tol[1][later], f"dk, {which}")
+        same(dv[later], want[2][later], tol[2][later], f"dv, {which}")
+        assert not bool(torch.isfinite(dk[:n + shift + 1, 0]).all())
+    p.close()
