@@ -122,7 +122,7 @@ class Cache:
 
     def __init__(self, block, requests, capacity):
         m = self.m = block
-        self.capacity, self.requests = capacity, requests
+        self.capacity, self.requests, self.used = capacity, requests, 0
         self.k, self.v = (torch.empty(requests * capacity, m.kv_heads * m.dim, dtype=m.dtype, device="cuda") for _ in range(2))
         self.lengths = torch.zeros(requests, dtype=torch.int32, device="cuda")
         self.q_offsets = torch.arange(requests + 1, dtype=torch.int32, device="cuda")
@@ -132,7 +132,10 @@ class Cache:
         self.workspace = torch.empty(dnb.dnb_attn_workspace_bytes(self.attn), dtype=torch.uint8, device="cuda")
 
     def next(self, tokens):
-        """Logits after one more token of each request."""
+        """Logits after one more token of each request.  ValueError where there is no room for it."""
+        if self.used == self.capacity:
+            raise ValueError(f"the cache holds {self.capacity} tokens a request")
+        self.used += 1
         m = self.m
         x = m.p["embed"].to(m.dtype)[tokens]
         q, k, v = m.qkv(m.product(x, m.p["qkv"]), self.lengths)
