@@ -1,7 +1,7 @@
-"""A decoder block on packed documents, trained for a few steps, then asked for single tokens over a cache:
-the sequence operators of the library (attention, rotary positions, the norms around a block, clipping of
-all gradients by their norm) in the order in which such a program calls them.  The matrix products between
-them are torch's.
+"""The attention half of a decoder block on packed documents, trained for a few steps, then asked for single
+tokens over a cache: the sequence operators of the library (attention, rotary positions, the norms around a
+block, clipping of all gradients by their norm) in the order in which such a program calls them.  The matrix
+products between them are torch's; there is no first norm and no feed-forward half.
 
     python example_decoder.py [--steps 20] [--width 256] [--heads 8] [--kv-heads 2] [--dtype bf16]
 
@@ -18,7 +18,7 @@ import paper_1707_06990_amd as dnb
 
 
 class Block:
-    """Embedding -> norm -> attention with rotary positions -> norm, gate and residual -> symbols.  Parameters
+    """Embedding -> attention with rotary positions -> norm, gate and residual -> norm -> symbols.  Parameters
     fp32; activations and the gradients of matrices in `dtype`."""
 
     def __init__(self, symbols, width, heads, kv_heads, dtype, seed=0):
