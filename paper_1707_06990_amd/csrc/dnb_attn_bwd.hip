@@ -309,9 +309,10 @@ constexpr int kQRows = 64;      // packed rows of a step of k_attn_dkv
 // tiles; above: four, with k and v in registers, since LDS holds no more than the rows' tiles.
 constexpr int keys_of(bool bf16, int blocks) { return bf16 ? (blocks == 4 ? 128 : 64) : blocks <= 2 ? 128 : 64; }
 
-// What an item costs beside its rows, in rows: some 5 us, three steps in bf16, less than one in fp32, whose
-// products take sixteen times as long.
-constexpr int item_cost(bool bf16) { return bf16 ? 192 : 48; }
+// What an item costs beside its rows, in rows: some 5 us, three steps in bf16, one and a half in fp32, whose steps
+// are six products for one.  (fp32, 48 / 96 / 160: a step over 2264 packed rows of 16/8 heads of 128, causal, 590 / 540 /
+// 530 us, of 64 290 / 283 / 286; 1320 of 4 heads of 64, full, 127 / 128 / 131.)
+constexpr int item_cost(bool bf16) { return bf16 ? 192 : 96; }
 // Cost of the smallest part worth a workgroup.
 constexpr int least_cost(bool bf16) { return item_cost(bf16) + kQRows; }
 
