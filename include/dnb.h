@@ -461,7 +461,8 @@ int dnb_op_maxpool3s2_backward(const void* dout, const void* pos, void* din, int
 /* ------------------------------------------------------------------------------------------
  * Sequence operators: attention over packed sequences, rotary positions, the norms around a block, and
  * the clipping of many gradients by their global norm.  Types: DNB_F32 or DNB_BF16 for the tensors named
- * "of the type"; sums, statistics and softmax are fp32 in both.  Pointers, streams and errors as above;
+ * "of the type"; sums, statistics, exponentials and what is kept of a softmax are fp32 in both (see
+ * attention for what DNB_BF16 rounds between two products).  Pointers, streams and errors as above;
  * tensors of the type are 16-byte aligned.  No call allocates device memory, copies to the host or
  * synchronises; all of them may be captured into a graph.
  *
@@ -477,6 +478,11 @@ int dnb_op_maxpool3s2_backward(const void* dout, const void* pos, void* din, int
  *   k_lengths: `sequences` int32 on the device or null.  Rows of no sequence are neither read nor
  *   written; dk and dv of rows that are not in use yet are zero.  Offsets that leave the tensors are cut
  *   to them, and offsets that decrease give undefined values in the outputs, but no access outside.
+ * DNB_BF16 rounds to bf16, besides its results: the softmax's weights before their products with v and
+ * dout, and the gradients of the scores before theirs with q and k (of rows that see up to 128 keys these
+ * in two parts, of 16 bits together).  Results are 1.2 to 1.4 times as far from exact ones as their own
+ * rounding alone.  DNB_F32 takes each value in three parts of 8 bits and leaves out products below 2^-23 of
+ * the whole, where many rows share keys (4.2e-7 from exact gradients, after 3.9e-7 of fp32 arithmetic).
  * A value that is infinite or NaN in q, k, v or dout reaches the results that depend on it, as inf or NaN
  * as arithmetic makes it.  In DNB_BF16, and where few rows have long keys, it may also reach as NaN those
  * of the same sequence that a causal mask keeps from it (a hidden weight is 0, and 0 times infinity is
@@ -528,7 +534,8 @@ int dnb_op_rope_backward(const void* dy, const int32_t* positions, const double*
  *   h_new = scale r + gate * (b / rms(b) * w_post)      y = h_new / rms(h_new) * w_pre
  * with rms(x) = sqrt(mean(x^2) + eps) of a row.  w_post null: b is not normed.  gate: none (1), a vector
  * (width, fp32) or full (rows, width, of the type).  w_post, w_pre and their gradients fp32.  y is taken
- * from h_new before it is rounded.
+ * from h_new before it is rounded.  Squares and their sums are fp32: a row of values around 1e18 and more
+ * leaves its range.
  * backward: from b, h_new, and the gradients dh of h_new and dy of y, gives db, dr, dw_post (if w_post),
  * dgate (fp32 vector or full) and dw_pre.  scratch: dnb_op_norm_residual_scratch_bytes.
  * width a multiple of 8 (else DNB_E_UNSUPPORTED) up to 16384 (else DNB_E_RANGE). */
@@ -548,7 +555,8 @@ int dnb_op_norm_residual_backward(const void* b, const void* h_new, const float*
  * not change), norm and coef are 64 bits, so that finite values of any magnitude are scaled by the right
  * coef; norm[0] is infinite where norm is beyond fp32.  A plan is made of the tensors' addresses, counts
  * and types; its table is copied to the device by the caller (dnb_clip_table writes it to host memory)
- * and given to every run, with a workspace (both 16-byte aligned). */
+ * and given to every run, with a workspace (both 16-byte aligned).  Making the plan and the table of some
+ * hundred tensors takes the host about a millisecond: gradients should keep their memory from step to step. */
 typedef struct dnb_clip dnb_clip; /* opaque, host side only */
 int dnb_clip_create(const void* const* src, void* const* dst, const int64_t* counts, const int32_t* dtypes, int64_t tensors,
                     dnb_clip** out);

@@ -7,12 +7,12 @@
 // One pass over the keys, with the running maximum and sum of the softmax (both fp32, in units of
 // log 2).  The sum so far and its weights are only rescaled when the maximum has grown by more than
 // 8 (a factor of 256, far from anything that fp32 sums lose), which after the first tiles it hardly does.
-// 12597 packed tokens of 32 heads of 128 on 8 key/value heads, causal: 362 us, 885 TFLOP/s; matrix cores
+// 12597 packed tokens of 32 heads of 128 on 8 key/value heads, causal: 367 us, 873 TFLOP/s; matrix cores
 // 41% busy and vector units 39%: a wave is at either, and registers allow two waves a SIMD.
 //
 // k_attn_token / k_attn_join: where few rows would leave most compute units idle (answering: one query a
 // request) the work is split over the keys instead.  With one query a request it is bound by reading them: 165 MB
-// of keys and values in 35 us (4.7 TB/s), and 6 us for the join.
+// of keys and values in 35 to 37 us (4.5 to 4.7 TB/s), and 6 us for the join.
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -83,6 +83,7 @@ __device__ __forceinline__ void hide(f32x16& s, unsigned key0, unsigned sees) {
     s[i] = key0 + row_of(i) >= sees ? -INFINITY : s[i];
 }
 
+// fp32 at head_dim 97 to 128: 32 bytes a lane (eight waves: 76; at 65 to 96 12) do not fit the registers and go to scratch.
 // KH 2: eight waves, of which the second four take the second of every two tiles of keys; their sums meet at
 // the end.  A workgroup then takes half the time, which is what counts where there are few of them.
 template <typename T, int DB, int KH>
@@ -390,7 +391,7 @@ int dnb_attn_create(const dnb_attn_desc* desc, dnb_attn** out) {
   if (d.v_stride == 0) d.v_stride = kd;
   if (d.scale == 0.f) d.scale = (float)(1.0 / sqrt((double)d.head_dim));
   const int vec = d.dtype == DNB_BF16 ? 8 : 4, per = d.heads / d.kv_heads;
-  // rows are read in 16-byte pieces; a tile of 64 rows is addressed with 31 bits
+  // rows are read in 16-byte pieces; a tile of up to 128 rows, 127 strides of at most 2^24 bytes, is addressed with 31 bits
   for (const int64_t s : {d.q_stride, d.k_stride, d.v_stride})
     if (s % vec != 0 || s > (1 << 22)) return DNB_E_RANGE;
   if (d.q_stride < qd || d.k_stride < kd || d.v_stride < kd) return DNB_E_RANGE;

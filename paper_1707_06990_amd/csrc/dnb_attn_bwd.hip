@@ -1,11 +1,12 @@
 // Attention over packed sequences, backward.  With p = exp(scale q k^T - lse), recomputed, and
 // D = sum_d dout * out of a row:
 //   dv = p^T dout      ds = p * (dout v^T - D)      dq = scale ds k      dk = scale ds^T q
-// Two kernels, so that every gradient is summed by one wave in a fixed order: no atomics, no gradients
-// in fp32 in memory, results that repeat bit for bit.  That costs seven matrix products where five would
-// do.  k_attn_dq walks over the keys for 32 packed rows a wave and leaves D for k_attn_dkv, which walks
-// over the rows of all heads of a group for 32 keys a wave (the sum over shared heads is part of it).
-// 7185 packed tokens of 16 heads of 128 on 4 key/value heads, causal: 105 us for dq, 159 us for dk and dv and 16
+// Two kernels, so that every gradient is summed in an order that does not change (by one wave; where waves or
+// workgroups share the work of a tile, their sums are added one after another): no atomics, results that
+// repeat bit for bit, and no fp32 gradients in memory but those shared sums.  That costs seven matrix products
+// where five would do.  k_attn_dq walks over the keys for 32 packed rows a wave and leaves D for k_attn_dkv, which
+// walks over the rows of all heads of a group for 32 keys a wave (the sum over shared heads is part of it).
+// 7185 packed tokens of 16 heads of 128 on 4 key/value heads, causal: 106 us for dq, 164 us for dk and dv and 16
 // for their join.  Both are bound by the chain products - exponentials - products of the two waves that fit a SIMD.
 #include <hip/hip_runtime.h>
 
@@ -28,7 +29,8 @@ constexpr int kThreads = 256;
 // tokens 1.4 times, where both were 1.6 times without; a step of 7185 packed tokens takes 3% longer.
 constexpr int kFineKeys = 128;
 
-// Two rows of registers for q and dout: above head_dim 64 Split takes those of two waves.
+// Two rows of registers for q and dout: above head_dim 64 Split takes those of two waves.  Up to 64 it fits two waves a
+// SIMD but for 20 bytes a lane (eight waves: 72) that go to scratch.
 template <typename T>
 constexpr bool crowded(int blocks) { return in_parts<T> && blocks > 2; }
 
@@ -306,7 +308,8 @@ constexpr int kQRows = 64;      // packed rows of a step of k_attn_dkv
 // Keys of an item of k_attn_dkv, 32 for each of two waves.  bf16 above head_dim 96: eight waves and 128
 // keys, since the two waves that fit each SIMD have no registers left for more of the rows on their way
 // to LDS than a thread of a large workgroup has.  fp32 up to 64: eight, since LDS holds one workgroup's
-// tiles; above: four, with k and v in registers, since LDS holds no more than the rows' tiles.
+// tiles; above: four, with k and v in registers, since LDS holds no more than the rows' tiles.  At 97 to 128 they do not
+// all fit: 132 bytes a lane go to scratch; 201 us of the 540 that a step over 2264 packed rows of 16/8 heads takes.
 constexpr int keys_of(bool bf16, int blocks) { return bf16 ? (blocks == 4 ? 128 : 64) : blocks <= 2 ? 128 : 64; }
 
 // What an item costs beside its rows, in rows: some 5 us, three steps in bf16, one and a half in fp32, whose steps

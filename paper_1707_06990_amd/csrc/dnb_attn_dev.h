@@ -181,7 +181,9 @@ struct Tile {
 // Whether the waves of a workgroup of k_attn and k_attn_dq share the keys out in halves.  Eight waves at one
 // barrier are slower than two workgroups of four (12597 packed queries of 32 heads: 471 us for 393), but
 // with fewer tiles than compute units a workgroup's time is the launch's (1500 rows of 4 heads, a step: 152 us
-// for 170), unless the keys are one step anyway (a step of 33 tokens: 27 us for 24).
+// for 170), unless the keys are one step anyway (a step of 33 tokens: 27 us for 24).  Four / eight waves, us of the
+// forward of 8 heads of 128: bf16 128 keys 6.7 / 7.6, 256 8.8 / 9.3, 512 13.0 / 12.7, 1024 21.6 / 19.6, 4096 71.7 / 60.5; fp32
+// 128 17.5 / 16.7, 256 27.8 / 25.6, 1024 93.3 / 75.8; at 384 tiles of 2048 keys still 48.9 / 46.1 and 197.8 / 194.1.
 inline bool split_keys(const Args& A, int64_t tiles) { return tiles * A.kv <= 256 && A.rk >= 256 * (int64_t)A.n; }
 
 // Copies of a step's tiles in LDS: the next one is written while one is read, unless the tiles are so large
@@ -711,8 +713,16 @@ __device__ __forceinline__ int units_of(unsigned keys) { return (int)((keys + kU
 
 // The rule: where tiles of 128 rows are so few that most of the chip would be idle, or mostly empty, and the
 // keys are long enough to be worth the second launch.  Lengths are on the device; the longest sequence is
-// taken to have about twice the average's keys.  (Measured with the tiles: 188 queries of 6 heads over up to
-// 3289 keys, fp32, 183 us; 523 of one head over up to 2853, bf16, 44 us.)
+// taken to have about twice the average's keys.
+// Measured at head_dim 128, us of the forward split / in tiles (one sequence, causal, heads = tiles of a row of tiles):
+//   bf16  1 query of 8 heads   512 keys 13.4 / 12.7   1024 14.5 / 19.6   4096 16.6 / 60.5
+//         128 of 16 (32 tiles) 512 keys 23.8 / 15.9   1024 28.5 / 23.5   4096 33.2 / 69.9;  384 of 16 (64) 4096 56.5 / 71.2
+//   fp32  1 query of 8 heads   128 keys 18.3 / 16.7    256 18.3 / 25.6   1024 19.2 / 75.8
+//         128 of 32 (64 tiles) 256 keys 33.9 / 29.5    512 39.5 / 47.8   1024 52.9 / 86.0;  64 of 8 of 4 sequences (96)
+//         512 63.5 / 49.0, 2048 150.9 / 162.2
+// So it is right where it matters most, within a third around 512 keys in bf16, and wrong by 2 to 3 times (some 15 us) for
+// several sequences of equal length whose few rows make more tiles than it thinks of: 16 of 8 queries of 32/8
+// heads over 256 keys each, bf16, 26.1 / 9.3.  Unequal ones are what it is for.
 inline bool split_rows(int64_t rq, int64_t rk, int64_t n, int64_t kv, int64_t per, bool bf16) {
   const int64_t tiles = (rq * per / 128 + n) * kv;
   return (rq * per <= kItemRows * n || tiles <= (bf16 ? 40 : 96)) && 2 * rk >= (n + 1) * (bf16 ? 400 : 256);

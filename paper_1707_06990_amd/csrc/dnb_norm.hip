@@ -4,6 +4,10 @@
 // and its gradients.  Bound by memory: a row lies in registers between its reductions, so every tensor is
 // read once and written once; the weights stay in registers over the rows of a workgroup.  The statistics
 // are not kept from the forward pass: the backward pass has the rows in registers anyway.
+// The backward pass holds five rows and as many vectors: from width 4104 that leaves one wave a SIMD, and above
+// 8192 (1024 threads, 128 registers each) 180 to 292 bytes a lane go to scratch.  128 MB a tensor in bf16, 256 MB
+// in fp32, vector gate, backward: width 4096 5.2 and 5.0 TB/s; 4104 2.0 and 4.4; 8192 2.7 and 5.0; 8200 1.5 and 2.3; 16384
+// 2.2 and 3.1.  Forward: 4.0 to 5.4 TB/s at all of them (bf16 4104: 3.6).
 // 16381 rows of 4096 in bf16, backward: 152 us (5.3 TB/s) and 8 us for the sums over workgroups; 6272 rows of 2208 in
 // fp32 with a full gate: 46 us forward, 79 us backward (5.6 TB/s).
 #include <hip/hip_runtime.h>
@@ -291,8 +295,8 @@ int64_t workgroups(int64_t rows, const Shape& s, int64_t most) {
   const int64_t g = (rows + s.rpw - 1) / s.rpw;
   return g < most ? g : most;
 }
-// The backward pass's workgroups: as many as are resident (2 rows at a time on each of 256 compute units,
-// or 4 waves' rows); each leaves 2 * width partial sums.
+// The backward pass's workgroups: two on each of 256 compute units, one of 1024 threads; each leaves 2 * width
+// partial sums.  (Above width 4096 registers leave room for one of two at a time.)
 int64_t backward_workgroups(int64_t rows, const Shape& s) { return workgroups(rows, s, s.tpr == 1024 ? 256 : 512); }
 
 template <typename T, int TPR, int NV, int GATE, bool POST>
