@@ -154,3 +154,33 @@ def test_no_workspace_is_refused(dnb):
         dnb.dnb_attn_backward(plan, None, k, k, None, None, None, off, off, None, None, torch.empty_like(k), torch.empty_like(k), None)
     assert e.value.status == dnb.DNB_E_NULL
     dnb.dnb_attn_destroy(plan)
+
+
+@pytest.mark.parametrize("dim", [8, 64, 96, 128])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_every_size_of_head(dnb, dtype, dim):
+    """Key items of 64 and of 128 keys, in both types, and the split form's registers at every block count."""
+    q, k = lengths(390, dim, 30, 40)
+    p = Problem(dnb, dtype, q, k, 2, 1, dim, True)
+    attn_forms.check(dnb, p, "four")
+    p.check_forward()
+    p.check_backward()
+    p.close()
+    q, k = lengths(140, dim, 3, 350, none=0.05)
+    p = Problem(dnb, dtype, q, k, 4, 2, dim, True, capacity=[x + 130 for x in k])
+    attn_forms.check(dnb, p, "split")
+    p.check_forward()
+    p.check_backward()
+    p.close()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_tiles_of_eight_waves(dnb, dtype):
+    """Enough sequences for an index in the backward pass, and few enough tiles for eight waves."""
+    r = np.random.default_rng(4)
+    q, k = [int(x) for x in r.integers(0, 68, 195)], [int(x) for x in r.integers(0, 540, 195)]
+    p = Problem(dnb, dtype, q, k, 1, 1, 32, True)
+    attn_forms.check(dnb, p, "eight")
+    p.check_forward()
+    p.check_backward()
+    p.close()
