@@ -534,8 +534,8 @@ int dnb_op_rope_backward(const void* dy, const int32_t* positions, const double*
  *   h_new = scale r + gate * (b / rms(b) * w_post)      y = h_new / rms(h_new) * w_pre
  * with rms(x) = sqrt(mean(x^2) + eps) of a row.  w_post null: b is not normed.  gate: none (1), a vector
  * (width, fp32) or full (rows, width, of the type).  w_post, w_pre and their gradients fp32.  y is taken
- * from h_new before it is rounded.  Squares and their sums are fp32: a row of values around 1e18 and more
- * leaves its range.
+ * from h_new before it is rounded.  Squares and their sums are fp32: rows of values from 1e17 (at width
+ * 16384) or 6e18 (at 8) on leave its range.
  * backward: from b, h_new, and the gradients dh of h_new and dy of y, gives db, dr, dw_post (if w_post),
  * dgate (fp32 vector or full) and dw_pre.  scratch: dnb_op_norm_residual_scratch_bytes.
  * width a multiple of 8 (else DNB_E_UNSUPPORTED) up to 16384 (else DNB_E_RANGE). */
