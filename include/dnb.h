@@ -566,6 +566,120 @@ int dnb_clip_table(const dnb_clip* plan, void* host);
 size_t dnb_clip_workspace_bytes(const dnb_clip* plan);
 int dnb_clip_run(const dnb_clip* plan, const void* table, float max_norm, float* norm, void* workspace, void* stream);
 
+/* ------------------------------------------------------------------------------------------
+ * A decoder's paged cache: what fills it, what reads it, what moves its pages.  Types, pointers, streams and errors as for
+ * the sequence operators above; no call allocates device memory, copies to the host or synchronises (dnb_pages_* work on
+ * host memory alone), and all that take a stream may be captured into a graph.
+ *
+ * Keys (or values) of all sequences lie in a pool of pages of page_size tokens.  Token j of sequence s is row j % page_size
+ * of page table[s][j / page_size]; row r of page p, head g is at p * page_stride + r * row_stride + g * head_stride
+ * elements.  (Tokens first: row_stride kv_heads * head_dim, head_stride head_dim, which is what 0 for all three means.
+ * Heads first: head_stride page_size * row_stride, row_stride head_dim.  A page_stride of two pages lets keys and values
+ * lie by turns.)  Keys and values have the same layout.
+ *   table      (sequences, max_pages) int32 on the device; entries past a sequence's length are not read
+ *   k_lengths  `sequences` int32 on the device: tokens that each has in the cache, those of this call among them
+ *   q_offsets  sequences + 1 int32 on the device, not decreasing: sequence s has the rows q_offsets[s] .. q_offsets[s+1] - 1
+ *              of what is new, its last tokens; none is allowed
+ * Whatever these hold, nothing outside the tensors is read or written: offsets are cut to the rows, lengths to the table's
+ * width; a page that is not of the pool is read as zeros, and nothing is written to it. */
+typedef struct {
+  int64_t pages;         /* of the pool                                                           */
+  int32_t page_size;     /* a power of two up to 65536 (else DNB_E_UNSUPPORTED)                   */
+  int32_t kv_heads;
+  int32_t head_dim;      /* a multiple of 8 up to 128 (else DNB_E_UNSUPPORTED)                    */
+  int32_t sequences;     /* 1 to 2^20                                                             */
+  int32_t max_pages;     /* columns of the table; max_pages * page_size below 2^31                */
+  int32_t dtype;         /* DNB_F32 | DNB_BF16                                                    */
+  int64_t page_stride, row_stride, head_stride; /* multiples of 16 bytes, at most 2^30 elements   */
+} dnb_paged_layout;
+
+/* Attention of new tokens over a paged cache: one new token a request, chunks of prompts and whole prompts, in one batch.
+ * For sequence s, head h and query i of nq, with nk = k_lengths[s] keys,
+ *   out_i = sum_j softmax_j(scale q_i . k_j) v_j        lse_i = log sum_j exp(scale q_i . k_j)
+ * over all j, or with `causal` over j <= i + nk - nq (the last query sees the last key).  Head h reads key/value head
+ * h / (heads / kv_heads).  A query that sees no key has out 0 and lse -inf.  Rows of no sequence are neither read nor written.
+ *   q, out (rows_q, heads, head_dim) of the type, out dense; lse (heads, rows_q) fp32, or null.
+ * Roundings, and infinities and NaN in what is seen, as for dnb_attn_forward.  In DNB_BF16 infinities and NaN in values that a causal mask
+ * hides from a query may reach it as NaN, as there; what lies past a sequence's length never does.
+ * Workspace: 16-byte aligned; nothing in it lasts from one call to the next. */
+typedef struct dnb_paged_attn dnb_paged_attn; /* opaque, host side only */
+typedef struct {
+  dnb_paged_layout cache;
+  int32_t heads;         /* a multiple of cache.kv_heads                       */
+  int32_t causal;
+  int64_t rows_q;        /* rows of q and out; 0 is allowed                    */
+  int64_t q_stride;      /* elements between rows of q; 0: dense.  A multiple of 16 bytes, at most 2^22 */
+  float scale;           /* 0: 1 / sqrt(head_dim)                              */
+} dnb_paged_attn_desc;
+int dnb_paged_attn_create(const dnb_paged_attn_desc* desc, dnb_paged_attn** out);
+void dnb_paged_attn_destroy(dnb_paged_attn* plan);
+size_t dnb_paged_attn_workspace_bytes(const dnb_paged_attn* plan);
+int dnb_paged_attn_forward(const dnb_paged_attn* plan, const void* q, const void* k_pages, const void* v_pages, const int32_t* q_offsets,
+                           const int32_t* k_lengths, const int32_t* table, void* out, float* lse, void* workspace, void* stream);
+
+/* Queries and keys of a block, before the attention: every head's norm and its rotation in one pass,
+ *   n = x / sqrt(mean(x^2) + eps) * w        y = n turned as by dnb_op_rope_forward (turns, positions, order, factor)
+ * w_q, w_k (head_dim fp32; any may be null: those heads are not normed).  rotary_dim 0: nothing is turned (turns and positions may be null).
+ * backward: from q and k as they were, the gradients of both outputs, gives dq, dk, dw_q (if w_q) and dw_k (if w_k); sums
+ * over rows in an order that does not change.  scratch: dnb_op_qk_rope_scratch_bytes, 16-byte aligned.
+ * An output may be its own input's memory (y of x, dx of dy, with equal strides). */
+typedef struct {
+  int64_t rows;
+  int32_t q_heads, k_heads;   /* 0 to 4096, not both 0                                                     */
+  int32_t head_dim;           /* even, up to 256 (else DNB_E_UNSUPPORTED)                                  */
+  int32_t rotary_dim, order;  /* even, up to head_dim; DNB_ROPE_*                                          */
+  int32_t dtype;
+  float eps, factor;
+  int64_t q_stride, k_stride, v_stride;  /* elements between rows of q and dq, k and dk, v; even, 0: dense   */
+  int64_t q_out_stride, k_out_stride;    /* ... of q_out and dq_out, k_out and dk_out                      */
+} dnb_qk_layout;
+int dnb_op_qk_rope_forward(const dnb_qk_layout* qk, const void* q, const void* k, const float* w_q, const float* w_k,
+                           const int32_t* positions, const double* turns, void* q_out, void* k_out, void* stream);
+size_t dnb_op_qk_rope_scratch_bytes(const dnb_qk_layout* qk);
+int dnb_op_qk_rope_backward(const dnb_qk_layout* qk, const void* q, const void* k, const float* w_q, const float* w_k,
+                            const int32_t* positions, const double* turns, const void* dq_out, const void* dk_out, void* dq,
+                            void* dk, float* dw_q, float* dw_k, void* scratch, void* stream);
+
+/* The same pass for new tokens of requests: q_out as above, and each row's keys (normed and turned) and values (as they are)
+ * go to the token's place in the cache, which for row i of nq of sequence s is token k_lengths[s] - nq + i.  positions null: that is its
+ * position too.  (Rows whose token would lie before the first or past the table write no key and value; of no sequence: nothing.)
+ * q, k, v: rows of the type, k and v of k_heads == cache->kv_heads heads; dtype and head_dim are cache's.  Pages that are
+ * written must be one sequence's own (dnb_pages_extend sees to that). */
+int dnb_op_paged_append(const dnb_qk_layout* qk, const dnb_paged_layout* cache, const void* q, const void* k, const void* v,
+                        const float* w_q, const float* w_k, const int32_t* positions, const double* turns, const int32_t* q_offsets,
+                        const int32_t* k_lengths, const int32_t* table, void* q_out, void* k_pages, void* v_pages, void* stream);
+
+/* Copies pages: for each of `count` pairs (source, target) of int32 on the device and each plane (the keys or values of a
+ * layer), page `target` becomes what page `source` is.  Page p of plane i is page_bytes bytes at
+ * pool + i * plane_stride + p * page_bytes; all multiples of 16.  A pair with a page outside the pool, or twice the same,
+ * does nothing (so a list may be filled up with -1).  No target may be another pair's source or target: what is in it then
+ * is undefined.  Lists of dnb_pages_copies are so. */
+int dnb_op_paged_copy(void* pool, int64_t pages, int64_t page_bytes, int64_t planes, int64_t plane_stride, const int32_t* pairs,
+                      int64_t count, void* stream);
+
+/* Who has which pages, on the host: every page is counted by the sequences that have it.  One thread at a time.
+ *   extend    gives sequence `s` room for `tokens` more.  A last page that is not full and is shared is replaced by a copy.
+ *             DNB_E_NOMEM: not that many free pages; nothing has changed then.
+ *   fork      sequence `to`, which must be empty, gets what `from` has: the same pages.
+ *   truncate  leaves the first `length` tokens; 0 frees the sequence.
+ *   compact   moves the pages in use to the lowest numbers.  Pages whose content a copy that has not been taken yet needs
+ *             stay: taken, a second call moves on.
+ *   copies    takes the copies that extend and compact have asked for since the last call, as pairs for dnb_op_paged_copy (in
+ *             one call, before anything new is written to the pages).  *count: how many there are; DNB_E_RANGE if they are
+ *             more than `capacity`, and they stay.  pairs null with capacity 0: how many there are.
+ *   table     writes (sequences, max_pages) entries, -1 past a sequence's pages, and the lengths.  Either may be null.
+ * DNB_E_RANGE: a sequence that is none, a length beyond the table.  DNB_E_BADDESC: a `to` that is not empty. */
+typedef struct dnb_pages dnb_pages; /* opaque, host side only */
+int dnb_pages_create(int64_t pages, int32_t page_size, int32_t sequences, int32_t max_pages, dnb_pages** out);
+void dnb_pages_destroy(dnb_pages* p);
+int dnb_pages_extend(dnb_pages* p, int32_t s, int64_t tokens);
+int dnb_pages_fork(dnb_pages* p, int32_t from, int32_t to);
+int dnb_pages_truncate(dnb_pages* p, int32_t s, int64_t length);
+int dnb_pages_compact(dnb_pages* p);
+int64_t dnb_pages_free_count(const dnb_pages* p); /* pages that no sequence has and no copy needs */
+int dnb_pages_copies(dnb_pages* p, int32_t* pairs, int64_t capacity, int64_t* count);
+int dnb_pages_table(const dnb_pages* p, int32_t* table, int32_t* k_lengths);
+
 #ifdef __cplusplus
 }
 #endif

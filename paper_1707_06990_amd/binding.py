@@ -46,6 +46,34 @@ class dnb_attn_desc(C.Structure):
                 ("v_stride", C.c_int64), ("dtype", C.c_int32), ("causal", C.c_int32), ("scale", C.c_float)]
 
 
+class dnb_paged_layout(C.Structure):
+    """A paged cache; strides of 0: tokens first, dense."""
+    _fields_ = [("pages", C.c_int64), ("page_size", C.c_int32), ("kv_heads", C.c_int32), ("head_dim", C.c_int32),
+                ("sequences", C.c_int32), ("max_pages", C.c_int32), ("dtype", C.c_int32), ("page_stride", C.c_int64),
+                ("row_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+    def __init__(self, pages, page_size, kv_heads, head_dim, sequences, max_pages, dtype=DNB_BF16, page_stride=0, row_stride=0,
+                 head_stride=0):
+        super().__init__(pages, page_size, kv_heads, head_dim, sequences, max_pages, dtype, page_stride, row_stride, head_stride)
+
+
+class dnb_paged_attn_desc(C.Structure):
+    _fields_ = [("cache", dnb_paged_layout), ("heads", C.c_int32), ("causal", C.c_int32), ("rows_q", C.c_int64),
+                ("q_stride", C.c_int64), ("scale", C.c_float)]
+
+
+class dnb_qk_layout(C.Structure):
+    """Queries and keys whose heads are normed and turned; strides of 0: dense."""
+    _fields_ = [("rows", C.c_int64), ("q_heads", C.c_int32), ("k_heads", C.c_int32), ("head_dim", C.c_int32), ("rotary_dim", C.c_int32),
+                ("order", C.c_int32), ("dtype", C.c_int32), ("eps", C.c_float), ("factor", C.c_float), ("q_stride", C.c_int64),
+                ("k_stride", C.c_int64), ("v_stride", C.c_int64), ("q_out_stride", C.c_int64), ("k_out_stride", C.c_int64)]
+
+    def __init__(self, rows, q_heads, k_heads, head_dim, rotary_dim, order=DNB_ROPE_HALF, dtype=DNB_BF16, eps=1e-6, factor=1.0,
+                 q_stride=0, k_stride=0, v_stride=0, q_out_stride=0, k_out_stride=0):
+        super().__init__(rows, q_heads, k_heads, head_dim, rotary_dim, order, dtype, eps, factor, q_stride, k_stride, v_stride,
+                         q_out_stride, k_out_stride)
+
+
 class dnb_block_memory(C.Structure):
     _fields_ = [(n, C.c_uint64) for n in ("stored_fwd_bytes", "shared_fwd_bytes", "grad_bytes", "peak_bytes",
                                            "stats_bytes", "scratch_bytes", "workspace_bytes")]
@@ -153,6 +181,24 @@ _SIGS = {
     "dnb_clip_table": (C.c_int, [_vp, _vp]),
     "dnb_clip_workspace_bytes": (_sz, [_vp]),
     "dnb_clip_run": (C.c_int, [_vp, _vp, C.c_float, _vp, _vp, _vp]),
+    "dnb_paged_attn_create": (C.c_int, [C.POINTER(dnb_paged_attn_desc), C.POINTER(_vp)]),
+    "dnb_paged_attn_destroy": (None, [_vp]),
+    "dnb_paged_attn_workspace_bytes": (_sz, [_vp]),
+    "dnb_paged_attn_forward": (C.c_int, [_vp] * 11),
+    "dnb_op_qk_rope_forward": (C.c_int, [C.POINTER(dnb_qk_layout)] + [_vp] * 9),
+    "dnb_op_qk_rope_scratch_bytes": (_sz, [C.POINTER(dnb_qk_layout)]),
+    "dnb_op_qk_rope_backward": (C.c_int, [C.POINTER(dnb_qk_layout)] + [_vp] * 14),
+    "dnb_op_paged_append": (C.c_int, [C.POINTER(dnb_qk_layout), C.POINTER(dnb_paged_layout)] + [_vp] * 14),
+    "dnb_op_paged_copy": (C.c_int, [_vp, _i64, _i64, _i64, _i64, _vp, _i64, _vp]),
+    "dnb_pages_create": (C.c_int, [_i64, C.c_int32, C.c_int32, C.c_int32, C.POINTER(_vp)]),
+    "dnb_pages_destroy": (None, [_vp]),
+    "dnb_pages_extend": (C.c_int, [_vp, C.c_int32, _i64]),
+    "dnb_pages_fork": (C.c_int, [_vp, C.c_int32, C.c_int32]),
+    "dnb_pages_truncate": (C.c_int, [_vp, C.c_int32, _i64]),
+    "dnb_pages_compact": (C.c_int, [_vp]),
+    "dnb_pages_free_count": (_i64, [_vp]),
+    "dnb_pages_copies": (C.c_int, [_vp, _vp, _i64, C.POINTER(_i64)]),
+    "dnb_pages_table": (C.c_int, [_vp, _vp, _vp]),
 }
 for _name, (_res, _args) in _SIGS.items():
     _f = getattr(_lib, _name)
@@ -647,3 +693,101 @@ def dnb_clip_workspace_bytes(plan) -> int:
 
 def dnb_clip_run(plan, table, max_norm, norm, workspace, stream=None) -> None:
     _check(_lib.dnb_clip_run(plan, _ptr(table), max_norm, _ptr(norm), _ptr(workspace), _stream(stream)))
+
+
+# ---------------------------------------------------------------- a decoder's paged cache
+
+def dnb_paged_attn_create(cache, heads, rows_q, causal=True, scale=0.0, q_stride=0):
+    """cache: a dnb_paged_layout."""
+    desc = dnb_paged_attn_desc(cache, heads, int(bool(causal)), rows_q, q_stride, scale)
+    out = _vp()
+    _check(_lib.dnb_paged_attn_create(C.byref(desc), C.byref(out)))
+    return out
+
+
+def dnb_paged_attn_destroy(plan) -> None:
+    _lib.dnb_paged_attn_destroy(plan)
+
+
+def dnb_paged_attn_workspace_bytes(plan) -> int:
+    return int(_lib.dnb_paged_attn_workspace_bytes(plan))
+
+
+def dnb_paged_attn_forward(plan, q, k_pages, v_pages, q_offsets, k_lengths, table, out, lse, workspace, stream=None) -> None:
+    _check(_lib.dnb_paged_attn_forward(plan, _ptr(q), _ptr(k_pages), _ptr(v_pages), _ptr(q_offsets), _ptr(k_lengths), _ptr(table),
+                                       _ptr(out), _ptr(lse), _ptr(workspace), _stream(stream)))
+
+
+def dnb_op_qk_rope_forward(qk, q, k, w_q, w_k, positions, turns, q_out, k_out, stream=None) -> None:
+    """qk: a dnb_qk_layout."""
+    _check(_lib.dnb_op_qk_rope_forward(qk, _ptr(q), _ptr(k), _ptr(w_q), _ptr(w_k), _ptr(positions), _ptr(turns), _ptr(q_out),
+                                       _ptr(k_out), _stream(stream)))
+
+
+def dnb_op_qk_rope_scratch_bytes(qk) -> int:
+    return int(_lib.dnb_op_qk_rope_scratch_bytes(qk))
+
+
+def dnb_op_qk_rope_backward(qk, q, k, w_q, w_k, positions, turns, dq_out, dk_out, dq, dk, dw_q, dw_k, scratch, stream=None) -> None:
+    _check(_lib.dnb_op_qk_rope_backward(qk, _ptr(q), _ptr(k), _ptr(w_q), _ptr(w_k), _ptr(positions), _ptr(turns), _ptr(dq_out),
+                                        _ptr(dk_out), _ptr(dq), _ptr(dk), _ptr(dw_q), _ptr(dw_k), _ptr(scratch), _stream(stream)))
+
+
+def dnb_op_paged_append(qk, cache, q, k, v, w_q, w_k, positions, turns, q_offsets, k_lengths, table, q_out, k_pages, v_pages,
+                        stream=None) -> None:
+    _check(_lib.dnb_op_paged_append(qk, cache, _ptr(q), _ptr(k), _ptr(v), _ptr(w_q), _ptr(w_k), _ptr(positions), _ptr(turns),
+                                    _ptr(q_offsets), _ptr(k_lengths), _ptr(table), _ptr(q_out), _ptr(k_pages), _ptr(v_pages),
+                                    _stream(stream)))
+
+
+def dnb_op_paged_copy(pool, pages, page_bytes, planes, plane_stride, pairs, count, stream=None) -> None:
+    _check(_lib.dnb_op_paged_copy(_ptr(pool), pages, page_bytes, planes, plane_stride, _ptr(pairs), count, _stream(stream)))
+
+
+def dnb_pages_create(pages, page_size, sequences, max_pages):
+    out = _vp()
+    _check(_lib.dnb_pages_create(pages, page_size, sequences, max_pages, C.byref(out)))
+    return out
+
+
+def dnb_pages_destroy(p) -> None:
+    _lib.dnb_pages_destroy(p)
+
+
+def dnb_pages_extend(p, s, tokens) -> None:
+    _check(_lib.dnb_pages_extend(p, s, tokens))
+
+
+def dnb_pages_fork(p, source, to) -> None:
+    _check(_lib.dnb_pages_fork(p, source, to))
+
+
+def dnb_pages_truncate(p, s, length) -> None:
+    _check(_lib.dnb_pages_truncate(p, s, length))
+
+
+def dnb_pages_compact(p) -> None:
+    _check(_lib.dnb_pages_compact(p))
+
+
+def dnb_pages_free_count(p) -> int:
+    return int(_lib.dnb_pages_free_count(p))
+
+
+def dnb_pages_copies(p):
+    """The copies asked for since the last call, as a numpy array of (source, target) rows, to be copied to the device."""
+    import numpy as np
+    n = _i64()
+    _check(_lib.dnb_pages_copies(p, None, 0, C.byref(n)))
+    pairs = np.empty((n.value, 2), dtype=np.int32)
+    if n.value:
+        _check(_lib.dnb_pages_copies(p, pairs.ctypes.data, n.value, C.byref(n)))
+    return pairs
+
+
+def dnb_pages_table(p, sequences, max_pages):
+    """(table, lengths) as numpy arrays of int32, to be copied to the device; the sizes are those that p was made with."""
+    import numpy as np
+    table, lengths = np.empty((sequences, max_pages), dtype=np.int32), np.empty(sequences, dtype=np.int32)
+    _check(_lib.dnb_pages_table(p, table.ctypes.data, lengths.ctypes.data))
+    return table, lengths

@@ -555,6 +555,61 @@ __device__ __forceinline__ bool any_wave(lds_t at, bool v) {
   return __builtin_amdgcn_readfirstlane(any) != 0;
 }
 
+// The state of 32 rows: O^T, running maximum (log2 units of the scaled scores) and this half's sum.
+template <int DB>
+struct Online {
+  f32x16 o[DB];
+  float m, l;
+  __device__ __forceinline__ void init() {
+#pragma unroll
+    for (int i = 0; i < DB; ++i) o[i] = (f32x16){};
+    m = -INFINITY;
+    l = 0.f;
+  }
+};
+
+// One more set of N blocks of 32 keys: scores s (scaled by c inside), values from `vt`.
+template <typename T, int DB, int N, bool HOLD, int TR>
+__device__ __forceinline__ void online_step(Online<DB>& S, f32x16 (&s)[N], float c, lds_t vt, int row0) {
+  float mx = -INFINITY;
+#pragma unroll
+  for (int b = 0; b < N; ++b)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) mx = fmaxf(mx, s[b][i]);
+  // c > 0: the scaled maximum is the maximum scaled
+  mx = half_max(mx) * c;
+  if (__any(mx > S.m + 8.f || (S.m == -INFINITY && mx > -INFINITY))) {
+    const float m = fmaxf(S.m, mx);
+    const float a = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(S.m - m);
+    S.m = m;
+    S.l *= a;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) S.o[db][i] *= a;
+  }
+  const float m = S.m == -INFINITY ? 0.f : S.m;  // nothing seen yet: exp2(-inf - 0) = 0
+#pragma unroll
+  for (int b = 0; b < N; ++b) {
+    float t = 0.f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      s[b][i] = __builtin_amdgcn_exp2f(fmaf(s[b][i], c, -m));
+      t += s[b][i];
+    }
+    S.l += t;
+  }
+#pragma unroll
+  for (int b = 0; b < N; ++b) col_mul<T, DB, HOLD, TR>(vt, row0 + 32 * b, s[b], S.o);
+}
+
+// Scores of keys key0 + row_of(i) that a query which sees keys below `sees` does not see
+__device__ __forceinline__ void hide(f32x16& s, unsigned key0, unsigned sees) {
+#pragma unroll
+  for (int i = 0; i < 16; ++i)
+    s[i] = key0 + row_of(i) >= sees ? -INFINITY : s[i];
+}
+
 // One sequence, as its offsets say; whatever they hold, the rows stay inside the tensors.  nk may be 2^31 - 1:
 // positions of keys, which go up to a tile further, are unsigned.
 struct Seq {

@@ -1,0 +1,496 @@
+// Attention of new tokens over a paged cache: softmax(scale q k^T) v for each sequence and head, the queries being a sequence's
+// last tokens and the keys rows of pages that a table names.
+//
+// As in dnb_attn.hip the `per` query heads of a key/value head are rows of one matrix (packed row m is query m / per, head
+// m % per of the group).  A workgroup of four waves takes a block of packed rows of one key/value head and walks over its keys
+// in steps of KT.  A wave holds 32 rows: with many rows the four have 32 each and share all keys, with
+// few they share the rows and each step's keys (KH waves to a set of rows).
+// Batches mix single tokens over long caches with chunks of prompts, and only the device knows which: all (block, step)
+// units lie on one line, in units of their cost, which is cut into equal parts, one a workgroup.  A block that several
+// workgroups share leaves its sums, not yet divided, in the workspace, and k_paged_join adds them.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <new>
+#include <type_traits>
+
+#include "dnb_attn_dev.h"
+#include "dnb_paged.h"
+
+namespace dnb {
+namespace attn {
+namespace {
+
+constexpr int kThreads = 256;
+
+// A block that workgroups share, as its first one leaves it for the join; parts 0: none.
+struct Shared {
+  int q0, m0, rows, g, parts;
+};
+
+struct PArgs {
+  const void *q, *k, *v;
+  void* o;
+  float *lse, *part;
+  Shared* shared;
+  const int32_t *qo, *lens, *table;
+  int n, heads, kv, per, d, causal, columns, shift, W;
+  int64_t pages, rq, qs, ps, rs, hs;
+  float c;  // scale * log2(e)
+};
+
+// 16 bytes of the tensors' zeros, twice: where rows that are not there are read
+__device__ __attribute__((aligned(32))) const float kZeros[8] = {};
+
+struct PSeq {
+  int q0, nq, nk;
+};
+__device__ __forceinline__ PSeq pseq_at(const PArgs& A, int i) {
+  PSeq s;
+  const int64_t q0 = min(max((int64_t)A.qo[i], (int64_t)0), A.rq), q1 = min(max((int64_t)A.qo[i + 1], q0), A.rq);
+  s.q0 = (int)q0;
+  s.nq = (int)(q1 - q0);
+  s.nk = (int)min((int64_t)max(A.lens[i], 0), (int64_t)A.columns << A.shift);
+  return s;
+}
+__device__ __forceinline__ unsigned pseen(const PArgs& A, const PSeq& S, int m) {
+  return A.causal ? max(S.nk + min(m / A.per + 1 - S.nq, 0), 0) : S.nk;
+}
+
+// Blocks of a sequence: RW of the four waves take 32 * NC rows each.  Cost: of a step, in units of the line.
+template <int KT, int NC>
+struct Blocks {
+  int rw, rows, count, cost, M;
+  __device__ __forceinline__ Blocks(const PArgs& A, const PSeq& S) {
+    M = S.nq * A.per;
+    rw = KT >= 128 && M <= 32 * NC ? 1 : M <= 64 * NC ? 2 : 4;
+    rows = 32 * NC * rw;
+    count = (M + rows - 1) / rows;
+    cost = rw == 4 ? 4 : rw == 2 ? 3 : 2;
+  }
+  // (a block whose rows see nothing takes a step too: its results are written)
+  __device__ __forceinline__ int steps(const PArgs& A, const PSeq& S, int t) const {
+    return max((int)((pseen(A, S, min((t + 1) * rows, M) - 1) + KT - 1) / KT), 1);
+  }
+};
+// of one key/value head, by a lane alone
+template <int KT, int NC>
+__device__ __forceinline__ int64_t head_units(const PArgs& A, const PSeq& S) {
+  const Blocks<KT, NC> B(A, S);
+  int64_t u = 0;
+  if (!A.causal) return (int64_t)B.count * (B.count > 0 ? B.steps(A, S, 0) : 0) * B.cost;
+  for (int t = 0; t < B.count; ++t) u += B.steps(A, S, t);
+  return u * B.cost;
+}
+
+// Sum over the threads up to each; *total: over all.  `red`: room for four in LDS, free again after the caller's next barrier.
+__device__ __forceinline__ int64_t block_scan(int64_t v, int64_t* red, int64_t* total) {
+  const int wave = threadIdx.x >> 6;
+  int64_t s = wave_scan(v);
+  __syncthreads();
+  if (lane_id() == 63) red[wave] = s;
+  __syncthreads();
+  int64_t all = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if (i < wave) s += red[i];
+    all += red[i];
+  }
+  *total = all;
+  return s;
+}
+
+// A tile's rows on their way to LDS; rows of keys from key0 on, of which nk exist, as the table says where they lie.
+template <typename T, int DB, int ROWS>
+struct PagedStage {
+  using L = Tile<T, DB>;
+  using E = elem_t<T>;
+  static constexpr int U = ROWS * L::CH / kThreads;
+  static_assert(ROWS * L::CH % kThreads == 0, "");
+  u32x4 k[U * L::LD], v[U * L::LD];
+  __device__ __forceinline__ void load(const PArgs& A, const int32_t* table, int64_t head, int tid, unsigned key0, unsigned nk) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int i = tid + u * kThreads, row = i / L::CH, c = i - row * L::CH;
+      const unsigned key = key0 + row;
+      bool in = key < nk && c * L::EP < A.d;
+      const int page = in ? table[key >> A.shift] : -1;
+      in = page >= 0 && page < A.pages;
+      const int64_t at = page * A.ps + (int64_t)(key & ((1u << A.shift) - 1)) * A.rs + head + c * L::EP;
+      const E* kp = in ? (const E*)A.k + at : (const E*)kZeros;
+      const E* vp = in ? (const E*)A.v + at : (const E*)kZeros;
+#pragma unroll
+      for (int p = 0; p < L::LD; ++p) {
+        k[u * L::LD + p] = reinterpret_cast<const u32x4*>(kp)[p];
+        v[u * L::LD + p] = reinterpret_cast<const u32x4*>(vp)[p];
+      }
+    }
+  }
+  __device__ __forceinline__ void store(lds_t kt, lds_t vt, int tid) {
+    store_pieces<T, DB, U, kThreads, ROWS>(kt, tid, k);
+    store_pieces<T, DB, U, kThreads, ROWS>(vt, tid, v);
+  }
+};
+
+template <int DB>
+constexpr int part_floats(int rows) { return rows * (32 * DB + 2); }
+
+// Where a block's results go: the output, or a part's place.
+struct Target {
+  int q0, m0, M, g;
+  float* part;  // null: the output
+  int rows;     // of the part's place
+};
+
+// The KH waves of a set of rows join: O, m and l of waves kh > 0 through LDS (free, behind a barrier).
+template <int DB>
+__device__ __forceinline__ void join_waves(Online<DB>& R, char* shared, int wave, int KH) {
+  const int l = lane_id(), kh = wave & (KH - 1);
+  constexpr int PIECES = DB * 4 + 1;
+  f32x4* to = reinterpret_cast<f32x4*>(shared) + wave * PIECES * 64 + l;
+  if (kh > 0) {
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) to[(db * 4 + q) * 64] = (f32x4){R.o[db][4 * q], R.o[db][4 * q + 1], R.o[db][4 * q + 2], R.o[db][4 * q + 3]};
+    to[DB * 4 * 64] = (f32x4){R.m, R.l, 0.f, 0.f};
+  }
+  __syncthreads();
+  if (kh > 0) return;
+  for (int w = 1; w < KH; ++w) {
+    const f32x4* from = to + w * PIECES * 64;
+    const f32x4 ml = from[DB * 4 * 64];
+    const float m = fmaxf(R.m, ml[0]), t = m == -INFINITY ? 0.f : m;
+    const float a = __builtin_amdgcn_exp2f(R.m - t), b = __builtin_amdgcn_exp2f(ml[0] - t);
+    R.m = m;
+    R.l = R.l * a + ml[1] * b;
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const f32x4 x = from[(db * 4 + q) * 64];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) R.o[db][4 * q + k] = R.o[db][4 * q + k] * a + x[k] * b;
+      }
+  }
+}
+
+template <typename E, int DB>
+__device__ __forceinline__ void write_rows(const PArgs& A, const Target& to, const Online<DB>& R, int row0) {
+  const int l = lane_id(), r = row0 + (l & 31), m = to.m0 + r;
+  const bool valid = m < to.M;
+  const float sum = half_sum(R.l);
+  if (to.part) {
+    store_cols<float, DB>(to.part + (int64_t)r * 32 * DB, valid, 32 * DB, R.o, 1.f);
+    if (valid && l < 32) {
+      to.part[to.rows * 32 * DB + r] = R.m;
+      to.part[to.rows * (32 * DB + 1) + r] = sum;
+    }
+    return;
+  }
+  const int query = m / A.per, head = to.g * A.per + m - query * A.per;
+  const int64_t qrow = (int64_t)to.q0 + query;
+  store_cols<E, DB>((E*)A.o + (qrow * A.heads + head) * A.d, valid, A.d, R.o, sum == 0.f ? 0.f : 1.f / sum);
+  if (valid && l < 32 && A.lse) A.lse[(int64_t)head * A.rq + qrow] = sum == 0.f ? -INFINITY : (R.m + log2f(sum)) * kLn2;
+}
+
+template <typename T, int DB>
+struct Walk {
+  static constexpr int KT = 64, NC = 1;
+  using L = Tile<T, DB>;
+  using E = elem_t<T>;
+  static constexpr int TILE = KT * L::PITCH * L::PL;
+  static constexpr int JOIN = 4 * (DB * 4 + 1) * 64 * 16;
+  static constexpr int BYTES = (2 * TILE > JOIN ? 2 * TILE : JOIN) + kFlags;
+
+  // Steps first .. last - 1 of a block.
+  static __device__ __forceinline__ void run(const PArgs& A, char* shared, const PSeq& S, const int32_t* table, const Blocks<KT, NC>& B, int g,
+                                             int t, int first, int last, const Target& to) {
+    const lds_t lds = lds_start(shared);
+    const int wave = threadIdx.x >> 6, l = lane_id(), KH = 4 / B.rw, kh = wave & (KH - 1), row0 = wave / KH * 32;
+    const int m = t * B.rows + row0 + (l & 31), query = m / A.per, head = g * A.per + m - query * A.per;
+    const bool valid = m < B.M;
+    const unsigned sees = pseen(A, S, m);
+    const int m0 = t * B.rows + row0;
+    const unsigned most = m0 >= B.M ? 0 : pseen(A, S, min(m0 + 31, B.M - 1)), least = pseen(A, S, m0);
+    const unsigned all = pseen(A, S, min((t + 1) * B.rows, B.M) - 1);  // keys that the block's last row sees
+    const int blocks = KT / 32 / KH;
+    Online<DB> R;
+    auto walk = [&](auto form) {
+      using F = decltype(form);
+      Columns<F, DB> qf;
+      load_cols<F, DB>(qf, (const E*)A.q + ((int64_t)S.q0 + apart<F>(query)) * A.qs + (int64_t)apart<F>(head) * A.d, valid, A.d);
+      R.init();
+      PagedStage<F, DB, KT> stage;
+      const int tid = apart<F>((int)threadIdx.x);
+      if (!is_whole<F> && first < last) stage.load(A, table, g * A.hs, tid, first * KT, all);
+      for (int s = first; s < last; ++s) {
+        if (is_whole<F>) stage.load(A, table, g * A.hs, tid, s * KT, all);
+        __syncthreads();
+        stage.store(lds, lds + TILE, tid);
+        __syncthreads();
+        if (!is_whole<F> && s + 1 < last) stage.load(A, table, g * A.hs, tid, (s + 1) * KT, all);
+        for (int b = 0; b < blocks; ++b) {
+          const int r = (kh * blocks + b) * 32;
+          const unsigned key = (unsigned)s * KT + r;
+          if (key >= most) break;
+          f32x16 x[1] = {row_mul<F, DB, false, KT>(lds, r, qf)};
+          if (key + 32 > least) hide(x[0], key, sees);
+          online_step<F, DB, 1, false, KT>(R, x, A.c, lds + TILE, r);
+        }
+      }
+    };
+    walk(T());
+    if constexpr (L::PL == 3) {
+      __syncthreads();
+      if (any_wave<4>(lds + BYTES - kFlags, not_finite(R.o))) walk(Whole());
+    }
+    if (KH > 1) {
+      __syncthreads();
+      join_waves<DB>(R, shared, wave, KH);
+    }
+    if (kh == 0) write_rows<E, DB>(A, to, R, row0);
+  }
+};
+
+template <typename T, int DB>
+__global__ __launch_bounds__(kThreads, 1) void k_paged(PArgs A, int max_rows) {
+  using K = Walk<T, DB>;
+  constexpr int KT = K::KT, NC = K::NC;
+  using B_ = Blocks<KT, NC>;
+  extern __shared__ __attribute__((aligned(512))) char shared[];
+  int64_t* red = reinterpret_cast<int64_t*>(shared);
+  const int tid = threadIdx.x, l = lane_id();
+  int64_t mine = 0, first_units = 0, total;
+  for (int i = tid; i < A.n; i += kThreads) {
+    const int64_t u = head_units<KT, NC>(A, pseq_at(A, i)) * A.kv;
+    if (i < kThreads) first_units = u;
+    mine += u;
+  }
+  const int64_t scan = block_scan(mine, red, &total);
+  const int W = (int)min((int64_t)A.W, max(total / 4, (int64_t)1));
+  // workgroups that lie side by side on the line run on one XCD, whose cache has the keys that they share
+  const int w = A.W % 8 == 0 ? (int)(blockIdx.x % 8) * (A.W / 8) + (int)blockIdx.x / 8 : (int)blockIdx.x;
+  if (tid == 0) A.shared[w].parts = 0;
+  if (w >= W || total == 0) return;
+  const int64_t a = w * total / W, b = (w + 1) * total / W;
+  // the sequence at a, and where on the line it begins
+  int64_t* found = red + 4;
+  int64_t before = 0;
+  for (int base = 0; base < A.n; base += kThreads) {
+    const int64_t u = A.n <= kThreads ? first_units : base + tid < A.n ? head_units<KT, NC>(A, pseq_at(A, base + tid)) * A.kv : 0;
+    int64_t chunk = total;
+    const int64_t end = before + (A.n <= kThreads ? scan : block_scan(u, red, &chunk));
+    if (end > a && end - u <= a) {
+      found[0] = base + tid;
+      found[1] = end - u;
+    }
+    before += chunk;
+    if (before > a) break;
+  }
+  __syncthreads();
+  int i = __builtin_amdgcn_readfirstlane((int)found[0]);
+  int64_t s0 = bcast64(found[1], 0);
+  int64_t pos = a;
+  while (pos < b && i < A.n) {
+    PSeq S = pseq_at(A, i);
+    S = {bcast(S.q0, 0), bcast(S.nq, 0), bcast(S.nk, 0)};
+    const B_ B(A, S);
+    int64_t H = 0;
+    for (int t = 0; t < B.count; t += 64) H += bcast64(wave_scan(t + l < B.count ? B.steps(A, S, t + l) : 0), 63);
+    H *= B.cost;
+    if (H == 0 || pos >= s0 + H * A.kv) {  // the next sequence that has rows
+      s0 += H * A.kv;
+      for (++i; i < A.n; i += 64) {
+        const uint64_t some = __ballot(i + l < A.n && pseq_at(A, min(i + l, A.n - 1)).nq > 0);
+        if (some) {
+          i += __builtin_ctzll(some);
+          break;
+        }
+      }
+      continue;
+    }
+    const int g = (int)((pos - s0) / H);
+    int64_t a0 = s0 + g * H;
+    int t = 0, steps = 0;
+    for (int t0 = 0; t0 < B.count; t0 += 64) {
+      const int64_t v = t0 + l < B.count ? (int64_t)B.steps(A, S, t0 + l) * B.cost : 0, end = a0 + wave_scan(v);
+      const uint64_t past = __ballot(end > pos);
+      if (past) {
+        const int at = __builtin_ctzll(past);
+        t = t0 + at;
+        steps = (int)(bcast64(v, at) / B.cost);
+        a0 = bcast64(end - v, at);
+        break;
+      }
+      a0 = bcast64(end, 63);
+    }
+    const int64_t a1 = a0 + (int64_t)steps * B.cost;
+    // a step is the workgroup's in whose part of the line it begins
+    const int first = (int)((max(a - a0, (int64_t)0) + B.cost - 1) / B.cost), last = (int)min((int64_t)steps, (b - a0 + B.cost - 1) / B.cost);
+    Target to = {S.q0, t * B.rows, B.M, g, nullptr, max_rows};
+    if (a0 < a || a1 > b) {
+      to.part = A.part + (int64_t)(2 * w + (a0 < a ? 0 : 1)) * part_floats<DB>(max_rows);
+      if (a0 >= a && tid == 0) {
+        const int64_t wend = (a1 * W - 1) / total;
+        A.shared[w] = {S.q0, t * B.rows, min(B.rows, B.M - t * B.rows), g, (int)(wend - w + 1)};
+      }
+    }
+    __syncthreads();
+    K::run(A, shared, S, A.table + (int64_t)i * A.columns, B, g, t, first, last, to);
+    pos = a1;
+  }
+}
+
+// Adds the parts of a shared block: 32 lanes (at head_dim 128) hold a row, and as many such groups as there are parts, up
+// to all, take a row's parts side by side.  Workgroup (w, y): rows of the block that begins in workgroup w's part.
+template <typename T, int DB>
+__global__ __launch_bounds__(kThreads) void k_paged_join(PArgs A, int max_rows) {
+  constexpr int DP = 32 * DB, LANES = DP / 4 > 16 ? 32 : DP / 4 > 8 ? 16 : 8, G = kThreads / LANES;
+  __shared__ float red[G][DP + 2];
+  const int w = blockIdx.x;
+  const Shared S = A.shared[w];
+  if (S.parts == 0) return;
+  int split = 1;  // groups to a row
+  while (split < S.parts && split < G) split *= 2;
+  const int grp = threadIdx.x / LANES, c = threadIdx.x % LANES, at = grp % split, rows = G / split;
+  for (int r0 = blockIdx.y * rows; r0 < S.rows; r0 += gridDim.y * rows) {
+    const int r = r0 + grp / split;
+    float M = -INFINITY, sum = 0.f;
+    f32x4 o = {};
+    if (r < S.rows) {
+#pragma unroll 4
+      for (int i = at; i < S.parts; i += split) {
+        // the block's first part is its workgroup's last, the others are their workgroups' first
+        const float* p = A.part + (int64_t)(2 * (w + i) + (i == 0)) * part_floats<DB>(max_rows);
+        const float mi = p[max_rows * DP + r], li = p[max_rows * (DP + 1) + r];
+        const f32x4 v = 4 * c < DP ? *reinterpret_cast<const f32x4*>(p + (int64_t)r * DP + 4 * c) : (f32x4){};
+        const float top = fmaxf(M, mi), t = top == -INFINITY ? 0.f : top;
+        const float x = __builtin_amdgcn_exp2f(M - t), y = __builtin_amdgcn_exp2f(mi - t);
+        M = top;
+        sum = sum * x + li * y;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) o[k] = o[k] * x + v[k] * y;
+      }
+    }
+    if (4 * c < DP)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) red[grp][4 * c + k] = o[k];
+    if (c == 0) {
+      red[grp][DP] = M;
+      red[grp][DP + 1] = sum;
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < rows * DP; e += kThreads) {
+      const int q = e / DP, x = e - q * DP, m = S.m0 + r0 + q;
+      if (r0 + q >= S.rows) continue;
+      float top = -INFINITY;
+      for (int i = 0; i < split; ++i) top = fmaxf(top, red[q * split + i][DP]);
+      const float t = top == -INFINITY ? 0.f : top;
+      float all = 0.f, y = 0.f;
+      for (int i = 0; i < split; ++i) {
+        const float f = __builtin_amdgcn_exp2f(red[q * split + i][DP] - t);
+        all = fmaf(red[q * split + i][DP + 1], f, all);
+        y = fmaf(red[q * split + i][x], f, y);
+      }
+      const int query = m / A.per, head = S.g * A.per + m - query * A.per;
+      const int64_t qrow = (int64_t)S.q0 + query;
+      if (x < A.d) ((T*)A.o)[(qrow * A.heads + head) * A.d + x] = (T)(all == 0.f ? 0.f : y / all);
+      if (x == 0 && A.lse) A.lse[(int64_t)head * A.rq + qrow] = all == 0.f ? -INFINITY : (top + log2f(all)) * kLn2;
+    }
+    __syncthreads();
+  }
+}
+
+template <typename T, int DB>
+hipError_t run_paged(const PArgs& A, int max_rows, hipStream_t st) {
+  using M = typename std::conditional<std::is_same<T, float>::value, Split, T>::type;
+  constexpr int BYTES = Walk<M, DB>::BYTES;
+  hipLaunchKernelGGL((k_paged<M, DB>), dim3(A.W), dim3(kThreads), BYTES, st, A, max_rows);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || A.W == 1) return e;
+  hipLaunchKernelGGL((k_paged_join<T, DB>), dim3(A.W - 1, max_rows > 32 ? 4 : 1), dim3(kThreads), 0, st, A, max_rows);
+  return hipGetLastError();
+}
+
+template <typename T>
+hipError_t run_paged_db(const PArgs& A, int max_rows, hipStream_t st) {
+  switch ((A.d + 31) / 32) {
+    case 1: return run_paged<T, 1>(A, max_rows, st);
+    case 2: return run_paged<T, 2>(A, max_rows, st);
+    case 3: return run_paged<T, 3>(A, max_rows, st);
+    default: return run_paged<T, 4>(A, max_rows, st);
+  }
+}
+
+inline bool off16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
+
+}  // namespace
+}  // namespace attn
+}  // namespace dnb
+
+using namespace dnb::attn;
+
+struct dnb_paged_attn {
+  dnb_paged_attn_desc d;
+  int W, max_rows;
+  size_t ws_part, ws_bytes;
+};
+
+extern "C" {
+
+int dnb_paged_attn_create(const dnb_paged_attn_desc* desc, dnb_paged_attn** out) {
+  if (!desc || !out) return DNB_E_NULL;
+  dnb_paged_attn_desc d = *desc;
+  const int rc = dnb::paged::check_layout(desc->cache, &d.cache);
+  if (rc != DNB_OK) return rc;
+  if (d.heads < 1 || d.heads % d.cache.kv_heads != 0 || d.rows_q < 0 || d.q_stride < 0 || !(d.scale >= 0.f && d.scale < INFINITY)) return DNB_E_BADDESC;
+  const int64_t qd = (int64_t)d.heads * d.cache.head_dim, per = d.heads / d.cache.kv_heads, most = 0x7fffffff;
+  if (d.q_stride == 0) d.q_stride = qd;
+  if (d.scale == 0.f) d.scale = (float)(1.0 / sqrt((double)d.cache.head_dim));
+  if (d.heads > 65536 || d.q_stride % (d.cache.dtype == DNB_BF16 ? 8 : 4) != 0 || d.q_stride > (1 << 22) || d.q_stride < qd || d.rows_q > most ||
+      d.rows_q * per > most - 256 || d.rows_q * d.heads > most)
+    return DNB_E_RANGE;
+  dnb_paged_attn* p = new (std::nothrow) dnb_paged_attn();
+  if (!p) return DNB_E_NOMEM;
+  p->d = d;
+  p->W = 256;
+  const int64_t M = d.rows_q * per;
+  p->max_rows = M <= 64 ? 64 : 128;
+  const int dp = (d.cache.head_dim + 31) / 32 * 32;
+  p->ws_part = ((size_t)p->W * sizeof(Shared) + 255) / 256 * 256;
+  p->ws_bytes = p->ws_part + (size_t)2 * p->W * p->max_rows * (dp + 2) * sizeof(float);
+  *out = p;
+  return DNB_OK;
+}
+
+void dnb_paged_attn_destroy(dnb_paged_attn* p) { delete p; }
+
+size_t dnb_paged_attn_workspace_bytes(const dnb_paged_attn* p) { return p ? p->ws_bytes : 0; }
+
+int dnb_paged_attn_forward(const dnb_paged_attn* p, const void* q, const void* k_pages, const void* v_pages, const int32_t* q_offsets,
+                           const int32_t* k_lengths, const int32_t* table, void* out, float* lse, void* workspace, void* stream) {
+  if (!p) return DNB_E_NULL;
+  if (p->d.rows_q == 0) return DNB_OK;
+  const dnb_paged_layout& c = p->d.cache;
+  if (!q || !out || !q_offsets || !k_lengths || !table || !workspace || (c.pages > 0 && (!k_pages || !v_pages))) return DNB_E_NULL;
+  for (const void* x : {q, k_pages, v_pages, (const void*)out, (const void*)workspace})
+    if (off16(x)) return DNB_E_ALIGN;
+  for (const void* x : {(const void*)q_offsets, (const void*)k_lengths, (const void*)table, (const void*)lse})
+    if (reinterpret_cast<uintptr_t>(x) & 3u) return DNB_E_ALIGN;
+  PArgs A{};
+  A.q = q; A.k = k_pages; A.v = v_pages; A.o = out; A.lse = lse;
+  A.shared = (Shared*)workspace;
+  A.part = (float*)((char*)workspace + p->ws_part);
+  A.qo = q_offsets; A.lens = k_lengths; A.table = table;
+  A.n = c.sequences; A.heads = p->d.heads; A.kv = c.kv_heads; A.per = p->d.heads / c.kv_heads; A.d = c.head_dim;
+  A.causal = p->d.causal != 0; A.columns = c.max_pages; A.shift = dnb::paged::log2_of(c.page_size);
+  A.W = p->W;
+  A.pages = c.pages; A.rq = p->d.rows_q; A.qs = p->d.q_stride; A.ps = c.page_stride; A.rs = c.row_stride; A.hs = c.head_stride;
+  A.c = p->d.scale * kLog2e;
+  const hipError_t e = c.dtype == DNB_BF16 ? run_paged_db<__bf16>(A, p->max_rows, (hipStream_t)stream)
+                                           : run_paged_db<float>(A, p->max_rows, (hipStream_t)stream);
+  return e == hipSuccess ? DNB_OK : DNB_E_LAUNCH;
+}
+
+}  // extern "C"

@@ -1,0 +1,262 @@
+// Pages of a paged cache: who has which, on the host, and the copying of pages on the device.
+//
+// Bookkeeping.  refs counts the sequences that have a page.  Copies that were asked for but not taken yet are a list of
+// (source, target) that any order and any overlap in time may carry out: no target is a source, because a copy of
+// a page that is itself still to be filled is made from what fills it, and no page that is a source is given
+// out again before the copies are taken (reads counts the copies that read it).  A target that nobody has any more takes
+// its copy off the list.  All memory is taken at creation, so that later calls fail for lack of pages alone.
+//
+// k_paged_copy is bound by memory: 32 planes of 600 pages of 32 KB, as fast as one large copy.
+#include <hip/hip_runtime.h>
+
+#include <new>
+#include <stdint.h>
+#include <vector>
+
+#include "../../include/dnb.h"
+
+struct dnb_pages {
+  int64_t pages;
+  int32_t page_size, sequences, max_pages;
+  struct Copy {
+    int32_t from, to;
+  };
+  std::vector<int32_t> refs, reads, copy_to, moved;  // copy_to: index of the copy that fills the page, -1: none
+  std::vector<int32_t> table, used;
+  std::vector<int64_t> length;
+  std::vector<int32_t> free_;  // a stack
+  std::vector<Copy> copies;
+
+  int32_t* row(int32_t s) { return table.data() + (int64_t)s * max_pages; }
+  int64_t need(int64_t tokens) const { return (tokens + page_size - 1) / page_size; }
+  void maybe_free(int32_t p) {
+    if (refs[p] == 0 && reads[p] == 0) free_.push_back(p);
+  }
+  int32_t take() {
+    const int32_t p = free_.back();
+    free_.pop_back();
+    refs[p] = 1;
+    return p;
+  }
+  void copy(int32_t from, int32_t to) {
+    if (copy_to[from] >= 0) from = copies[copy_to[from]].from;
+    ++reads[from];
+    copy_to[to] = (int32_t)copies.size();
+    copies.push_back({from, to});
+  }
+  void drop_copy(int32_t to) {
+    const int32_t i = copy_to[to], from = copies[i].from;
+    copies[i] = copies.back();
+    copy_to[copies[i].to] = i;
+    copies.pop_back();
+    copy_to[to] = -1;
+    --reads[from];
+    maybe_free(from);
+  }
+  void leave(int32_t p) {
+    if (--refs[p] > 0) return;
+    if (copy_to[p] >= 0) drop_copy(p);
+    maybe_free(p);
+  }
+  bool has(int32_t s) const { return s >= 0 && s < sequences; }
+};
+
+namespace {
+
+constexpr int kThreads = 256, kPer = 4;  // 16-byte pieces of a thread
+constexpr int64_t kChunk = kThreads * kPer * 16;
+constexpr unsigned kAcross = 1u << 22;
+
+struct CopyArgs {
+  char* pool;
+  const int32_t* pairs;
+  int64_t pages, page_bytes, plane_stride, total;
+  int chunks, count;
+};
+
+// A workgroup copies 16 KB of a page: (plane, pair, chunk), chunks first.
+__global__ __launch_bounds__(kThreads) void k_paged_copy(CopyArgs A) {
+  const int64_t id = (int64_t)blockIdx.y * kAcross + blockIdx.x;
+  if (id >= A.total) return;
+  const int64_t pp = id / A.chunks, chunk = id - pp * A.chunks;
+  const int64_t plane = pp / A.count, pair = pp - plane * A.count;
+  const int64_t from = A.pairs[2 * pair], to = A.pairs[2 * pair + 1];
+  if (from < 0 || from >= A.pages || to < 0 || to >= A.pages || from == to) return;
+  typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+  const int64_t at = chunk * kChunk + threadIdx.x * 16;
+  const char* src = A.pool + plane * A.plane_stride + from * A.page_bytes;
+  char* dst = A.pool + plane * A.plane_stride + to * A.page_bytes;
+  u32x4 v[kPer];
+#pragma unroll
+  for (int i = 0; i < kPer; ++i)
+    if (at + i * kThreads * 16 < A.page_bytes) v[i] = *reinterpret_cast<const u32x4*>(src + at + i * kThreads * 16);
+#pragma unroll
+  for (int i = 0; i < kPer; ++i)
+    if (at + i * kThreads * 16 < A.page_bytes) *reinterpret_cast<u32x4*>(dst + at + i * kThreads * 16) = v[i];
+}
+
+}  // namespace
+
+extern "C" {
+
+int dnb_op_paged_copy(void* pool, int64_t pages, int64_t page_bytes, int64_t planes, int64_t plane_stride, const int32_t* pairs,
+                      int64_t count, void* stream) {
+  if (pages < 0 || page_bytes < 16 || planes < 0 || plane_stride < 0 || count < 0) return DNB_E_BADDESC;
+  if (page_bytes % 16 != 0 || plane_stride % 16 != 0) return DNB_E_UNSUPPORTED;
+  const int64_t most = 0x7fffffff;
+  if (pages > most || planes > most || count > most || page_bytes > ((int64_t)1 << 40) || plane_stride > ((int64_t)1 << 50)) return DNB_E_RANGE;
+  if (planes > 1 && plane_stride / page_bytes < pages) return DNB_E_RANGE;
+  const int64_t chunks = (page_bytes + kChunk - 1) / kChunk;
+  // at most 2^37 workgroups, 2^22 by 2^15
+  if (count > 0 && planes > 0 && ((int64_t)1 << 37) / count / planes < chunks) return DNB_E_RANGE;
+  const int64_t total = count * planes * chunks;
+  if (total == 0 || pages == 0) return DNB_OK;
+  if (!pool || !pairs) return DNB_E_NULL;
+  if (((uintptr_t)pool & 15) || ((uintptr_t)pairs & 3)) return DNB_E_ALIGN;
+  const CopyArgs A{(char*)pool, pairs, pages, page_bytes, plane_stride, total, (int)chunks, (int)count};
+  const unsigned x = total < (int64_t)kAcross ? (unsigned)total : kAcross, y = (unsigned)((total + kAcross - 1) / kAcross);
+  hipLaunchKernelGGL(k_paged_copy, dim3(x, y), dim3(kThreads), 0, (hipStream_t)stream, A);
+  return hipGetLastError() == hipSuccess ? DNB_OK : DNB_E_LAUNCH;
+}
+
+int dnb_pages_create(int64_t pages, int32_t page_size, int32_t sequences, int32_t max_pages, dnb_pages** out) {
+  if (!out) return DNB_E_NULL;
+  if (pages < 1 || page_size < 1 || sequences < 1 || max_pages < 1) return DNB_E_BADDESC;
+  if ((page_size & (page_size - 1)) != 0 || page_size > 65536) return DNB_E_UNSUPPORTED;
+  if (pages > 0x7fffffff || sequences > (1 << 20) || (int64_t)max_pages * page_size > 0x7fffffff) return DNB_E_RANGE;
+  dnb_pages* p = nullptr;
+  try {
+    p = new dnb_pages();
+    p->pages = pages; p->page_size = page_size; p->sequences = sequences; p->max_pages = max_pages;
+    p->table.assign((size_t)sequences * max_pages, -1);
+    p->refs.assign(pages, 0);
+    p->reads.assign(pages, 0);
+    p->copy_to.assign(pages, -1);
+    p->moved.assign(pages, -1);
+    p->used.assign(sequences, 0);
+    p->length.assign(sequences, 0);
+    p->copies.reserve(pages);
+    p->free_.reserve(pages);
+    for (int64_t i = pages - 1; i >= 0; --i) p->free_.push_back((int32_t)i);
+  } catch (...) {
+    delete p;
+    return DNB_E_NOMEM;
+  }
+  *out = p;
+  return DNB_OK;
+}
+
+void dnb_pages_destroy(dnb_pages* p) { delete p; }
+
+int dnb_pages_extend(dnb_pages* p, int32_t s, int64_t tokens) {
+  if (!p) return DNB_E_NULL;
+  if (!p->has(s) || tokens < 0 || tokens > (int64_t)p->max_pages * p->page_size - p->length[s]) return DNB_E_RANGE;
+  if (tokens == 0) return DNB_OK;
+  int32_t* row = p->row(s);
+  const int32_t used = p->used[s];
+  const int64_t need = p->need(p->length[s] + tokens);
+  const bool own = p->length[s] % p->page_size != 0 && p->refs[row[used - 1]] > 1;
+  if (need - used + own > (int64_t)p->free_.size()) return DNB_E_NOMEM;
+  if (own) {
+    const int32_t from = row[used - 1], to = p->take();
+    p->copy(from, to);
+    row[used - 1] = to;
+    p->leave(from);
+  }
+  for (int64_t i = used; i < need; ++i) row[i] = p->take();
+  p->used[s] = (int32_t)need;
+  p->length[s] += tokens;
+  return DNB_OK;
+}
+
+int dnb_pages_fork(dnb_pages* p, int32_t from, int32_t to) {
+  if (!p) return DNB_E_NULL;
+  if (!p->has(from) || !p->has(to)) return DNB_E_RANGE;
+  if (from == to || p->length[to] != 0) return DNB_E_BADDESC;
+  for (int32_t i = 0; i < p->used[from]; ++i) {
+    p->row(to)[i] = p->row(from)[i];
+    ++p->refs[p->row(from)[i]];
+  }
+  p->used[to] = p->used[from];
+  p->length[to] = p->length[from];
+  return DNB_OK;
+}
+
+int dnb_pages_truncate(dnb_pages* p, int32_t s, int64_t length) {
+  if (!p) return DNB_E_NULL;
+  if (!p->has(s) || length < 0 || length > p->length[s]) return DNB_E_RANGE;
+  const int32_t keep = (int32_t)p->need(length);
+  for (int32_t i = p->used[s] - 1; i >= keep; --i) {
+    p->leave(p->row(s)[i]);
+    p->row(s)[i] = -1;
+  }
+  p->used[s] = keep;
+  p->length[s] = length;
+  return DNB_OK;
+}
+
+int dnb_pages_compact(dnb_pages* p) {
+  if (!p) return DNB_E_NULL;
+  int64_t lo = 0, hi = p->pages - 1;
+  bool any = false;
+  for (;;) {
+    while (lo < hi && (p->refs[lo] > 0 || p->reads[lo] > 0)) ++lo;
+    while (hi > lo && p->refs[hi] == 0) --hi;
+    if (lo >= hi) break;
+    // (a page that is still to be filled moves by its copy's target)
+    const int32_t i = p->copy_to[hi];
+    if (i >= 0) {
+      p->copies[i].to = (int32_t)lo;
+      p->copy_to[lo] = i;
+      p->copy_to[hi] = -1;
+    } else {
+      p->copy((int32_t)hi, (int32_t)lo);
+    }
+    p->refs[lo] = p->refs[hi];
+    p->refs[hi] = 0;
+    p->moved[hi] = (int32_t)lo;
+    any = true;
+  }
+  if (!any) return DNB_OK;
+  for (int32_t s = 0; s < p->sequences; ++s)
+    for (int32_t i = 0; i < p->used[s]; ++i) {
+      int32_t& page = p->row(s)[i];
+      if (p->moved[page] >= 0) page = p->moved[page];
+    }
+  p->free_.clear();
+  for (int64_t i = p->pages - 1; i >= 0; --i) {
+    p->moved[i] = -1;
+    p->maybe_free((int32_t)i);
+  }
+  return DNB_OK;
+}
+
+int64_t dnb_pages_free_count(const dnb_pages* p) { return p ? (int64_t)p->free_.size() : 0; }
+
+int dnb_pages_copies(dnb_pages* p, int32_t* pairs, int64_t capacity, int64_t* count) {
+  if (!p || !count) return DNB_E_NULL;
+  if (capacity < 0) return DNB_E_RANGE;
+  *count = (int64_t)p->copies.size();
+  if (!pairs) return capacity == 0 ? DNB_OK : DNB_E_NULL;
+  if (*count > capacity) return DNB_E_RANGE;
+  for (size_t i = 0; i < p->copies.size(); ++i) {
+    const dnb_pages::Copy c = p->copies[i];
+    pairs[2 * i] = c.from;
+    pairs[2 * i + 1] = c.to;
+    p->copy_to[c.to] = -1;
+    if (--p->reads[c.from] == 0) p->maybe_free(c.from);
+  }
+  p->copies.clear();
+  return DNB_OK;
+}
+
+int dnb_pages_table(const dnb_pages* p, int32_t* table, int32_t* k_lengths) {
+  if (!p) return DNB_E_NULL;
+  if (table)
+    for (size_t i = 0; i < p->table.size(); ++i) table[i] = p->table[i];
+  if (k_lengths)
+    for (int32_t s = 0; s < p->sequences; ++s) k_lengths[s] = (int32_t)p->length[s];
+  return DNB_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,273 @@
+"""CPU-side checks of the paged cache: what its entry points refuse before any launch, and the bookkeeping of pages."""
+import ctypes
+import random
+
+import numpy as np
+import pytest
+
+LAYOUT = dict(pages=100, page_size=16, kv_heads=2, head_dim=64, sequences=4, max_pages=20)
+QK = dict(rows=10, q_heads=8, k_heads=2, head_dim=64, rotary_dim=64)
+
+
+def status(call):
+    import paper_1707_06990_amd as dnb
+    try:
+        call()
+        return 0
+    except dnb.DnbError as e:
+        return e.status
+
+
+LAYOUTS = [(dict(pages=-1), -1), (dict(page_size=0), -1), (dict(page_size=24), -5), (dict(page_size=1 << 17), -5), (dict(kv_heads=0), -1),
+           (dict(head_dim=0), -1), (dict(head_dim=36), -5), (dict(head_dim=136), -5), (dict(sequences=0), -1), (dict(sequences=1 << 21), -6),
+           (dict(max_pages=0), -1), (dict(max_pages=1 << 28), -6), (dict(dtype=2), -1), (dict(pages=2 ** 31), -6), (dict(page_stride=12), -6),
+           (dict(row_stride=-8), -1), (dict(row_stride=56), -6), (dict(head_stride=8), -6), (dict(page_stride=(1 << 30) + 8), -6)]
+
+
+@pytest.mark.parametrize("kw,code", LAYOUTS + [
+    (dict(heads=0), -1), (dict(heads=3), -1), (dict(heads=1 << 17), -6), (dict(rows_q=-1), -1), (dict(rows_q=2 ** 31), -6), (dict(rows_q=2 ** 30), -6),
+    (dict(scale=-1.0), -1), (dict(scale=float("nan")), -1), (dict(scale=float("inf")), -1), (dict(q_stride=100), -6), (dict(q_stride=516), -6),
+    (dict(q_stride=-8), -1), (dict(q_stride=(1 << 22) + 8), -6)])
+def test_attention_plans_that_are_refused(dnb, kw, code):
+    plan = dict(heads=8, rows_q=50)
+    for k in list(kw):
+        if k in ("heads", "rows_q", "scale", "q_stride"):
+            plan[k] = kw[k]
+    layout = dnb.dnb_paged_layout(**{**LAYOUT, **{k: v for k, v in kw.items() if k not in plan}})
+    assert status(lambda: dnb.dnb_paged_attn_create(layout, **plan)) == code
+
+
+@pytest.mark.parametrize("kw", [{}, dict(pages=0), dict(page_size=1), dict(page_size=65536, max_pages=1), dict(head_dim=8), dict(head_dim=128), dict(dtype=0),
+                                dict(page_stride=16 * 1024, row_stride=64, head_stride=1024), dict(sequences=1 << 20)])
+def test_attention_arguments(dnb, kw):
+    lib = ctypes.CDLL(dnb.binding.LIB_PATH)
+    fwd = lib.dnb_paged_attn_forward
+    fwd.argtypes = [ctypes.c_void_p] * 11
+    p = dnb.dnb_paged_attn_create(dnb.dnb_paged_layout(**{**LAYOUT, **kw}), 8, 50)
+    assert dnb.dnb_paged_attn_workspace_bytes(p) > 0
+    ok = [4096 * (i + 1) for i in range(9)]
+    for missing in (0, 1, 2, 3, 4, 5, 6, 8):   # (lse, 7, may be null)
+        if kw.get("pages") == 0 and missing in (1, 2):
+            continue
+        assert fwd(p, *[None if i == missing else ok[i] for i in range(9)], None) == -2, missing
+    for odd, by in ((0, 8), (1, 8), (2, 8), (3, 2), (4, 2), (5, 2), (6, 8), (7, 2), (8, 8)):
+        assert fwd(p, *[ok[i] + by if i == odd else ok[i] for i in range(9)], None) == -3, odd
+    assert fwd(None, *ok, None) == -2
+    dnb.dnb_paged_attn_destroy(p)
+    p = dnb.dnb_paged_attn_create(dnb.dnb_paged_layout(**{**LAYOUT, **kw}), 8, 0)
+    assert fwd(p, *[None] * 9, None) == 0   # nothing to do
+    dnb.dnb_paged_attn_destroy(p)
+    assert lib.dnb_paged_attn_create(None, None) == -2
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(rows=-1), -1), (dict(q_heads=-1), -1), (dict(q_heads=0, k_heads=0), -1), (dict(q_heads=4097), -6), (dict(k_heads=4097), -6), (dict(head_dim=0), -1),
+    (dict(head_dim=63, rotary_dim=62), -5), (dict(head_dim=258), -5), (dict(rotary_dim=66), -1), (dict(rotary_dim=7), -1), (dict(rotary_dim=-2), -1),
+    (dict(order=2), -1), (dict(dtype=2), -1), (dict(eps=-1.0), -1), (dict(eps=float("nan")), -1), (dict(eps=float("inf")), -1),
+    (dict(factor=float("nan")), -1), (dict(factor=float("inf")), -1), (dict(rows=(1 << 29) + 1), -6), (dict(q_stride=100), -6), (dict(k_stride=129), -6),
+    (dict(q_out_stride=511), -6), (dict(k_out_stride=-128), -6), (dict(q_stride=2 ** 31), -6), (dict(rows=0), 0)])
+def test_rotation_layouts(dnb, kw, code):
+    qk = dnb.dnb_qk_layout(**{**QK, **kw})
+    p = [4096 * (i + 1) for i in range(14)]
+    if code:
+        assert status(lambda: dnb.dnb_op_qk_rope_forward(qk, *p[:8], stream=0)) == code
+        assert dnb.dnb_op_qk_rope_scratch_bytes(qk) == 0
+        assert status(lambda: dnb.dnb_op_qk_rope_backward(qk, *p[:13], stream=0)) == code
+        assert status(lambda: dnb.dnb_op_paged_append(qk, dnb.dnb_paged_layout(**LAYOUT), *p[:13], stream=0)) == code
+    else:
+        assert status(lambda: dnb.dnb_op_qk_rope_forward(qk, *[None] * 8, stream=0)) == 0
+
+
+def test_rotation_arguments(dnb):
+    qk = dnb.dnb_qk_layout(**QK)
+    p = [4096 * (i + 1) for i in range(14)]
+    fwd = lambda a: status(lambda: dnb.dnb_op_qk_rope_forward(qk, *a, stream=0))  # noqa: E731
+    for i in (0, 1, 4, 5, 6, 7):   # (2, 3: weights)
+        assert fwd([None if j == i else p[j] for j in range(8)]) == -2, i
+    for i, by in ((0, 8), (1, 8), (2, 4), (3, 4), (4, 2), (5, 4), (6, 8), (7, 8)):
+        assert fwd([p[j] + by if j == i else p[j] for j in range(8)]) == -3, i
+    back = lambda a: status(lambda: dnb.dnb_op_qk_rope_backward(qk, *a, stream=0))  # noqa: E731
+    for i in (0, 1, 4, 5, 6, 7, 8, 9, 10, 11, 12):
+        assert back([None if j == i else p[j] for j in range(13)]) == -2, i
+    for i, by in ((0, 8), (1, 8), (2, 4), (3, 4), (4, 2), (5, 4), (6, 8), (7, 8), (8, 8), (9, 8), (10, 4), (11, 4), (12, 8)):
+        assert back([p[j] + by if j == i else p[j] for j in range(13)]) == -3, i
+    assert status(lambda: dnb.dnb_op_qk_rope_forward(None, *p[:8], stream=0)) == -2
+
+
+def test_append_arguments(dnb):
+    qk, cache = dnb.dnb_qk_layout(**QK), dnb.dnb_paged_layout(**LAYOUT)
+    p = [4096 * (i + 1) for i in range(13)]
+    call = lambda a, qk=qk, cache=cache: status(lambda: dnb.dnb_op_paged_append(qk, cache, *a, stream=0))  # noqa: E731
+    for i in (0, 1, 2, 6, 7, 8, 9, 10, 11, 12):   # (weights and positions may be null)
+        assert call([None if j == i else p[j] for j in range(13)]) == -2, i
+    for i, by in ((0, 8), (1, 8), (2, 8), (3, 4), (4, 4), (5, 2), (6, 4), (7, 2), (8, 2), (9, 2), (10, 8), (11, 8), (12, 8)):
+        assert call([p[j] + by if j == i else p[j] for j in range(13)]) == -3, i
+    for kw in (dict(kv_heads=4), dict(head_dim=32), dict(dtype=0)):
+        assert call(p, cache=dnb.dnb_paged_layout(**{**LAYOUT, **kw})) == -1
+    for kw, code in LAYOUTS:
+        if not {"kv_heads", "head_dim", "dtype"} & set(kw):
+            assert call(p, cache=dnb.dnb_paged_layout(**{**LAYOUT, **kw})) == code, kw
+    assert call(p, cache=None) == -2 and call(p, qk=None) == -2
+    assert call([None] * 13, qk=dnb.dnb_qk_layout(**{**QK, "rows": 0})) == 0
+
+
+@pytest.mark.parametrize("kw,code", [
+    (dict(pages=-1), -1), (dict(page_bytes=0), -1), (dict(page_bytes=24), -5), (dict(planes=-1), -1), (dict(plane_stride=-16), -1), (dict(plane_stride=9000), -5),
+    (dict(plane_stride=8 * 32), -6), (dict(count=-1), -1), (dict(count=2 ** 31), -6), (dict(pages=2 ** 31), -6), (dict(planes=2 ** 31), -6),
+    (dict(count=2 ** 30, planes=2 ** 10, plane_stride=1 << 30), -6), (dict(pool=None), -2), (dict(pairs=None), -2), (dict(pool=4104), -3), (dict(pairs=4098), -3),
+    (dict(count=0, pool=None, pairs=None), 0), (dict(planes=0, pool=None), 0), (dict(pages=0, pool=None), 0)])
+def test_copy_arguments(dnb, kw, code):
+    base = dict(pool=4096, pages=10, page_bytes=32, planes=2, plane_stride=320, pairs=8192, count=3, stream=0)
+    assert status(lambda: dnb.dnb_op_paged_copy(**{**base, **kw})) == code
+
+
+@pytest.mark.parametrize("args,code", [((0, 16, 1, 1), -1), ((10, 0, 1, 1), -1), ((10, 24, 1, 1), -5), ((10, 16, 0, 1), -1), ((10, 16, 1, 0), -1),
+                                       ((2 ** 31, 16, 1, 1), -6), ((10, 16, 1 << 21, 1), -6), ((10, 65536, 1, 1 << 15), -6), ((2 ** 31 - 1, 16, 1 << 20, 1 << 24), -7)])
+def test_books_that_are_refused(dnb, args, code):
+    assert status(lambda: dnb.dnb_pages_create(*args)) == code
+
+
+class Model:
+    """What sequences hold, token by token, in a pool of rows: a page's content is moved only by the copies that are taken."""
+
+    def __init__(self, dnb, pages, page, sequences, columns):
+        self.dnb, self.page, self.n, self.columns, self.pages = dnb, page, sequences, columns, pages
+        self.p = dnb.dnb_pages_create(pages, page, sequences, columns)
+        self.pool = np.full((pages, page), -1, dtype=np.int64)
+        self.texts, self.next = [[] for _ in range(sequences)], 0
+
+    def settle(self):
+        pairs = self.dnb.dnb_pages_copies(self.p)
+        sources, targets = set(pairs[:, 0].tolist()), pairs[:, 1].tolist()
+        assert len(set(targets)) == len(targets) and not sources & set(targets)
+        self.pool[pairs[:, 1]] = self.pool[pairs[:, 0]]
+        return pairs
+
+    def write(self, s, tokens):
+        """New tokens go where the table says, after the copies."""
+        self.settle()
+        table, lengths = self.dnb.dnb_pages_table(self.p, self.n, self.columns)
+        for _ in range(tokens):
+            j = len(self.texts[s])
+            self.pool[table[s, j // self.page], j % self.page] = self.next
+            self.texts[s].append(self.next)
+            self.next += 1
+
+    def check(self):
+        table, lengths = self.dnb.dnb_pages_table(self.p, self.n, self.columns)
+        used = set()
+        for s, text in enumerate(self.texts):
+            assert lengths[s] == len(text)
+            need = -(-len(text) // self.page)
+            assert (table[s, need:] == -1).all() and (table[s, :need] >= 0).all()
+            used |= set(table[s, :need].tolist())
+        free = self.dnb.dnb_pages_free_count(self.p)
+        assert free <= self.pages - len(used)
+        return table, used
+
+    def check_content(self):
+        self.settle()
+        table, used = self.check()
+        for s, text in enumerate(self.texts):
+            got = [int(self.pool[table[s, j // self.page], j % self.page]) for j in range(len(text))]
+            assert got == text, s
+        assert self.dnb.dnb_pages_free_count(self.p) == self.pages - len(used)
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_books_against_a_model(dnb, seed):
+    rng = random.Random(seed)
+    m = Model(dnb, rng.choice([8, 30, 60]), rng.choice([1, 4, 16]), 6, 12)
+    for _ in range(600):
+        s, what = rng.randrange(6), rng.random()
+        if what < 0.45:
+            n = rng.randint(0, 2 * m.page)
+            free, copies = dnb.dnb_pages_free_count(m.p), None
+            code = status(lambda: dnb.dnb_pages_extend(m.p, s, n))
+            if code == 0:
+                m.write(s, n)
+            else:
+                assert code in (-6, -7)
+                assert code != -6 or len(m.texts[s]) + n > 12 * m.page
+                assert dnb.dnb_pages_free_count(m.p) == free
+        elif what < 0.65:
+            t = rng.randrange(6)
+            code = status(lambda: dnb.dnb_pages_fork(m.p, s, t))
+            assert code == (-1 if s == t or m.texts[t] else 0)
+            if code == 0:
+                m.texts[t] = list(m.texts[s])
+        elif what < 0.9:
+            n = rng.choice([0, rng.randint(0, len(m.texts[s]))])
+            dnb.dnb_pages_truncate(m.p, s, n)
+            del m.texts[s][n:]
+        elif what < 0.95:
+            dnb.dnb_pages_compact(m.p)
+        else:
+            m.check_content()
+            dnb.dnb_pages_compact(m.p)
+            m.check_content()
+            _, used = m.check()
+            assert used == set(range(len(used)))   # nothing was pending: the lowest numbers
+        m.check()
+    m.check_content()
+    for s in range(6):
+        dnb.dnb_pages_truncate(m.p, s, 0)
+    m.settle()
+    assert dnb.dnb_pages_free_count(m.p) == m.pages
+    dnb.dnb_pages_destroy(m.p)
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_copies_that_wait(dnb, seed):
+    """Forks, copies and moves of which many happen before the copies are taken: what counts is what was written before.  (Room for one token
+    at a time is given and taken back, so that nothing new is written.)"""
+    rng = random.Random(100 + seed)
+    m = Model(dnb, 40, 4, 8, 6)
+    for s in range(3):
+        dnb.dnb_pages_extend(m.p, s, 4 * s + 3)
+        m.write(s, 4 * s + 3)
+    for _ in range(60):
+        for _ in range(rng.randint(1, 12)):
+            s, what = rng.randrange(8), rng.random()
+            if what < 0.4:
+                n = len(m.texts[s])
+                if status(lambda: dnb.dnb_pages_extend(m.p, s, 1)) == 0:
+                    dnb.dnb_pages_truncate(m.p, s, n)
+            elif what < 0.7:
+                t = rng.randrange(8)
+                if status(lambda: dnb.dnb_pages_fork(m.p, s, t)) == 0:
+                    m.texts[t] = list(m.texts[s])
+            elif what < 0.85 and sum(bool(t) for t in m.texts) > 1:
+                dnb.dnb_pages_truncate(m.p, s, 0)
+                m.texts[s] = []
+            else:
+                dnb.dnb_pages_compact(m.p)
+            m.check()
+        m.check_content()
+    dnb.dnb_pages_destroy(m.p)
+
+
+def test_a_fork_and_its_copy(dnb):
+    p = dnb.dnb_pages_create(10, 4, 3, 5)
+    dnb.dnb_pages_extend(p, 0, 6)
+    dnb.dnb_pages_fork(p, 0, 1)
+    assert dnb.dnb_pages_free_count(p) == 8 and len(dnb.dnb_pages_copies(p)) == 0
+    dnb.dnb_pages_extend(p, 1, 1)
+    table, lengths = dnb.dnb_pages_table(p, 3, 5)
+    assert lengths.tolist() == [6, 7, 0] and table[0, 0] == table[1, 0] and table[0, 1] != table[1, 1]
+    lib = ctypes.CDLL(dnb.binding.LIB_PATH)
+    lib.dnb_pages_copies.argtypes = [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int64, ctypes.POINTER(ctypes.c_int64)]
+    n = ctypes.c_int64()
+    buf = (ctypes.c_int32 * 2)()
+    assert lib.dnb_pages_copies(p, buf, 0, ctypes.byref(n)) == -6 and n.value == 1
+    assert lib.dnb_pages_copies(p, None, 1, ctypes.byref(n)) == -2 and lib.dnb_pages_copies(p, buf, -1, ctypes.byref(n)) == -6
+    assert dnb.dnb_pages_copies(p).tolist() == [[table[0, 1], table[1, 1]]]
+    dnb.dnb_pages_extend(p, 0, 1)   # now its own
+    assert len(dnb.dnb_pages_copies(p)) == 0
+    for call, code in ((lambda: dnb.dnb_pages_extend(p, 3, 1), -6), (lambda: dnb.dnb_pages_extend(p, -1, 1), -6), (lambda: dnb.dnb_pages_extend(p, 0, -1), -6),
+                       (lambda: dnb.dnb_pages_extend(p, 0, 14), -6), (lambda: dnb.dnb_pages_truncate(p, 0, 8), -6), (lambda: dnb.dnb_pages_fork(p, 0, 3), -6),
+                       (lambda: dnb.dnb_pages_fork(p, 0, 1), -1), (lambda: dnb.dnb_pages_extend(p, 2, 2 ** 62), -6), (lambda: dnb.dnb_pages_extend(None, 0, 1), -2)):
+        assert status(call) == code
+    dnb.dnb_pages_extend(p, 0, 13)
+    assert status(lambda: dnb.dnb_pages_extend(p, 2, 20)) == -7
+    dnb.dnb_pages_destroy(p)
