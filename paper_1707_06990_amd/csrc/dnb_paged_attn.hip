@@ -37,7 +37,11 @@ struct PArgs {
   int n, heads, kv, per, d, causal, columns, shift, W;
   int64_t pages, rq, qs, ps, rs, hs;
   float c;  // scale * log2(e)
+  uint32_t per_mul, per_shift;
 };
+
+// m / per, m below 2^31
+__device__ __forceinline__ int query_of(const PArgs& A, int m) { return A.per == 1 ? m : (int)(__umulhi((uint32_t)m, A.per_mul) >> A.per_shift); }
 
 // 16 bytes of the tensors' zeros, twice: where rows that are not there are read
 __device__ __attribute__((aligned(32))) const float kZeros[8] = {};
@@ -54,7 +58,7 @@ __device__ __forceinline__ PSeq pseq_at(const PArgs& A, int i) {
   return s;
 }
 __device__ __forceinline__ unsigned pseen(const PArgs& A, const PSeq& S, int m) {
-  return A.causal ? max(S.nk + min(m / A.per + 1 - S.nq, 0), 0) : S.nk;
+  return A.causal ? max(S.nk + min(query_of(A, m) + 1 - S.nq, 0), 0) : S.nk;
 }
 
 // Blocks of a sequence: RW of the four waves take 32 * NC rows each.  Cost: of a step, in units of the line.
@@ -176,22 +180,22 @@ __device__ __forceinline__ void join_waves(Online<DB>& R, char* shared, int wave
 }
 
 template <typename E, int DB>
-__device__ __forceinline__ void write_rows(const PArgs& A, const Target& to, const Online<DB>& R, int row0) {
+__device__ __forceinline__ void write_rows(const PArgs& A, const Target& to, const f32x16 (&o)[DB], float top, float half, int row0) {
   const int l = lane_id(), r = row0 + (l & 31), m = to.m0 + r;
   const bool valid = m < to.M;
-  const float sum = half_sum(R.l);
+  const float sum = half_sum(half);
   if (to.part) {
-    store_cols<float, DB>(to.part + (int64_t)r * 32 * DB, valid, 32 * DB, R.o, 1.f);
+    store_cols<float, DB>(to.part + (int64_t)r * 32 * DB, valid, 32 * DB, o, 1.f);
     if (valid && l < 32) {
-      to.part[to.rows * 32 * DB + r] = R.m;
+      to.part[to.rows * 32 * DB + r] = top;
       to.part[to.rows * (32 * DB + 1) + r] = sum;
     }
     return;
   }
-  const int query = m / A.per, head = to.g * A.per + m - query * A.per;
+  const int query = query_of(A, m), head = to.g * A.per + m - query * A.per;
   const int64_t qrow = (int64_t)to.q0 + query;
-  store_cols<E, DB>((E*)A.o + (qrow * A.heads + head) * A.d, valid, A.d, R.o, sum == 0.f ? 0.f : 1.f / sum);
-  if (valid && l < 32 && A.lse) A.lse[(int64_t)head * A.rq + qrow] = sum == 0.f ? -INFINITY : (R.m + log2f(sum)) * kLn2;
+  store_cols<E, DB>((E*)A.o + (qrow * A.heads + head) * A.d, valid, A.d, o, sum == 0.f ? 0.f : 1.f / sum);
+  if (valid && l < 32 && A.lse) A.lse[(int64_t)head * A.rq + qrow] = sum == 0.f ? -INFINITY : (top + log2f(sum)) * kLn2;
 }
 
 template <typename T, int DB>
@@ -208,7 +212,7 @@ struct Walk {
                                              int t, int first, int last, const Target& to) {
     const lds_t lds = lds_start(shared);
     const int wave = threadIdx.x >> 6, l = lane_id(), KH = 4 / B.rw, kh = wave & (KH - 1), row0 = wave / KH * 32;
-    const int m = t * B.rows + row0 + (l & 31), query = m / A.per, head = g * A.per + m - query * A.per;
+    const int m = t * B.rows + row0 + (l & 31), query = query_of(A, m), head = g * A.per + m - query * A.per;
     const bool valid = m < B.M;
     const unsigned sees = pseen(A, S, m);
     const int m0 = t * B.rows + row0;
@@ -249,7 +253,408 @@ struct Walk {
       __syncthreads();
       join_waves<DB>(R, shared, wave, KH);
     }
-    if (kh == 0) write_rows<E, DB>(A, to, R, row0);
+    if (kh == 0) write_rows<E, DB>(A, to, R.o, R.m, R.l, row0);
+  }
+};
+
+// ---------------------------------------------------------------- bf16
+
+// O, maximum and sum of N sets of 32 rows.
+template <int DB, int N>
+struct Sets {
+  f32x16 o[N][DB];
+  float m[N], l[N];
+};
+
+// Keys and values of a step on their way from the pages to LDS, without passing through registers: a load instruction of
+// a wave fills 1 KB of LDS, RPI rows, lane after lane; which piece of its row a lane fetches is turned round so that the tile's
+// order comes out.  The wave has rows wave * 32 .. + 31, U instructions for K and as many for V.
+template <int DB>
+struct Fetch {
+  using L = Tile<__bf16, DB>;
+  static constexpr int RPI = 64 / L::PC, U = 32 / RPI, WINDOW = 64 / U;  // WINDOW: steps whose pages one register's lanes hold
+  int now, next;      // pages of row groups: lane i: step base + i / U, group i % U; of this window and the following
+  int base;           // the window's first step
+  uint32_t row_at;    // bytes from the group's first row to the lane's
+  const int32_t* table;
+  int64_t head;       // bytes
+
+  __device__ __forceinline__ int window(const PArgs& A, int step, unsigned nk) const {
+    const int l = lane_id();
+    const unsigned key = (unsigned)(step + l / U) * 128u + (threadIdx.x >> 6) * 32u + (l % U) * RPI;
+    return key < nk ? table[key >> A.shift] : 0;
+  }
+  __device__ __forceinline__ void init(const PArgs& A, const int32_t* t, int g, int first, unsigned nk) {
+    const int l = lane_id();
+    table = t;
+    head = (int64_t)g * A.hs * 2;
+    base = first;
+    row_at = (uint32_t)(l / L::PC) * (uint32_t)(A.rs * 2);
+    now = window(A, first, nk);
+    next = window(A, first + WINDOW, nk);
+  }
+  __device__ __forceinline__ void turn(const PArgs& A, int step, unsigned nk) {
+    if (step < base + WINDOW) return;
+    base += WINDOW;
+    now = next;
+    next = window(A, base + WINDOW, nk);
+  }
+  static __device__ __forceinline__ void load(lds_t to, uint32_t voff, const char* from) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(voff), "s"(from) : "memory");
+  }
+  static __device__ __forceinline__ void load(lds_t to, const char* from) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory");
+  }
+  // Step `step` into the tiles at kt and vt; nk: keys that exist.
+  __device__ __forceinline__ void issue(const PArgs& A, lds_t kt, lds_t vt, int step, unsigned nk) const {
+    const int l = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const unsigned key0 = (unsigned)step * 128u + wave * 32u, mask = (1u << A.shift) - 1;
+    const char *kp = (const char*)A.k + head, *vp = (const char*)A.v + head;
+    const uint32_t ps = (uint32_t)(A.ps * 2), rs = (uint32_t)(A.rs * 2);  // (both at most 2^31)
+    kt += wave * 32 * L::PITCH;
+    vt += wave * 32 * L::PITCH;
+    const int at = (step - base) * U;
+    const bool mine = l >= at && l < at + U;
+    const int c0 = (l % L::PC) ^ L::swz(l / L::PC);
+    const bool grouped = (1 << A.shift) >= RPI;  // a group of rows lies within a page
+    // all rows there, of pages of the pool, with as many pieces as a tile's, and offsets of 32 bits
+    if (grouped && key0 + 32 <= nk && A.d == 32 * DB && A.rs < (1 << 26) && !__any(mine && (unsigned)now >= A.pages)) {
+#pragma unroll 2
+      for (int u = 0; u < U; ++u) {
+        const uint64_t from = (uint64_t)(uint32_t)__builtin_amdgcn_readlane(now, at + u) * ps + (uint64_t)((key0 + u * RPI) & mask) * rs;
+        const uint32_t off = row_at + min(c0 ^ L::swz(u * RPI), L::CH - 1) * 16;  // (pieces past a row's are not read)
+        load(kt + u * 1024, off, kp + from);
+        load(vt + u * 1024, off, vp + from);
+      }
+      return;
+    }
+    // What is not there comes from the zeros.  (Pages of less than a group: a lookup each lane, all before the first load into
+    // LDS, for which a later one would wait.)
+    int pages[U];
+    if (!grouped) {
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const unsigned key = key0 + u * RPI + l / L::PC;
+        pages[u] = key < nk ? table[key >> A.shift] : 0;
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) asm volatile("" ::"v"(pages[u]));
+    } else {
+#pragma unroll
+      for (int u = 0; u < U; ++u) pages[u] = __builtin_amdgcn_readlane(now, at + u);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const unsigned key = key0 + u * RPI + l / L::PC;
+      const int c = c0 ^ L::swz(u * RPI);
+      const bool in = key < nk && c * 8 < A.d && pages[u] >= 0 && pages[u] < A.pages;
+      const uint64_t from = (uint64_t)(uint32_t)pages[u] * ps + (uint64_t)(key & mask) * rs + c * 16;
+      load(kt + u * 1024, in ? kp + from : (const char*)kZeros);
+      load(vt + u * 1024, in ? vp + from : (const char*)kZeros);
+    }
+  }
+};
+
+template <int N>
+__device__ __forceinline__ void wait_loads() { asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void wait_lds() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+__device__ __forceinline__ void meet() {
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+template <int DB>
+struct Walk<__bf16, DB> {
+  static constexpr int KT = 128, NC = 2;
+  using L = Tile<__bf16, DB>;
+  using F = Fetch<DB>;
+  static constexpr int TILE = KT * L::PITCH;
+  static constexpr int JOIN = 256 * (32 * DB + 2) * 4;
+  static constexpr int BYTES = 4 * TILE > JOIN ? 4 * TILE : JOIN;
+
+  template <int N>
+  using Scores = f32x16[N];
+  template <int N>
+  using Queries = Piece[N][L::NS][1];
+
+  template <int N>
+  static __device__ __forceinline__ void scores(Scores<N>& s, const Queries<N>& q, lds_t at) {
+#pragma unroll
+    for (int n = 0; n < N; ++n) s[n] = (f32x16){};
+#pragma unroll
+    for (int k = 0; k < L::NS; ++k) {
+      Piece a[1];
+      a[0].q = lds_read<u32x4>(at ^ (k << 5));
+#pragma unroll
+      for (int n = 0; n < N; ++n) mma(s[n], a, q[n][k], (__bf16*)nullptr);
+    }
+  }
+  template <int N>
+  static __device__ __forceinline__ void values(Sets<DB, N>& R, const Scores<N>& s, lds_t at) {
+    using lds4 = __attribute__((address_space(3))) s16x4;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      Piece y[N][1];
+#pragma unroll
+      for (int n = 0; n < N; ++n)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) y[n][0].b[j] = (__bf16)s[n][8 * t + j];
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        Piece x[1];
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(uintptr_t)((at ^ (db << 6)) + 16 * t * L::PITCH));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(uintptr_t)((at ^ (db << 6) ^ 32) + (16 * t + 8) * L::PITCH));
+        const uint2 a = __builtin_bit_cast(uint2, lo), b = __builtin_bit_cast(uint2, hi);
+        x[0].q = (u32x4){a.x, a.y, b.x, b.y};
+#pragma unroll
+        for (int n = 0; n < N; ++n) mma(R.o[n][db], x, y[n], (__bf16*)nullptr);
+      }
+    }
+  }
+  // Largest raw score of each column
+  template <int N>
+  static __device__ __forceinline__ void tops(float (&top)[N], const Scores<N>& s) {
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      float t = s[n][0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) t = fmaxf(t, s[n][i]);
+      top[n] = half_max(t);
+    }
+  }
+  // The sums so far take the new maximum where it has grown by more than 8 (a factor of 256).
+  template <int N>
+  static __device__ __forceinline__ void rescale(Sets<DB, N>& R, float (&top)[N], float c) {
+    bool grow = false;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      top[n] *= c;  // c > 0
+      grow = grow || top[n] > R.m[n] + 8.f || (R.m[n] == -INFINITY && top[n] > -INFINITY);
+    }
+    if (!__any(grow)) return;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const float m = fmaxf(R.m[n], top[n]);
+      const float a = m == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(R.m[n] - m);
+      R.m[n] = m;
+      R.l[n] *= a;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) R.o[n][db][i] *= a;
+    }
+  }
+  template <int N>
+  static __device__ __forceinline__ void weights(Sets<DB, N>& R, Scores<N>& s, float c) {
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const float m = R.m[n] == -INFINITY ? 0.f : R.m[n];
+      float t = 0.f;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        s[n][i] = __builtin_amdgcn_exp2f(fmaf(s[n][i], c, -m));
+        t += s[n][i];
+      }
+      R.l[n] += t;
+    }
+  }
+
+  // A block of 32 keys, whose scores are s and their tops `top`, and beside it the scores of the following one: a
+  // product's 32 cycles are another five instructions' time.
+  template <int N>
+  static __device__ __forceinline__ void block(Sets<DB, N>& R, Scores<N>& s, Scores<N>& sn, float (&top)[N], const Queries<N>& q, float c, lds_t k_at,
+                                               lds_t v_at) {
+    rescale<N>(R, top, c);
+    __builtin_amdgcn_sched_barrier(0);
+    scores<N>(sn, q, k_at);
+    weights<N>(R, s, c);
+    values<N>(R, s, v_at);
+    tops<N>(top, sn);
+    __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);
+#pragma unroll
+    for (int k = 0; k < L::NS; ++k) {
+#pragma unroll
+      for (int n = 0; n < N; ++n) {
+        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x2, 5, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    }
+#pragma unroll
+    for (int k = 0; k < 2 * DB * N; ++k) {
+      __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x2, 5, 0);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+
+  static constexpr int N = NC;
+
+  // The KH waves of a set of rows join, and the results go where they belong.  Each wave's sums go to LDS, a row after
+  // another, 16-byte pieces turned round by the row against bank conflicts; then a thread takes four values of a row.
+  static __device__ __forceinline__ void join(const PArgs& A, char* shared, const Sets<DB, N>& R, const Blocks<KT, NC>& B, const Target& to) {
+    constexpr int PIECES = 8 * DB, DP = 32 * DB;
+    const int wave = threadIdx.x >> 6, l = lane_id(), KH = 4 / B.rw;
+    f32x4* o = reinterpret_cast<f32x4*>(shared);                       // (wave, row, piece)
+    float2* ml = reinterpret_cast<float2*>(shared + 256 * DP * 4);  // (wave, row)
+    const int rows = min(B.rows, to.M - to.m0);
+    __syncthreads();
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int r = 32 * n + (l & 31), slot = wave * 32 * N + r;
+      const float sum = half_sum(R.l[n]);
+      if (wave / KH * 32 * N + r < rows) {
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+          for (int g = 0; g < 4; ++g)
+            o[slot * PIECES + ((8 * db + 2 * g + (l >> 5)) ^ (r & 7))] = (f32x4){R.o[n][db][4 * g], R.o[n][db][4 * g + 1], R.o[n][db][4 * g + 2], R.o[n][db][4 * g + 3]};
+        if (l < 32) ml[slot] = make_float2(R.m[n], sum);
+      }
+    }
+    __syncthreads();
+    for (int e = threadIdx.x; e < rows * PIECES; e += kThreads) {
+      const int row = e / PIECES, c = e - row * PIECES, r = row % (32 * N), slot = row / (32 * N) * KH * 32 * N + r;
+      float m = -INFINITY, sum = 0.f;
+      for (int k = 0; k < KH; ++k) m = fmaxf(m, ml[slot + k * 32 * N].x);
+      const float z = m == -INFINITY ? 0.f : m;
+      f32x4 y = {};
+      for (int k = 0; k < KH; ++k) {
+        const float2 x = ml[slot + k * 32 * N];
+        const float f = __builtin_amdgcn_exp2f(x.x - z);
+        const f32x4 v = o[(slot + k * 32 * N) * PIECES + (c ^ (r & 7))];
+        sum = fmaf(x.y, f, sum);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) y[j] = fmaf(v[j], f, y[j]);
+      }
+      const int mm = to.m0 + row;
+      if (to.part) {
+        *reinterpret_cast<f32x4*>(to.part + (int64_t)row * DP + 4 * c) = y;
+        if (c == 0) {
+          to.part[to.rows * DP + row] = m;
+          to.part[to.rows * (DP + 1) + row] = sum;
+        }
+        continue;
+      }
+      const int query = query_of(A, mm), head = to.g * A.per + mm - query * A.per;
+      const int64_t qrow = (int64_t)to.q0 + query;
+      if (4 * c < A.d) {
+        typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+        const float f = sum == 0.f ? 0.f : 1.f / sum;
+        *reinterpret_cast<bf16x4*>((__bf16*)A.o + (qrow * A.heads + head) * A.d + 4 * c) = (bf16x4){(__bf16)(y[0] * f), (__bf16)(y[1] * f), (__bf16)(y[2] * f), (__bf16)(y[3] * f)};
+      }
+      if (c == 0 && A.lse) A.lse[(int64_t)head * A.rq + qrow] = sum == 0.f ? -INFINITY : (m + log2f(sum)) * kLn2;
+    }
+  }
+
+  static __device__ __forceinline__ void run(const PArgs& A, char* shared, const PSeq& S, const int32_t* table, const Blocks<KT, NC>& B, int g, int t,
+                                             int first, int last, const Target& to) {
+    const lds_t lds = lds_start(shared), kt = lds, vt = lds + 2 * TILE;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = lane_id(), KH = 4 / B.rw, kh = wave & (KH - 1), row0 = wave / KH * 32 * NC;
+    const unsigned all = pseen(A, S, min((t + 1) * B.rows, B.M) - 1);  // keys that the block's last row sees
+    F f;
+    if (first < last) f.init(A, table, g, first, all);
+    Queries<N> q;
+    Sets<DB, N> R;
+    unsigned sees[N];
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int m = t * B.rows + row0 + 32 * n + (l & 31), query = query_of(A, m), head = g * A.per + m - query * A.per;
+      sees[n] = pseen(A, S, m);
+      load_cols<__bf16, DB>(q[n], (const __bf16*)A.q + ((int64_t)S.q0 + query) * A.qs + (int64_t)head * A.d, m < B.M, A.d);
+#pragma unroll
+      for (int db = 0; db < DB; ++db) R.o[n][db] = (f32x16){};
+      R.m[n] = -INFINITY;
+      R.l[n] = 0.f;
+    }
+    // keys that all rows of the wave see; that all of the workgroup see, by which the waves choose their way between barriers
+    const unsigned least = pseen(A, S, t * B.rows + row0), lowest = pseen(A, S, t * B.rows);
+    if (first < last) {
+      f.issue(A, kt, vt, first, all);
+      if (first + 1 < last) {
+        f.turn(A, first + 1, all);
+        f.issue(A, kt + TILE, vt + TILE, first + 1, all);
+        wait_loads<2 * F::U>();
+      } else {
+        wait_loads<0>();
+      }
+      if (KH < 4) meet();
+      const int nb = 4 / KH;  // blocks of 32 keys of this wave in a step
+      const lds_t k_lane = L::at(l & 31, l >> 5) + kt + kh * nb * 32 * L::PITCH;
+      const lds_t v_lane = L::at(4 * (l >> 5) + ((l >> 2) & 3), 2 * ((l >> 4) & 1) + ((l >> 1) & 1)) + (l & 1) * 8 + vt + kh * nb * 32 * L::PITCH;
+      lds_t buf = 0;  // of the step at hand
+      Scores<N> a, b;
+      float top[N];
+      scores<N>(a, q, k_lane);
+      int s = first;
+      // Steps after which another comes and all of whose keys, and the next one's first, all rows see: the scores of a block beside the weights
+      // and values of the one before.
+      if (KH < 4) {
+        tops<N>(top, a);
+#pragma unroll 1
+        for (; s + 1 < last && ((unsigned)s + 2) * KT <= lowest; ++s) {
+          lds_t k_at = k_lane + buf, v_at = v_lane + buf;
+#pragma unroll 1
+          for (int j = 2; j < nb; j += 2) {
+            block<N>(R, a, b, top, q, A.c, k_at + 32 * L::PITCH, v_at);
+            block<N>(R, b, a, top, q, A.c, k_at + 64 * L::PITCH, v_at + 32 * L::PITCH);
+            k_at += 64 * L::PITCH;
+            v_at += 64 * L::PITCH;
+          }
+          block<N>(R, a, b, top, q, A.c, k_at + 32 * L::PITCH, v_at);
+          buf ^= TILE;
+          // the next step is here
+          wait_loads<0>();
+          meet();
+          block<N>(R, b, a, top, q, A.c, k_lane + buf, v_at + 32 * L::PITCH);
+          if (s + 2 < last) {
+            // all have read this one
+            wait_lds();
+            meet();
+            f.turn(A, s + 2, all);
+            f.issue(A, kt + (buf ^ TILE), vt + (buf ^ TILE), s + 2, all);
+          }
+        }
+      }
+      // The others one by one.  (With four waves to the rows each reads what it has fetched itself, and waits for nobody.)
+#pragma unroll 1
+      for (; s < last; ++s) {
+#pragma unroll 1
+        for (int j = 0; j < nb; ++j) {
+          const unsigned key = (unsigned)s * KT + (kh * nb + j) * 32;
+          if (key + 32 > least) {
+            asm volatile("");  // a branch: as selections its 64 instructions were part of every block
+#pragma unroll
+            for (int n = 0; n < N; ++n) hide(a[n], key, sees[n]);
+          }
+          tops<N>(top, a);
+          rescale<N>(R, top, A.c);
+          weights<N>(R, a, A.c);
+          values<N>(R, a, v_lane + buf + j * 32 * L::PITCH);
+          if (j + 1 < nb) scores<N>(a, q, k_lane + buf + (j + 1) * 32 * L::PITCH);
+        }
+        if (s + 1 == last) break;
+        wait_lds();
+        if (KH < 4) meet();
+        if (s + 2 < last) {
+          f.turn(A, s + 2, all);
+          f.issue(A, kt + buf, vt + buf, s + 2, all);
+          wait_loads<2 * F::U>();
+        } else {
+          wait_loads<0>();
+        }
+        if (KH < 4) meet();
+        buf ^= TILE;
+        scores<N>(a, q, k_lane + buf);
+      }
+    }
+    if (KH > 1) {
+      join(A, shared, R, B, to);
+      return;
+    }
+#pragma unroll
+    for (int n = 0; n < N; ++n) write_rows<__bf16, DB>(A, to, R.o[n], R.m[n], R.l[n], row0 + 32 * n);
   }
 };
 
@@ -273,7 +678,9 @@ __global__ __launch_bounds__(kThreads, 1) void k_paged(PArgs A, int max_rows) {
   const int w = A.W % 8 == 0 ? (int)(blockIdx.x % 8) * (A.W / 8) + (int)blockIdx.x / 8 : (int)blockIdx.x;
   if (tid == 0) A.shared[w].parts = 0;
   if (w >= W || total == 0) return;
-  const int64_t a = w * total / W, b = (w + 1) * total / W;
+  // parts of the line: total * w / W.  (In doubles: total is below 2^53 and W at most 512, so that quotients are right.)
+  const int64_t share = (int64_t)((double)total / W), rest = total - share * W;
+  const int64_t a = w * share + (int)(w * rest) / W, b = (w + 1) * share + (int)((w + 1) * rest) / W;
   // the sequence at a, and where on the line it begins
   int64_t* found = red + 4;
   int64_t before = 0;
@@ -290,55 +697,64 @@ __global__ __launch_bounds__(kThreads, 1) void k_paged(PArgs A, int max_rows) {
   }
   __syncthreads();
   int i = __builtin_amdgcn_readfirstlane((int)found[0]);
-  int64_t s0 = bcast64(found[1], 0);
-  int64_t pos = a;
-  while (pos < b && i < A.n) {
-    PSeq S = pseq_at(A, i);
-    S = {bcast(S.q0, 0), bcast(S.nq, 0), bcast(S.nk, 0)};
+  int64_t a0 = bcast64(found[1], 0);
+  PSeq S = pseq_at(A, i);
+  S = {bcast(S.q0, 0), bcast(S.nq, 0), bcast(S.nk, 0)};
+  int g = 0, t = 0;
+  {
     const B_ B(A, S);
+    // key/value head and block at a
     int64_t H = 0;
-    for (int t = 0; t < B.count; t += 64) H += bcast64(wave_scan(t + l < B.count ? B.steps(A, S, t + l) : 0), 63);
+    for (int t0 = 0; t0 < B.count; t0 += 64) H += bcast64(wave_scan(t0 + l < B.count ? B.steps(A, S, t0 + l) : 0), 63);
     H *= B.cost;
-    if (H == 0 || pos >= s0 + H * A.kv) {  // the next sequence that has rows
-      s0 += H * A.kv;
-      for (++i; i < A.n; i += 64) {
-        const uint64_t some = __ballot(i + l < A.n && pseq_at(A, min(i + l, A.n - 1)).nq > 0);
-        if (some) {
-          i += __builtin_ctzll(some);
-          break;
-        }
-      }
-      continue;
-    }
-    const int g = (int)((pos - s0) / H);
-    int64_t a0 = s0 + g * H;
-    int t = 0, steps = 0;
+    g = (int)((double)(a - a0) / (double)H);
+    a0 += g * H;
     for (int t0 = 0; t0 < B.count; t0 += 64) {
       const int64_t v = t0 + l < B.count ? (int64_t)B.steps(A, S, t0 + l) * B.cost : 0, end = a0 + wave_scan(v);
-      const uint64_t past = __ballot(end > pos);
+      const uint64_t past = __ballot(end > a);
       if (past) {
         const int at = __builtin_ctzll(past);
         t = t0 + at;
-        steps = (int)(bcast64(v, at) / B.cost);
         a0 = bcast64(end - v, at);
         break;
       }
       a0 = bcast64(end, 63);
     }
+  }
+  for (;;) {
+    const B_ B(A, S);
+    const int steps = B.steps(A, S, t);
     const int64_t a1 = a0 + (int64_t)steps * B.cost;
     // a step is the workgroup's in whose part of the line it begins
-    const int first = (int)((max(a - a0, (int64_t)0) + B.cost - 1) / B.cost), last = (int)min((int64_t)steps, (b - a0 + B.cost - 1) / B.cost);
+    const int first = a0 < a ? (int)((uint32_t)(a - a0) + B.cost - 1) / B.cost : 0, last = a1 > b ? min(steps, (int)((uint32_t)(b - a0) + B.cost - 1) / B.cost) : steps;
     Target to = {S.q0, t * B.rows, B.M, g, nullptr, max_rows};
     if (a0 < a || a1 > b) {
       to.part = A.part + (int64_t)(2 * w + (a0 < a ? 0 : 1)) * part_floats<DB>(max_rows);
       if (a0 >= a && tid == 0) {
-        const int64_t wend = (a1 * W - 1) / total;
-        A.shared[w] = {S.q0, t * B.rows, min(B.rows, B.M - t * B.rows), g, (int)(wend - w + 1)};
+        // the last part's workgroup is the one with a1 - 1
+        int e = max(w + 1, (int)((double)a1 / (double)total * W) - 2);
+        while ((e + 1) * share + (int)((e + 1) * rest) / W < a1) ++e;
+        A.shared[w] = {S.q0, t * B.rows, min(B.rows, B.M - t * B.rows), g, e - w + 1};
       }
     }
     __syncthreads();
     K::run(A, shared, S, A.table + (int64_t)i * A.columns, B, g, t, first, last, to);
-    pos = a1;
+    if (a1 >= b) return;
+    a0 = a1;
+    if (++t < B.count) continue;
+    t = 0;
+    if (++g < A.kv) continue;
+    g = 0;
+    for (++i; i < A.n; i += 64) {  // the next sequence that has rows
+      const uint64_t some = __ballot(i + l < A.n && pseq_at(A, min(i + l, A.n - 1)).nq > 0);
+      if (some) {
+        i += __builtin_ctzll(some);
+        break;
+      }
+    }
+    if (i >= A.n) return;
+    S = pseq_at(A, i);
+    S = {bcast(S.q0, 0), bcast(S.nq, 0), bcast(S.nk, 0)};
   }
 }
 
@@ -351,8 +767,8 @@ __global__ __launch_bounds__(kThreads) void k_paged_join(PArgs A, int max_rows) 
   const int w = blockIdx.x;
   const Shared S = A.shared[w];
   if (S.parts == 0) return;
-  int split = 1;  // groups to a row
-  while (split < S.parts && split < G) split *= 2;
+  int split = 1;  // groups to a row: where there are few rows
+  while (split < S.parts && split < G && S.rows * 2 * split <= (int)gridDim.y * G) split *= 2;
   const int grp = threadIdx.x / LANES, c = threadIdx.x % LANES, at = grp % split, rows = G / split;
   for (int r0 = blockIdx.y * rows; r0 < S.rows; r0 += gridDim.y * rows) {
     const int r = r0 + grp / split;
@@ -393,7 +809,7 @@ __global__ __launch_bounds__(kThreads) void k_paged_join(PArgs A, int max_rows) 
         all = fmaf(red[q * split + i][DP + 1], f, all);
         y = fmaf(red[q * split + i][x], f, y);
       }
-      const int query = m / A.per, head = S.g * A.per + m - query * A.per;
+      const int query = query_of(A, m), head = S.g * A.per + m - query * A.per;
       const int64_t qrow = (int64_t)S.q0 + query;
       if (x < A.d) ((T*)A.o)[(qrow * A.heads + head) * A.d + x] = (T)(all == 0.f ? 0.f : y / all);
       if (x == 0 && A.lse) A.lse[(int64_t)head * A.rq + qrow] = all == 0.f ? -INFINITY : (top + log2f(all)) * kLn2;
@@ -409,7 +825,7 @@ hipError_t run_paged(const PArgs& A, int max_rows, hipStream_t st) {
   hipLaunchKernelGGL((k_paged<M, DB>), dim3(A.W), dim3(kThreads), BYTES, st, A, max_rows);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || A.W == 1) return e;
-  hipLaunchKernelGGL((k_paged_join<T, DB>), dim3(A.W - 1, max_rows > 32 ? 4 : 1), dim3(kThreads), 0, st, A, max_rows);
+  hipLaunchKernelGGL((k_paged_join<T, DB>), dim3(A.W - 1, max_rows / 8), dim3(kThreads), 0, st, A, max_rows);
   return hipGetLastError();
 }
 
@@ -456,7 +872,7 @@ int dnb_paged_attn_create(const dnb_paged_attn_desc* desc, dnb_paged_attn** out)
   p->d = d;
   p->W = 256;
   const int64_t M = d.rows_q * per;
-  p->max_rows = M <= 64 ? 64 : 128;
+  p->max_rows = M <= 64 ? 64 : M <= 128 || d.cache.dtype == DNB_F32 ? 128 : 256;
   const int dp = (d.cache.head_dim + 31) / 32 * 32;
   p->ws_part = ((size_t)p->W * sizeof(Shared) + 255) / 256 * 256;
   p->ws_bytes = p->ws_part + (size_t)2 * p->W * p->max_rows * (dp + 2) * sizeof(float);
@@ -488,6 +904,13 @@ int dnb_paged_attn_forward(const dnb_paged_attn* p, const void* q, const void* k
   A.W = p->W;
   A.pages = c.pages; A.rq = p->d.rows_q; A.qs = p->d.q_stride; A.ps = c.page_stride; A.rs = c.row_stride; A.hs = c.head_stride;
   A.c = p->d.scale * kLog2e;
+  // m / per = umulhi(m, floor(2^(31 + l) / per) + 1) >> (l - 1) for 2^(l - 1) < per <= 2^l, m below 2^31
+  if (A.per > 1) {
+    int l = 1;
+    while ((1 << l) < A.per) ++l;
+    A.per_mul = (uint32_t)(((uint64_t)1 << (31 + l)) / A.per + 1);
+    A.per_shift = l - 1;
+  }
   const hipError_t e = c.dtype == DNB_BF16 ? run_paged_db<__bf16>(A, p->max_rows, (hipStream_t)stream)
                                            : run_paged_db<float>(A, p->max_rows, (hipStream_t)stream);
   return e == hipSuccess ? DNB_OK : DNB_E_LAUNCH;
