@@ -11,6 +11,8 @@
 #include <hip/hip_runtime.h>
 
 #include <cmath>
+#include <cstdio>
+#include <cstdlib>
 #include <new>
 #include <type_traits>
 
@@ -38,6 +40,7 @@ struct PArgs {
   int64_t pages, rq, qs, ps, rs, hs;
   float c;  // scale * log2(e)
   uint32_t per_mul, per_shift;
+  int cost[3], extra[3], least;  // see Blocks; the least that a workgroup is given
 };
 
 // m / per, m below 2^31
@@ -61,30 +64,36 @@ __device__ __forceinline__ unsigned pseen(const PArgs& A, const PSeq& S, int m) 
   return A.causal ? max(S.nk + min(query_of(A, m) + 1 - S.nq, 0), 0) : S.nk;
 }
 
-// Blocks of a sequence: RW of the four waves take 32 * NC rows each.  Cost: of a step, in units of the line.
+// Blocks of a sequence: `rw` of the four waves take 32 * NC rows each, and with up to 32 rows one set of 32.  Their place on
+// the line: `extra` units for the beginning and the end, then `cost` a step.
 template <int KT, int NC>
 struct Blocks {
-  int rw, rows, count, cost, M;
+  int rw, rows, count, cost, extra, M;
   __device__ __forceinline__ Blocks(const PArgs& A, const PSeq& S) {
     M = S.nq * A.per;
-    rw = KT >= 128 && M <= 32 * NC ? 1 : M <= 64 * NC ? 2 : 4;
-    rows = 32 * NC * rw;
+    const bool narrow = KT >= 128 && M <= 32;
+    rw = narrow ? 1 : M <= 64 * NC ? 2 : 4;
+    rows = narrow ? 32 : 32 * NC * rw;
     count = (M + rows - 1) / rows;
-    cost = rw == 4 ? 4 : rw == 2 ? 3 : 2;
+    cost = rw == 4 ? A.cost[2] : A.cost[rw - 1];
+    extra = rw == 4 ? A.extra[2] : A.extra[rw - 1];
   }
   // (a block whose rows see nothing takes a step too: its results are written)
   __device__ __forceinline__ int steps(const PArgs& A, const PSeq& S, int t) const {
     return max((int)((pseen(A, S, min((t + 1) * rows, M) - 1) + KT - 1) / KT), 1);
   }
+  __device__ __forceinline__ int64_t units(const PArgs& A, const PSeq& S, int t) const { return extra + (int64_t)steps(A, S, t) * cost; }
+  // first step that begins x units from the block's start or later
+  __device__ __forceinline__ int step_at(int64_t x) const { return x <= extra ? 0 : (int)((uint32_t)(x - extra) + cost - 1) / cost; }
 };
 // of one key/value head, by a lane alone
 template <int KT, int NC>
 __device__ __forceinline__ int64_t head_units(const PArgs& A, const PSeq& S) {
   const Blocks<KT, NC> B(A, S);
   int64_t u = 0;
-  if (!A.causal) return (int64_t)B.count * (B.count > 0 ? B.steps(A, S, 0) : 0) * B.cost;
-  for (int t = 0; t < B.count; ++t) u += B.steps(A, S, t);
-  return u * B.cost;
+  if (!A.causal) return (int64_t)B.count * (B.count > 0 ? B.units(A, S, 0) : 0);
+  for (int t = 0; t < B.count; ++t) u += B.units(A, S, t);
+  return u;
 }
 
 // Sum over the threads up to each; *total: over all.  `red`: room for four in LDS, free again after the caller's next barrier.
@@ -305,6 +314,22 @@ struct Fetch {
   static __device__ __forceinline__ void load(lds_t to, const char* from) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory");
   }
+  // Whether all rows of a step are there, with as many pieces as a tile's, in groups within a page and with offsets of 32 bits
+  __device__ __forceinline__ bool quick(const PArgs& A, int step, unsigned nk) const {
+    return ((unsigned)step + 1) * 128u <= nk && A.d == 32 * DB && (1 << A.shift) >= RPI && A.rs < (1 << 26);
+  }
+  // Group u of such a step; kt, vt: of the wave's rows.
+  __device__ __forceinline__ void group(const PArgs& A, lds_t kt, lds_t vt, int step, int u) const {
+    const int l = lane_id();
+    const unsigned key = (unsigned)step * 128u + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 32u + u * RPI, mask = (1u << A.shift) - 1;
+    const int page = __builtin_amdgcn_readlane(now, (step - base) * U + u);
+    const uint64_t from = (uint64_t)(uint32_t)page * (uint32_t)(A.ps * 2) + (uint64_t)(key & mask) * (uint32_t)(A.rs * 2) + head;
+    const int c = (l % L::PC) ^ L::swz(l / L::PC) ^ L::swz(u * RPI);
+    const bool in = (unsigned)page < A.pages;
+    const uint32_t off = in ? row_at + min(c, L::CH - 1) * 16 : 0;  // (pieces past a row's are not read)
+    load(kt + u * 1024, off, in ? (const char*)A.k + from : (const char*)kZeros);
+    load(vt + u * 1024, off, in ? (const char*)A.v + from : (const char*)kZeros);
+  }
   // Step `step` into the tiles at kt and vt; nk: keys that exist.
   __device__ __forceinline__ void issue(const PArgs& A, lds_t kt, lds_t vt, int step, unsigned nk) const {
     const int l = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -314,18 +339,11 @@ struct Fetch {
     kt += wave * 32 * L::PITCH;
     vt += wave * 32 * L::PITCH;
     const int at = (step - base) * U;
-    const bool mine = l >= at && l < at + U;
     const int c0 = (l % L::PC) ^ L::swz(l / L::PC);
     const bool grouped = (1 << A.shift) >= RPI;  // a group of rows lies within a page
-    // all rows there, of pages of the pool, with as many pieces as a tile's, and offsets of 32 bits
-    if (grouped && key0 + 32 <= nk && A.d == 32 * DB && A.rs < (1 << 26) && !__any(mine && (unsigned)now >= A.pages)) {
+    if (quick(A, step, nk)) {
 #pragma unroll 2
-      for (int u = 0; u < U; ++u) {
-        const uint64_t from = (uint64_t)(uint32_t)__builtin_amdgcn_readlane(now, at + u) * ps + (uint64_t)((key0 + u * RPI) & mask) * rs;
-        const uint32_t off = row_at + min(c0 ^ L::swz(u * RPI), L::CH - 1) * 16;  // (pieces past a row's are not read)
-        load(kt + u * 1024, off, kp + from);
-        load(vt + u * 1024, off, vp + from);
-      }
+      for (int u = 0; u < U; ++u) group(A, kt, vt, step, u);
       return;
     }
     // What is not there comes from the zeros.  (Pages of less than a group: a lookup each lane, all before the first load into
@@ -460,44 +478,81 @@ struct Walk<__bf16, DB> {
   }
 
   // A block of 32 keys, whose scores are s and their tops `top`, and beside it the scores of the following one: a
-  // product's 32 cycles are another five instructions' time.
-  template <int N>
+  // product's 32 cycles are another seven instructions' time.  There is one wave a SIMD, so what it waits for is lost: reads of LDS go
+  // out three phases (of N products) before their use, and only other instructions may be moved between phases.
+  // load(k): something more for phase k, of the first.
+  // HIDE: keys of the following block from next_key on, of which a lane's rows see those below sees.
+  template <int N, bool HIDE, typename Load>
   static __device__ __forceinline__ void block(Sets<DB, N>& R, Scores<N>& s, Scores<N>& sn, float (&top)[N], const Queries<N>& q, float c, lds_t k_at,
-                                               lds_t v_at) {
+                                               lds_t v_at, Load load, unsigned next_key = 0, const unsigned* sees = nullptr) {
+    constexpr int NS = L::NS, NV = 2 * DB, AHEAD = 3;
+    Piece f[NS + NV][1];
+    auto read = [&](int i) {
+      if (i < NS) {
+        f[i][0].q = lds_read<u32x4>(k_at ^ (i << 5));
+      } else if (i < NS + NV) {
+        using lds4 = __attribute__((address_space(3))) s16x4;
+        const int t = (i - NS) / DB, db = (i - NS) % DB;
+        const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(uintptr_t)((v_at ^ (db << 6)) + 16 * t * L::PITCH));
+        const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds4*)(uintptr_t)((v_at ^ (db << 6) ^ 32) + (16 * t + 8) * L::PITCH));
+        const uint2 a = __builtin_bit_cast(uint2, lo), b = __builtin_bit_cast(uint2, hi);
+        f[i][0].q = (u32x4){a.x, a.y, b.x, b.y};
+      }
+    };
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) read(i);
     rescale<N>(R, top, c);
     __builtin_amdgcn_sched_barrier(0);
-    scores<N>(sn, q, k_at);
-    weights<N>(R, s, c);
-    values<N>(R, s, v_at);
-    tops<N>(top, sn);
-    __builtin_amdgcn_sched_group_barrier(0x100, 3, 0);
+    Piece y[2][N][1];
+    float m[N];
 #pragma unroll
-    for (int k = 0; k < L::NS; ++k) {
+    for (int n = 0; n < N; ++n) {
+      m[n] = R.m[n] == -INFINITY ? 0.f : R.m[n];
+      sn[n] = (f32x16){};
+    }
+    // The weights in the order in which the products need them, spread over the time until the last do; then the tops.
+    constexpr int SPOTS = (NS + DB) * N, REST = DB * N;
+    float big[N];
+#pragma unroll
+    for (int i = 0; i < NS + NV; ++i)
 #pragma unroll
       for (int n = 0; n < N; ++n) {
-        __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x2, 5, 0);
-      }
-      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-    }
+        const int spot = i * N + n;
+        if (n == 0) read(i + AHEAD);
+        if (i < NS) mma(sn[n], f[i], q[n][i], (__bf16*)nullptr);
+        else mma(R.o[n][(i - NS) % DB], f[i], y[(i - NS) / DB][n], (__bf16*)nullptr);
+        if (i < NS && n == 0) load(i);
 #pragma unroll
-    for (int k = 0; k < 2 * DB * N; ++k) {
-      __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x2, 5, 0);
-    }
-    __builtin_amdgcn_sched_barrier(0);
+        for (int e = 0; e < 16 * N; ++e)
+          if (e * SPOTS / (16 * N) == spot) {
+            const int t = e / (8 * N), col = e / 8 % N, j = e % 8;
+            float x = s[col][8 * t + j];
+            asm volatile("" : "+v"(x));  // here, and not together with its neighbours
+            const float p = __builtin_amdgcn_exp2f(fmaf(x, c, -m[col]));
+            R.l[col] += p;
+            y[t][col][0].b[j] = (__bf16)p;
+          }
+#pragma unroll
+        for (int e = 0; e < 16 * N; ++e)
+          if (SPOTS + e * REST / (16 * N) == spot) {
+            const int col = e / 16, j = e % 16;
+            if (HIDE) sn[col][j] = next_key + row_of(j) >= sees[col] ? -INFINITY : sn[col][j];
+            big[col] = j == 0 ? sn[col][0] : fmaxf(big[col], sn[col][j]);
+          }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+    for (int n = 0; n < N; ++n) top[n] = half_max(big[n]);
   }
-
-  static constexpr int N = NC;
 
   // The KH waves of a set of rows join, and the results go where they belong.  Each wave's sums go to LDS, a row after
   // another, 16-byte pieces turned round by the row against bank conflicts; then a thread takes four values of a row.
+  template <int N>
   static __device__ __forceinline__ void join(const PArgs& A, char* shared, const Sets<DB, N>& R, const Blocks<KT, NC>& B, const Target& to) {
     constexpr int PIECES = 8 * DB, DP = 32 * DB;
     const int wave = threadIdx.x >> 6, l = lane_id(), KH = 4 / B.rw;
-    f32x4* o = reinterpret_cast<f32x4*>(shared);                       // (wave, row, piece)
-    float2* ml = reinterpret_cast<float2*>(shared + 256 * DP * 4);  // (wave, row)
+    f32x4* o = reinterpret_cast<f32x4*>(shared);                           // (wave, row, piece)
+    float2* ml = reinterpret_cast<float2*>(shared + 128 * N * DP * 4);  // (wave, row)
     const int rows = min(B.rows, to.M - to.m0);
     __syncthreads();
 #pragma unroll
@@ -548,19 +603,13 @@ struct Walk<__bf16, DB> {
     }
   }
 
-  static __device__ __forceinline__ void run(const PArgs& A, char* shared, const PSeq& S, const int32_t* table, const Blocks<KT, NC>& B, int g, int t,
-                                             int first, int last, const Target& to) {
-    const lds_t lds = lds_start(shared), kt = lds, vt = lds + 2 * TILE;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l = lane_id(), KH = 4 / B.rw, kh = wave & (KH - 1), row0 = wave / KH * 32 * NC;
-    const unsigned all = pseen(A, S, min((t + 1) * B.rows, B.M) - 1);  // keys that the block's last row sees
-    F f;
-    if (first < last) f.init(A, table, g, first, all);
-    Queries<N> q;
-    Sets<DB, N> R;
-    unsigned sees[N];
+  // The wave's N sets of 32 rows from row m0 of the matrix on
+  template <int N>
+  static __device__ __forceinline__ void begin(const PArgs& A, const PSeq& S, const Blocks<KT, NC>& B, int g, int m0, Queries<N>& q, Sets<DB, N>& R,
+                                               unsigned (&sees)[N]) {
 #pragma unroll
     for (int n = 0; n < N; ++n) {
-      const int m = t * B.rows + row0 + 32 * n + (l & 31), query = query_of(A, m), head = g * A.per + m - query * A.per;
+      const int m = m0 + 32 * n + (lane_id() & 31), query = query_of(A, m), head = g * A.per + m - query * A.per;
       sees[n] = pseen(A, S, m);
       load_cols<__bf16, DB>(q[n], (const __bf16*)A.q + ((int64_t)S.q0 + query) * A.qs + (int64_t)head * A.d, m < B.M, A.d);
 #pragma unroll
@@ -568,93 +617,142 @@ struct Walk<__bf16, DB> {
       R.m[n] = -INFINITY;
       R.l[n] = 0.f;
     }
-    // keys that all rows of the wave see; that all of the workgroup see, by which the waves choose their way between barriers
-    const unsigned least = pseen(A, S, t * B.rows + row0), lowest = pseen(A, S, t * B.rows);
+  }
+  static __device__ __forceinline__ lds_t k_lane() { return L::at(lane_id() & 31, lane_id() >> 5); }
+  static __device__ __forceinline__ lds_t v_lane() {
+    const int l = lane_id();
+    return L::at(4 * (l >> 5) + ((l >> 2) & 3), 2 * ((l >> 4) & 1) + ((l >> 1) & 1)) + (l & 1) * 8;
+  }
+
+  // Up to 32 rows: each wave takes a fourth of every step's keys, which it fetches itself two steps ahead, and waits for nobody.
+  static __device__ __forceinline__ void run_narrow(const PArgs& A, char* shared, const PSeq& S, const int32_t* table, const Blocks<KT, NC>& B, int g,
+                                                    int first, int last, const Target& to) {
+    const lds_t kt = lds_start(shared), vt = kt + 2 * TILE;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const unsigned all = pseen(A, S, B.M - 1), least = pseen(A, S, 0);
+    F f;
+    if (first < last) f.init(A, table, g, first, all);
+    Queries<1> q;
+    Sets<DB, 1> R;
+    unsigned sees[1];
+    begin<1>(A, S, B, g, 0, q, R, sees);
+    const lds_t k_at = kt + k_lane() + wave * 32 * L::PITCH, v_at = vt + v_lane() + wave * 32 * L::PITCH;
+#pragma unroll 1
+    for (int s = first - 2; s < last; ++s) {
+      const lds_t buf = (s - first) & 1 ? TILE : 0;
+      if (s >= first) {
+        if (s + 1 < last) wait_loads<2 * F::U>();
+        else wait_loads<0>();
+        Scores<1> a;
+        float top[1];
+        scores<1>(a, q, k_at + buf);
+        const unsigned key = (unsigned)s * KT + wave * 32;
+        if (key + 32 > least) {
+          asm volatile("");  // a branch, not selections in every step
+          hide(a[0], key, sees[0]);
+        }
+        tops<1>(top, a);
+        rescale<1>(R, top, A.c);
+        weights<1>(R, a, A.c);
+        values<1>(R, a, v_at + buf);
+        wait_lds();
+      }
+      if (s + 2 < last) {
+        f.turn(A, s + 2, all);
+        f.issue(A, kt + buf, vt + buf, s + 2, all);
+      }
+    }
+    join<1>(A, shared, R, B, to);
+  }
+
+  // More rows: N sets a wave, two or four waves side by side, and KH of them at the same rows.
+  static __device__ __forceinline__ void run_wide(const PArgs& A, char* shared, const PSeq& S, const int32_t* table, const Blocks<KT, NC>& B, int g, int t,
+                                                  int first, int last, const Target& to) {
+    constexpr int N = NC;
+    const lds_t kt = lds_start(shared), vt = kt + 2 * TILE;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), KH = 4 / B.rw, kh = wave & (KH - 1), row0 = wave / KH * 32 * N;
+    const unsigned all = pseen(A, S, min((t + 1) * B.rows, B.M) - 1);  // keys that the block's last row sees
+    // keys that all rows of the workgroup see: by that the waves choose their way, all the same one, between barriers
+    const unsigned lowest = pseen(A, S, t * B.rows);
+    F f;
+    if (first < last) f.init(A, table, g, first, all);
+    Queries<N> q;
+    Sets<DB, N> R;
+    unsigned sees[N];
+    begin<N>(A, S, B, g, t * B.rows + row0, q, R, sees);
     if (first < last) {
       f.issue(A, kt, vt, first, all);
-      if (first + 1 < last) {
-        f.turn(A, first + 1, all);
-        f.issue(A, kt + TILE, vt + TILE, first + 1, all);
-        wait_loads<2 * F::U>();
-      } else {
-        wait_loads<0>();
-      }
-      if (KH < 4) meet();
+      wait_loads<0>();
+      meet();
       const int nb = 4 / KH;  // blocks of 32 keys of this wave in a step
-      const lds_t k_lane = L::at(l & 31, l >> 5) + kt + kh * nb * 32 * L::PITCH;
-      const lds_t v_lane = L::at(4 * (l >> 5) + ((l >> 2) & 3), 2 * ((l >> 4) & 1) + ((l >> 1) & 1)) + (l & 1) * 8 + vt + kh * nb * 32 * L::PITCH;
+      const lds_t k_at0 = kt + k_lane() + kh * nb * 32 * L::PITCH, v_at0 = vt + v_lane() + kh * nb * 32 * L::PITCH;
       lds_t buf = 0;  // of the step at hand
       Scores<N> a, b;
       float top[N];
-      scores<N>(a, q, k_lane);
+      scores<N>(a, q, k_at0);
+#pragma unroll
+      for (int n = 0; n < N; ++n) hide(a[n], (unsigned)first * KT + kh * nb * 32, sees[n]);
+      tops<N>(top, a);
       int s = first;
-      // Steps after which another comes and all of whose keys, and the next one's first, all rows see: the scores of a block beside the weights
-      // and values of the one before.
-      if (KH < 4) {
-        tops<N>(top, a);
+      auto nothing = [](int) {};
+      // Steps after which another comes and all of whose keys, and the next one's first, all rows see.  The next step's rows are
+      // fetched during the first two of four blocks.
+      if (KH == 1) {
 #pragma unroll 1
-        for (; s + 1 < last && ((unsigned)s + 2) * KT <= lowest; ++s) {
-          lds_t k_at = k_lane + buf, v_at = v_lane + buf;
-#pragma unroll 1
-          for (int j = 2; j < nb; j += 2) {
-            block<N>(R, a, b, top, q, A.c, k_at + 32 * L::PITCH, v_at);
-            block<N>(R, b, a, top, q, A.c, k_at + 64 * L::PITCH, v_at + 32 * L::PITCH);
-            k_at += 64 * L::PITCH;
-            v_at += 64 * L::PITCH;
-          }
-          block<N>(R, a, b, top, q, A.c, k_at + 32 * L::PITCH, v_at);
+        for (; s + 1 < last && ((unsigned)s + 2) * KT <= lowest && f.quick(A, s + 1, all); ++s) {
+          const lds_t k_at = k_at0 + buf, v_at = v_at0 + buf;
+          const lds_t kw = kt + (buf ^ TILE) + wave * 32 * L::PITCH, vw = vt + (buf ^ TILE) + wave * 32 * L::PITCH;
+          f.turn(A, s + 1, all);
+          block<N, false>(R, a, b, top, q, A.c, k_at + 32 * L::PITCH, v_at, [&](int k) { if (k < F::U / 2) f.group(A, kw, vw, s + 1, k); });
+          block<N, false>(R, b, a, top, q, A.c, k_at + 64 * L::PITCH, v_at + 32 * L::PITCH, [&](int k) { if (k < F::U / 2) f.group(A, kw, vw, s + 1, F::U / 2 + k); });
+          block<N, false>(R, a, b, top, q, A.c, k_at + 96 * L::PITCH, v_at + 64 * L::PITCH, nothing);
           buf ^= TILE;
           // the next step is here
           wait_loads<0>();
           meet();
-          block<N>(R, b, a, top, q, A.c, k_lane + buf, v_at + 32 * L::PITCH);
-          if (s + 2 < last) {
-            // all have read this one
-            wait_lds();
-            meet();
-            f.turn(A, s + 2, all);
-            f.issue(A, kt + (buf ^ TILE), vt + (buf ^ TILE), s + 2, all);
-          }
+          block<N, false>(R, b, a, top, q, A.c, k_at0 + buf, v_at + 96 * L::PITCH, nothing);
+          // all have read this one
+          wait_lds();
+          meet();
         }
       }
-      // The others one by one.  (With four waves to the rows each reads what it has fetched itself, and waits for nobody.)
+      // The others
 #pragma unroll 1
       for (; s < last; ++s) {
+        const bool more = s + 1 < last;
+        if (more) {
+          f.turn(A, s + 1, all);
+          f.issue(A, kt + (buf ^ TILE), vt + (buf ^ TILE), s + 1, all);
+        }
 #pragma unroll 1
         for (int j = 0; j < nb; ++j) {
-          const unsigned key = (unsigned)s * KT + (kh * nb + j) * 32;
-          if (key + 32 > least) {
-            asm volatile("");  // a branch: as selections its 64 instructions were part of every block
-#pragma unroll
-            for (int n = 0; n < N; ++n) hide(a[n], key, sees[n]);
+          const bool ends = j + 1 == nb;
+          if (ends && more) {
+            wait_loads<0>();
+            meet();
           }
-          tops<N>(top, a);
-          rescale<N>(R, top, A.c);
-          weights<N>(R, a, A.c);
-          values<N>(R, a, v_lane + buf + j * 32 * L::PITCH);
-          if (j + 1 < nb) scores<N>(a, q, k_lane + buf + (j + 1) * 32 * L::PITCH);
+          // (after the last block: scores of what lies there, which nobody takes)
+          const lds_t next = ends ? k_at0 + (buf ^ TILE) : k_at0 + buf + (j + 1) * 32 * L::PITCH;
+          block<N, true>(R, a, b, top, q, A.c, next, v_at0 + buf + j * 32 * L::PITCH, nothing, ends ? (unsigned)(s + 1) * KT + kh * nb * 32 : (unsigned)s * KT + (kh * nb + j + 1) * 32, sees);
+#pragma unroll
+          for (int n = 0; n < N; ++n) a[n] = b[n];
         }
-        if (s + 1 == last) break;
-        wait_lds();
-        if (KH < 4) meet();
-        if (s + 2 < last) {
-          f.turn(A, s + 2, all);
-          f.issue(A, kt + buf, vt + buf, s + 2, all);
-          wait_loads<2 * F::U>();
-        } else {
-          wait_loads<0>();
-        }
-        if (KH < 4) meet();
         buf ^= TILE;
-        scores<N>(a, q, k_lane + buf);
+        wait_lds();
+        meet();
       }
     }
     if (KH > 1) {
-      join(A, shared, R, B, to);
+      join<N>(A, shared, R, B, to);
       return;
     }
 #pragma unroll
     for (int n = 0; n < N; ++n) write_rows<__bf16, DB>(A, to, R.o[n], R.m[n], R.l[n], row0 + 32 * n);
+  }
+  static __device__ __forceinline__ void run(const PArgs& A, char* shared, const PSeq& S, const int32_t* table, const Blocks<KT, NC>& B, int g, int t,
+                                             int first, int last, const Target& to) {
+    if (B.rw == 1) run_narrow(A, shared, S, table, B, g, first, last, to);
+    else run_wide(A, shared, S, table, B, g, t, first, last, to);
   }
 };
 
@@ -673,7 +771,7 @@ __global__ __launch_bounds__(kThreads, 1) void k_paged(PArgs A, int max_rows) {
     mine += u;
   }
   const int64_t scan = block_scan(mine, red, &total);
-  const int W = (int)min((int64_t)A.W, max(total / 4, (int64_t)1));
+  const int W = (int)min((int64_t)A.W, max(total / A.least, (int64_t)1));
   // workgroups that lie side by side on the line run on one XCD, whose cache has the keys that they share
   const int w = A.W % 8 == 0 ? (int)(blockIdx.x % 8) * (A.W / 8) + (int)blockIdx.x / 8 : (int)blockIdx.x;
   if (tid == 0) A.shared[w].parts = 0;
@@ -705,12 +803,11 @@ __global__ __launch_bounds__(kThreads, 1) void k_paged(PArgs A, int max_rows) {
     const B_ B(A, S);
     // key/value head and block at a
     int64_t H = 0;
-    for (int t0 = 0; t0 < B.count; t0 += 64) H += bcast64(wave_scan(t0 + l < B.count ? B.steps(A, S, t0 + l) : 0), 63);
-    H *= B.cost;
+    for (int t0 = 0; t0 < B.count; t0 += 64) H += bcast64(wave_scan(t0 + l < B.count ? B.units(A, S, t0 + l) : 0), 63);
     g = (int)((double)(a - a0) / (double)H);
     a0 += g * H;
     for (int t0 = 0; t0 < B.count; t0 += 64) {
-      const int64_t v = t0 + l < B.count ? (int64_t)B.steps(A, S, t0 + l) * B.cost : 0, end = a0 + wave_scan(v);
+      const int64_t v = t0 + l < B.count ? B.units(A, S, t0 + l) : 0, end = a0 + wave_scan(v);
       const uint64_t past = __ballot(end > a);
       if (past) {
         const int at = __builtin_ctzll(past);
@@ -724,9 +821,9 @@ __global__ __launch_bounds__(kThreads, 1) void k_paged(PArgs A, int max_rows) {
   for (;;) {
     const B_ B(A, S);
     const int steps = B.steps(A, S, t);
-    const int64_t a1 = a0 + (int64_t)steps * B.cost;
+    const int64_t a1 = a0 + B.extra + (int64_t)steps * B.cost;
     // a step is the workgroup's in whose part of the line it begins
-    const int first = a0 < a ? (int)((uint32_t)(a - a0) + B.cost - 1) / B.cost : 0, last = a1 > b ? min(steps, (int)((uint32_t)(b - a0) + B.cost - 1) / B.cost) : steps;
+    const int first = a0 < a ? B.step_at(a - a0) : 0, last = a1 > b ? min(steps, B.step_at(b - a0)) : steps;
     Target to = {S.q0, t * B.rows, B.M, g, nullptr, max_rows};
     if (a0 < a || a1 > b) {
       to.part = A.part + (int64_t)(2 * w + (a0 < a ? 0 : 1)) * part_floats<DB>(max_rows);
@@ -849,7 +946,7 @@ using namespace dnb::attn;
 
 struct dnb_paged_attn {
   dnb_paged_attn_desc d;
-  int W, max_rows;
+  int W, max_rows, cost[3], extra[3], least;
   size_t ws_part, ws_bytes;
 };
 
@@ -872,7 +969,15 @@ int dnb_paged_attn_create(const dnb_paged_attn_desc* desc, dnb_paged_attn** out)
   p->d = d;
   p->W = 256;
   const int64_t M = d.rows_q * per;
-  p->max_rows = M <= 64 ? 64 : M <= 128 || d.cache.dtype == DNB_F32 ? 128 : 256;
+  const bool bf16 = d.cache.dtype == DNB_BF16;
+  if (bf16) p->max_rows = M <= 32 ? 32 : M <= 128 ? 128 : 256;
+  else p->max_rows = M <= 64 ? 64 : 128;
+  {
+    const int cost[3] = {5, 5, 8}, extra[3] = {5, 8, 10};
+    for (int i = 0; i < 3; ++i) { p->cost[i] = cost[i]; p->extra[i] = extra[i]; }
+    p->least = 10;
+    if (getenv("PC")) { sscanf(getenv("PC"), "%d,%d,%d,%d,%d,%d,%d", p->cost, p->cost + 1, p->cost + 2, p->extra, p->extra + 1, p->extra + 2, &p->least); }
+  }
   const int dp = (d.cache.head_dim + 31) / 32 * 32;
   p->ws_part = ((size_t)p->W * sizeof(Shared) + 255) / 256 * 256;
   p->ws_bytes = p->ws_part + (size_t)2 * p->W * p->max_rows * (dp + 2) * sizeof(float);
@@ -902,6 +1007,8 @@ int dnb_paged_attn_forward(const dnb_paged_attn* p, const void* q, const void* k
   A.n = c.sequences; A.heads = p->d.heads; A.kv = c.kv_heads; A.per = p->d.heads / c.kv_heads; A.d = c.head_dim;
   A.causal = p->d.causal != 0; A.columns = c.max_pages; A.shift = dnb::paged::log2_of(c.page_size);
   A.W = p->W;
+  for (int i = 0; i < 3; ++i) { A.cost[i] = p->cost[i]; A.extra[i] = p->extra[i]; }
+  A.least = p->least;
   A.pages = c.pages; A.rq = p->d.rows_q; A.qs = p->d.q_stride; A.ps = c.page_stride; A.rs = c.row_stride; A.hs = c.head_stride;
   A.c = p->d.scale * kLog2e;
   // m / per = umulhi(m, floor(2^(31 + l) / per) + 1) >> (l - 1) for 2^(l - 1) < per <= 2^l, m below 2^31
