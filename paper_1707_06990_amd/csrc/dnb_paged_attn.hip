@@ -11,8 +11,6 @@
 #include <hip/hip_runtime.h>
 
 #include <cmath>
-#include <cstdio>
-#include <cstdlib>
 #include <new>
 #include <type_traits>
 
@@ -277,98 +275,110 @@ struct Sets {
 
 // Keys and values of a step on their way from the pages to LDS, without passing through registers: a load instruction of
 // a wave fills 1 KB of LDS, RPI rows, lane after lane; which piece of its row a lane fetches is turned round so that the tile's
-// order comes out.  The wave has rows wave * 32 .. + 31, U instructions for K and as many for V.
+// order comes out.  The wave has rows wave * 32 .. + 31, U instructions for K and as many for V.  Where its groups of RPI rows begin
+// is computed for WINDOW steps at once, a group a lane.
 template <int DB>
 struct Fetch {
   using L = Tile<__bf16, DB>;
-  static constexpr int RPI = 64 / L::PC, U = 32 / RPI, WINDOW = 64 / U;  // WINDOW: steps whose pages one register's lanes hold
-  int now, next;      // pages of row groups: lane i: step base + i / U, group i % U; of this window and the following
+  static constexpr int RPI = 64 / L::PC, U = 32 / RPI, WINDOW = 64 / U;
+  uint64_t from;      // lane i: the first key row of step base + i / U, group i % U
+  int64_t apart_by;   // from a key's bytes to its value's
+  int clean;          // all pages of the window, of all waves, are of the pool
   int base;           // the window's first step
-  uint32_t row_at;    // bytes from the group's first row to the lane's
+  int next;           // the following window's pages
+  int next_clean;
+  uint32_t row_at, c16;  // bytes from a group's first row to the lane's; the lane's piece in group 0
   const int32_t* table;
   int64_t head;       // bytes
 
-  __device__ __forceinline__ int window(const PArgs& A, int step, unsigned nk) const {
+  __device__ __forceinline__ unsigned key_of(int step, int wave) const {
     const int l = lane_id();
-    const unsigned key = (unsigned)(step + l / U) * 128u + (threadIdx.x >> 6) * 32u + (l % U) * RPI;
-    return key < nk ? table[key >> A.shift] : 0;
+    return (unsigned)(step + l / U) * 128u + wave * 32u + (l % U) * RPI;
+  }
+  __device__ __forceinline__ void look(const PArgs& A, int step, unsigned nk) {
+    bool in = true;
+    const int mine = threadIdx.x >> 6;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const unsigned key = key_of(step, w);
+      const int page = key < nk ? table[key >> A.shift] : 0;
+      in = in && (unsigned)page < A.pages;
+      if (w == mine) next = page;
+    }
+    next_clean = __ballot(!in) == 0;
+  }
+  __device__ __forceinline__ void place(const PArgs& A) {
+    from = (uint64_t)A.k + head + (uint64_t)(uint32_t)next * (uint32_t)(A.ps * 2) +
+           (uint64_t)(key_of(base, threadIdx.x >> 6) & ((1u << A.shift) - 1)) * (uint32_t)(A.rs * 2);
+    clean = next_clean;
   }
   __device__ __forceinline__ void init(const PArgs& A, const int32_t* t, int g, int first, unsigned nk) {
     const int l = lane_id();
     table = t;
     head = (int64_t)g * A.hs * 2;
+    apart_by = (const char*)A.v - (const char*)A.k;
     base = first;
     row_at = (uint32_t)(l / L::PC) * (uint32_t)(A.rs * 2);
-    now = window(A, first, nk);
-    next = window(A, first + WINDOW, nk);
+    c16 = (uint32_t)((l % L::PC) ^ L::swz(l / L::PC)) * 16;
+    look(A, first, nk);
+    place(A);
+    look(A, first + WINDOW, nk);
   }
   __device__ __forceinline__ void turn(const PArgs& A, int step, unsigned nk) {
     if (step < base + WINDOW) return;
     base += WINDOW;
-    now = next;
-    next = window(A, base + WINDOW, nk);
+    place(A);
+    look(A, base + WINDOW, nk);
   }
-  static __device__ __forceinline__ void load(lds_t to, uint32_t voff, const char* from) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(voff), "s"(from) : "memory");
+  static __device__ __forceinline__ void load(lds_t to, uint32_t voff, uint64_t from) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(voff), "s"(from) : "memory");
   }
   static __device__ __forceinline__ void load(lds_t to, const char* from) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(to), "v"(from) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(from) : "memory");
   }
-  // Whether all rows of a step are there, with as many pieces as a tile's, in groups within a page and with offsets of 32 bits
+  // Whether all rows of a step (of this window) are there, with as many pieces as a tile's, in groups within a page and with
+  // offsets of 32 bits.  The same for all waves.
   __device__ __forceinline__ bool quick(const PArgs& A, int step, unsigned nk) const {
-    return ((unsigned)step + 1) * 128u <= nk && A.d == 32 * DB && (1 << A.shift) >= RPI && A.rs < (1 << 26);
+    return clean && ((unsigned)step + 1) * 128u <= nk && A.d == 32 * DB && (1 << A.shift) >= RPI && A.rs < (1 << 26);
   }
   // Group u of such a step; kt, vt: of the wave's rows.
-  __device__ __forceinline__ void group(const PArgs& A, lds_t kt, lds_t vt, int step, int u) const {
-    const int l = lane_id();
-    const unsigned key = (unsigned)step * 128u + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) * 32u + u * RPI, mask = (1u << A.shift) - 1;
-    const int page = __builtin_amdgcn_readlane(now, (step - base) * U + u);
-    const uint64_t from = (uint64_t)(uint32_t)page * (uint32_t)(A.ps * 2) + (uint64_t)(key & mask) * (uint32_t)(A.rs * 2) + head;
-    const int c = (l % L::PC) ^ L::swz(l / L::PC) ^ L::swz(u * RPI);
-    const bool in = (unsigned)page < A.pages;
-    const uint32_t off = in ? row_at + min(c, L::CH - 1) * 16 : 0;  // (pieces past a row's are not read)
-    load(kt + u * 1024, off, in ? (const char*)A.k + from : (const char*)kZeros);
-    load(vt + u * 1024, off, in ? (const char*)A.v + from : (const char*)kZeros);
+  __device__ __forceinline__ void group(lds_t kt, lds_t vt, int step, int u) const {
+    const int i = (step - base) * U + u;
+    const uint64_t f = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(from >> 32), i) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)from, i);
+    uint32_t c = c16 ^ (uint32_t)(L::swz(u * RPI) * 16);
+    if (L::CH < L::PC) c = min(c, (uint32_t)(L::CH - 1) * 16);  // (pieces past a row's are not read)
+    load(kt + u * 1024, row_at + c, f);
+    load(vt + u * 1024, row_at + c, f + apart_by);
   }
   // Step `step` into the tiles at kt and vt; nk: keys that exist.
   __device__ __forceinline__ void issue(const PArgs& A, lds_t kt, lds_t vt, int step, unsigned nk) const {
     const int l = lane_id(), wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const unsigned key0 = (unsigned)step * 128u + wave * 32u, mask = (1u << A.shift) - 1;
-    const char *kp = (const char*)A.k + head, *vp = (const char*)A.v + head;
-    const uint32_t ps = (uint32_t)(A.ps * 2), rs = (uint32_t)(A.rs * 2);  // (both at most 2^31)
     kt += wave * 32 * L::PITCH;
     vt += wave * 32 * L::PITCH;
-    const int at = (step - base) * U;
-    const int c0 = (l % L::PC) ^ L::swz(l / L::PC);
-    const bool grouped = (1 << A.shift) >= RPI;  // a group of rows lies within a page
     if (quick(A, step, nk)) {
 #pragma unroll 2
-      for (int u = 0; u < U; ++u) group(A, kt, vt, step, u);
+      for (int u = 0; u < U; ++u) group(kt, vt, step, u);
       return;
     }
-    // What is not there comes from the zeros.  (Pages of less than a group: a lookup each lane, all before the first load into
-    // LDS, for which a later one would wait.)
+    // What is not there comes from the zeros.  (The lookups all before the first load into LDS, for which a later one would wait.)
+    const unsigned key0 = (unsigned)step * 128u + wave * 32u, mask = (1u << A.shift) - 1;
     int pages[U];
-    if (!grouped) {
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const unsigned key = key0 + u * RPI + l / L::PC;
-        pages[u] = key < nk ? table[key >> A.shift] : 0;
-      }
-#pragma unroll
-      for (int u = 0; u < U; ++u) asm volatile("" ::"v"(pages[u]));
-    } else {
-#pragma unroll
-      for (int u = 0; u < U; ++u) pages[u] = __builtin_amdgcn_readlane(now, at + u);
-    }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const unsigned key = key0 + u * RPI + l / L::PC;
-      const int c = c0 ^ L::swz(u * RPI);
-      const bool in = key < nk && c * 8 < A.d && pages[u] >= 0 && pages[u] < A.pages;
-      const uint64_t from = (uint64_t)(uint32_t)pages[u] * ps + (uint64_t)(key & mask) * rs + c * 16;
-      load(kt + u * 1024, in ? kp + from : (const char*)kZeros);
-      load(vt + u * 1024, in ? vp + from : (const char*)kZeros);
+      pages[u] = key < nk ? table[key >> A.shift] : 0;
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) asm volatile("" ::"v"(pages[u]));
+    const char* k = (const char*)A.k + head;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const unsigned key = key0 + u * RPI + l / L::PC;
+      const int c = (l % L::PC) ^ L::swz(l / L::PC) ^ L::swz(u * RPI);
+      const bool in = key < nk && c * 8 < A.d && (unsigned)pages[u] < A.pages;
+      const char* p = k + (uint64_t)(uint32_t)pages[u] * (uint32_t)(A.ps * 2) + (uint64_t)(key & mask) * (uint32_t)(A.rs * 2) + c * 16;
+      load(kt + u * 1024, in ? p : (const char*)kZeros);
+      load(vt + u * 1024, in ? p + apart_by : (const char*)kZeros);
     }
   }
 };
@@ -388,7 +398,7 @@ struct Walk<__bf16, DB> {
   using F = Fetch<DB>;
   static constexpr int TILE = KT * L::PITCH;
   static constexpr int JOIN = 256 * (32 * DB + 2) * 4;
-  static constexpr int BYTES = 4 * TILE > JOIN ? 4 * TILE : JOIN;
+  static constexpr int BYTES = (4 * TILE > JOIN ? 4 * TILE : JOIN) + kFlags;
 
   template <int N>
   using Scores = f32x16[N];
@@ -447,9 +457,9 @@ struct Walk<__bf16, DB> {
 #pragma unroll
     for (int n = 0; n < N; ++n) {
       top[n] *= c;  // c > 0
-      grow = grow || top[n] > R.m[n] + 8.f || (R.m[n] == -INFINITY && top[n] > -INFINITY);
+      grow |= top[n] > R.m[n] + 8.f;  // (-inf + 8 is -inf: so is the first that is more)
     }
-    if (!__any(grow)) return;
+    if (__builtin_expect_with_probability(!__any(grow), 1, 0.999)) return;
 #pragma unroll
     for (int n = 0; n < N; ++n) {
       const float m = fmaxf(R.m[n], top[n]);
@@ -457,9 +467,10 @@ struct Walk<__bf16, DB> {
       R.m[n] = m;
       R.l[n] *= a;
 #pragma unroll
-      for (int db = 0; db < DB; ++db)
+      for (int db = 0; db < DB; ++db) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) R.o[n][db][i] *= a;
+      }
     }
   }
   template <int N>
@@ -477,14 +488,17 @@ struct Walk<__bf16, DB> {
     }
   }
 
-  // A block of 32 keys, whose scores are s and their tops `top`, and beside it the scores of the following one: a
-  // product's 32 cycles are another seven instructions' time.  There is one wave a SIMD, so what it waits for is lost: reads of LDS go
-  // out three phases (of N products) before their use, and only other instructions may be moved between phases.
+  // A block of 32 keys, whose scores are s, and beside it the scores of the following one: a product's 32 cycles are another
+  // seven instructions' time.  There is one wave a SIMD, so what it waits for is lost: reads of LDS go out three phases (of N
+  // products) before their use, and every product has its share of the other instructions behind it, which stay there.
+  // The maximum is that of the first block, R.m, for all: weights have the exponents of fp32, and are as exact at 2^60 as at 1.
+  // `far`: some score is above R.m by more than 64, and the work is done again with a running maximum (see again).
   // load(k): something more for phase k, of the first.
   // HIDE: keys of the following block from next_key on, of which a lane's rows see those below sees.
   template <int N, bool HIDE, typename Load>
-  static __device__ __forceinline__ void block(Sets<DB, N>& R, Scores<N>& s, Scores<N>& sn, float (&top)[N], const Queries<N>& q, float c, lds_t k_at,
-                                               lds_t v_at, Load load, unsigned next_key = 0, const unsigned* sees = nullptr) {
+  static __device__ __forceinline__ void block(Sets<DB, N>& R, Scores<N>& s, Scores<N>& sn, uint64_t& far, const float (&minus)[N],
+                                               const float (&limit)[N], const Queries<N>& q, float c, lds_t k_at, lds_t v_at, Load load,
+                                               unsigned next_key = 0, const unsigned* sees = nullptr) {
     constexpr int NS = L::NS, NV = 2 * DB, AHEAD = 3;
     Piece f[NS + NV][1];
     auto read = [&](int i) {
@@ -501,15 +515,9 @@ struct Walk<__bf16, DB> {
     };
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) read(i);
-    rescale<N>(R, top, c);
-    __builtin_amdgcn_sched_barrier(0);
     Piece y[2][N][1];
-    float m[N];
 #pragma unroll
-    for (int n = 0; n < N; ++n) {
-      m[n] = R.m[n] == -INFINITY ? 0.f : R.m[n];
-      sn[n] = (f32x16){};
-    }
+    for (int n = 0; n < N; ++n) sn[n] = (f32x16){};
     // The weights in the order in which the products need them, spread over the time until the last do; then the tops.
     constexpr int SPOTS = (NS + DB) * N, REST = DB * N;
     float big[N];
@@ -522,13 +530,12 @@ struct Walk<__bf16, DB> {
         if (i < NS) mma(sn[n], f[i], q[n][i], (__bf16*)nullptr);
         else mma(R.o[n][(i - NS) % DB], f[i], y[(i - NS) / DB][n], (__bf16*)nullptr);
         if (i < NS && n == 0) load(i);
+        asm volatile("" : "+s"(c));  // the weights that follow here, and not together with others
 #pragma unroll
         for (int e = 0; e < 16 * N; ++e)
           if (e * SPOTS / (16 * N) == spot) {
             const int t = e / (8 * N), col = e / 8 % N, j = e % 8;
-            float x = s[col][8 * t + j];
-            asm volatile("" : "+v"(x));  // here, and not together with its neighbours
-            const float p = __builtin_amdgcn_exp2f(fmaf(x, c, -m[col]));
+            const float p = __builtin_amdgcn_exp2f(fmaf(s[col][8 * t + j], c, minus[col]));
             R.l[col] += p;
             y[t][col][0].b[j] = (__bf16)p;
           }
@@ -542,7 +549,36 @@ struct Walk<__bf16, DB> {
         __builtin_amdgcn_sched_barrier(0);
       }
 #pragma unroll
-    for (int n = 0; n < N; ++n) top[n] = half_max(big[n]);
+    for (int n = 0; n < N; ++n) far |= __ballot(big[n] > limit[n]);
+  }
+  // The first block's scores: the maximum for all.
+  template <int N>
+  static __device__ __forceinline__ void settle(Sets<DB, N>& R, const Scores<N>& s, float c, float (&minus)[N], float (&limit)[N]) {
+    float top[N];
+    tops<N>(top, s);
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      R.m[n] = top[n] * c;
+      minus[n] = R.m[n] == -INFINITY ? 0.f : -R.m[n];
+      limit[n] = (R.m[n] + 64.f) / c;  // of scores as they are.  (-inf stays -inf.)
+    }
+  }
+  template <int N>
+  static __device__ __forceinline__ void clear(Sets<DB, N>& R) {
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+#pragma unroll
+      for (int db = 0; db < DB; ++db) R.o[n][db] = (f32x16){};
+      R.m[n] = -INFINITY;
+      R.l[n] = 0.f;
+    }
+  }
+  template <int N>
+  static __device__ __forceinline__ bool odd(const Sets<DB, N>& R) {
+    bool b = false;
+#pragma unroll
+    for (int n = 0; n < N; ++n) b = b || not_finite(R.o[n]);
+    return b;
   }
 
   // The KH waves of a set of rows join, and the results go where they belong.  Each wave's sums go to LDS, a row after
@@ -605,23 +641,47 @@ struct Walk<__bf16, DB> {
 
   // The wave's N sets of 32 rows from row m0 of the matrix on
   template <int N>
-  static __device__ __forceinline__ void begin(const PArgs& A, const PSeq& S, const Blocks<KT, NC>& B, int g, int m0, Queries<N>& q, Sets<DB, N>& R,
-                                               unsigned (&sees)[N]) {
+  static __device__ __forceinline__ void begin(const PArgs& A, const PSeq& S, const Blocks<KT, NC>& B, int g, int m0, Queries<N>& q, unsigned (&sees)[N]) {
 #pragma unroll
     for (int n = 0; n < N; ++n) {
       const int m = m0 + 32 * n + (lane_id() & 31), query = query_of(A, m), head = g * A.per + m - query * A.per;
       sees[n] = pseen(A, S, m);
       load_cols<__bf16, DB>(q[n], (const __bf16*)A.q + ((int64_t)S.q0 + query) * A.qs + (int64_t)head * A.d, m < B.M, A.d);
-#pragma unroll
-      for (int db = 0; db < DB; ++db) R.o[n][db] = (f32x16){};
-      R.m[n] = -INFINITY;
-      R.l[n] = 0.f;
     }
   }
   static __device__ __forceinline__ lds_t k_lane() { return L::at(lane_id() & 31, lane_id() >> 5); }
   static __device__ __forceinline__ lds_t v_lane() {
     const int l = lane_id();
     return L::at(4 * (l >> 5) + ((l >> 2) & 3), 2 * ((l >> 4) & 1) + ((l >> 1) & 1)) + (l & 1) * 8;
+  }
+  // The steps with a running maximum, for scores that leave the first block's far behind, and sums that are not finite: one after
+  // another, all four waves together.
+  template <int N>
+  static __device__ __forceinline__ void again(const PArgs& A, F& f, lds_t kt, lds_t vt, int g, int first, int last, unsigned all, int nb, int kh,
+                                               const Queries<N>& q, const unsigned (&sees)[N], Sets<DB, N>& R) {
+    clear<N>(R);
+    f.init(A, f.table, g, first, all);
+#pragma unroll 1
+    for (int s = first; s < last; ++s) {
+      __syncthreads();
+      f.turn(A, s, all);
+      f.issue(A, kt, vt, s, all);
+      wait_loads<0>();
+      __syncthreads();
+#pragma unroll 1
+      for (int j = 0; j < nb; ++j) {
+        const int r = (kh * nb + j) * 32;
+        Scores<N> a;
+        float top[N];
+        scores<N>(a, q, kt + k_lane() + r * L::PITCH);
+#pragma unroll
+        for (int n = 0; n < N; ++n) hide(a[n], (unsigned)s * KT + r, sees[n]);
+        tops<N>(top, a);
+        rescale<N>(R, top, A.c);
+        weights<N>(R, a, A.c);
+        values<N>(R, a, vt + v_lane() + r * L::PITCH);
+      }
+    }
   }
 
   // Up to 32 rows: each wave takes a fourth of every step's keys, which it fetches itself two steps ahead, and waits for nobody.
@@ -635,8 +695,11 @@ struct Walk<__bf16, DB> {
     Queries<1> q;
     Sets<DB, 1> R;
     unsigned sees[1];
-    begin<1>(A, S, B, g, 0, q, R, sees);
+    begin<1>(A, S, B, g, 0, q, sees);
+    clear<1>(R);
     const lds_t k_at = kt + k_lane() + wave * 32 * L::PITCH, v_at = vt + v_lane() + wave * 32 * L::PITCH;
+    float minus[1] = {0.f}, limit[1] = {0.f};
+    uint64_t far = 0;
 #pragma unroll 1
     for (int s = first - 2; s < last; ++s) {
       const lds_t buf = (s - first) & 1 ? TILE : 0;
@@ -644,16 +707,23 @@ struct Walk<__bf16, DB> {
         if (s + 1 < last) wait_loads<2 * F::U>();
         else wait_loads<0>();
         Scores<1> a;
-        float top[1];
         scores<1>(a, q, k_at + buf);
         const unsigned key = (unsigned)s * KT + wave * 32;
         if (key + 32 > least) {
           asm volatile("");  // a branch, not selections in every step
           hide(a[0], key, sees[0]);
         }
-        tops<1>(top, a);
-        rescale<1>(R, top, A.c);
-        weights<1>(R, a, A.c);
+        if (s == first) settle<1>(R, a, A.c, minus, limit);
+        float t = a[0][0], sum = 0.f;
+#pragma unroll
+        for (int i = 1; i < 16; ++i) t = fmaxf(t, a[0][i]);
+        far |= __ballot(t > limit[0]);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          a[0][i] = __builtin_amdgcn_exp2f(fmaf(a[0][i], A.c, minus[0]));
+          sum += a[0][i];
+        }
+        R.l[0] += sum;
         values<1>(R, a, v_at + buf);
         wait_lds();
       }
@@ -662,6 +732,7 @@ struct Walk<__bf16, DB> {
         f.issue(A, kt + buf, vt + buf, s + 2, all);
       }
     }
+    if (any_wave<4>(kt + BYTES - kFlags, far != 0 || odd<1>(R))) again<1>(A, f, kt, vt, g, first, last, all, 1, wave, q, sees, R);
     join<1>(A, shared, R, B, to);
   }
 
@@ -671,6 +742,7 @@ struct Walk<__bf16, DB> {
     constexpr int N = NC;
     const lds_t kt = lds_start(shared), vt = kt + 2 * TILE;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), KH = 4 / B.rw, kh = wave & (KH - 1), row0 = wave / KH * 32 * N;
+    const int nb = 4 / KH;  // blocks of 32 keys of this wave in a step
     const unsigned all = pseen(A, S, min((t + 1) * B.rows, B.M) - 1);  // keys that the block's last row sees
     // keys that all rows of the workgroup see: by that the waves choose their way, all the same one, between barriers
     const unsigned lowest = pseen(A, S, t * B.rows);
@@ -679,68 +751,76 @@ struct Walk<__bf16, DB> {
     Queries<N> q;
     Sets<DB, N> R;
     unsigned sees[N];
-    begin<N>(A, S, B, g, t * B.rows + row0, q, R, sees);
+    begin<N>(A, S, B, g, t * B.rows + row0, q, sees);
+    clear<N>(R);
     if (first < last) {
       f.issue(A, kt, vt, first, all);
       wait_loads<0>();
       meet();
-      const int nb = 4 / KH;  // blocks of 32 keys of this wave in a step
       const lds_t k_at0 = kt + k_lane() + kh * nb * 32 * L::PITCH, v_at0 = vt + v_lane() + kh * nb * 32 * L::PITCH;
       lds_t buf = 0;  // of the step at hand
       Scores<N> a, b;
-      float top[N];
+      float minus[N], limit[N];
+      uint64_t far = 0;
       scores<N>(a, q, k_at0);
 #pragma unroll
       for (int n = 0; n < N; ++n) hide(a[n], (unsigned)first * KT + kh * nb * 32, sees[n]);
-      tops<N>(top, a);
+      settle<N>(R, a, A.c, minus, limit);
       int s = first;
       auto nothing = [](int) {};
       // Steps after which another comes and all of whose keys, and the next one's first, all rows see.  The next step's rows are
-      // fetched during the first two of four blocks.
-      if (KH == 1) {
+      // fetched group by group beside the products of the first two of four blocks.
+      if (nb == 4) {
 #pragma unroll 1
-        for (; s + 1 < last && ((unsigned)s + 2) * KT <= lowest && f.quick(A, s + 1, all); ++s) {
+        for (; s + 1 < last && ((unsigned)s + 2) * KT <= lowest; ++s) {
+          f.turn(A, s + 1, all);
+          if (!f.quick(A, s + 1, all)) break;
           const lds_t k_at = k_at0 + buf, v_at = v_at0 + buf;
           const lds_t kw = kt + (buf ^ TILE) + wave * 32 * L::PITCH, vw = vt + (buf ^ TILE) + wave * 32 * L::PITCH;
-          f.turn(A, s + 1, all);
-          block<N, false>(R, a, b, top, q, A.c, k_at + 32 * L::PITCH, v_at, [&](int k) { if (k < F::U / 2) f.group(A, kw, vw, s + 1, k); });
-          block<N, false>(R, b, a, top, q, A.c, k_at + 64 * L::PITCH, v_at + 32 * L::PITCH, [&](int k) { if (k < F::U / 2) f.group(A, kw, vw, s + 1, F::U / 2 + k); });
-          block<N, false>(R, a, b, top, q, A.c, k_at + 96 * L::PITCH, v_at + 64 * L::PITCH, nothing);
+          block<N, false>(R, a, b, far, minus, limit, q, A.c, k_at + 32 * L::PITCH, v_at, [&](int k) { if (k < F::U / 2) f.group(kw, vw, s + 1, k); });
+          block<N, false>(R, b, a, far, minus, limit, q, A.c, k_at + 64 * L::PITCH, v_at + 32 * L::PITCH,
+                          [&](int k) { if (k < F::U / 2) f.group(kw, vw, s + 1, F::U / 2 + k); });
+          block<N, false>(R, a, b, far, minus, limit, q, A.c, k_at + 96 * L::PITCH, v_at + 64 * L::PITCH, nothing);
           buf ^= TILE;
           // the next step is here
           wait_loads<0>();
           meet();
-          block<N, false>(R, b, a, top, q, A.c, k_at0 + buf, v_at + 96 * L::PITCH, nothing);
+          block<N, false>(R, b, a, far, minus, limit, q, A.c, k_at0 + buf, v_at + 96 * L::PITCH, nothing);
           // all have read this one
           wait_lds();
           meet();
         }
       }
-      // The others
+      // The others.  (Blocks in one loop: loops of steps and blocks inside each other would copy all sums from one's registers to the
+      // other's.)
+      int j = 0;
 #pragma unroll 1
-      for (; s < last; ++s) {
-        const bool more = s + 1 < last;
-        if (more) {
+      while (s < last) {
+        const bool ends = j + 1 == nb, more = s + 1 < last;
+        if (j == 0 && more) {
           f.turn(A, s + 1, all);
           f.issue(A, kt + (buf ^ TILE), vt + (buf ^ TILE), s + 1, all);
         }
-#pragma unroll 1
-        for (int j = 0; j < nb; ++j) {
-          const bool ends = j + 1 == nb;
-          if (ends && more) {
-            wait_loads<0>();
-            meet();
-          }
-          // (after the last block: scores of what lies there, which nobody takes)
-          const lds_t next = ends ? k_at0 + (buf ^ TILE) : k_at0 + buf + (j + 1) * 32 * L::PITCH;
-          block<N, true>(R, a, b, top, q, A.c, next, v_at0 + buf + j * 32 * L::PITCH, nothing, ends ? (unsigned)(s + 1) * KT + kh * nb * 32 : (unsigned)s * KT + (kh * nb + j + 1) * 32, sees);
-#pragma unroll
-          for (int n = 0; n < N; ++n) a[n] = b[n];
+        if (ends && more) {  // the next step is here
+          wait_loads<0>();
+          meet();
         }
+        // (after the last block: scores of what lies there, all hidden)
+        const lds_t next = ends ? k_at0 + (buf ^ TILE) : k_at0 + buf + (j + 1) * 32 * L::PITCH;
+        const unsigned key = !ends ? (unsigned)s * KT + (kh * nb + j + 1) * 32 : more ? (unsigned)(s + 1) * KT + kh * nb * 32 : 0x80000000u;
+        block<N, true>(R, a, b, far, minus, limit, q, A.c, next, v_at0 + buf + j * 32 * L::PITCH, nothing, key, sees);
+#pragma unroll
+        for (int n = 0; n < N; ++n) a[n] = b[n];
+        ++j;
+        if (!ends) continue;
+        j = 0;
         buf ^= TILE;
+        ++s;
+        // all have read this one
         wait_lds();
         meet();
       }
+      if (any_wave<4>(kt + BYTES - kFlags, far != 0 || odd<N>(R))) again<N>(A, f, kt, vt, g, first, last, all, nb, kh, q, sees, R);
     }
     if (KH > 1) {
       join<N>(A, shared, R, B, to);
@@ -972,12 +1052,9 @@ int dnb_paged_attn_create(const dnb_paged_attn_desc* desc, dnb_paged_attn** out)
   const bool bf16 = d.cache.dtype == DNB_BF16;
   if (bf16) p->max_rows = M <= 32 ? 32 : M <= 128 ? 128 : 256;
   else p->max_rows = M <= 64 ? 64 : 128;
-  {
-    const int cost[3] = {5, 5, 8}, extra[3] = {5, 8, 10};
-    for (int i = 0; i < 3; ++i) { p->cost[i] = cost[i]; p->extra[i] = extra[i]; }
-    p->least = 10;
-    if (getenv("PC")) { sscanf(getenv("PC"), "%d,%d,%d,%d,%d,%d,%d", p->cost, p->cost + 1, p->cost + 2, p->extra, p->extra + 1, p->extra + 2, &p->least); }
-  }
+  const int cost[3] = {5, 5, 8}, extra_bf[3] = {15, 12, 40}, extra_f[3] = {5, 8, 10};
+  for (int i = 0; i < 3; ++i) { p->cost[i] = cost[i]; p->extra[i] = bf16 ? extra_bf[i] : extra_f[i]; }
+  p->least = 10;
   const int dp = (d.cache.head_dim + 31) / 32 * 32;
   p->ws_part = ((size_t)p->W * sizeof(Shared) + 255) / 256 * 256;
   p->ws_bytes = p->ws_part + (size_t)2 * p->W * p->max_rows * (dp + 2) * sizeof(float);
