@@ -491,13 +491,14 @@ struct Walk<__bf16, DB> {
   // A block of 32 keys, whose scores are s, and beside it the scores of the following one: a product's 32 cycles are another
   // seven instructions' time.  There is one wave a SIMD, so what it waits for is lost: reads of LDS go out three phases (of N
   // products) before their use, and every product has its share of the other instructions behind it, which stay there.
-  // The maximum is that of the first block, R.m, for all: weights have the exponents of fp32, and are as exact at 2^60 as at 1.
-  // `far`: some score is above R.m by more than 64, and the work is done again with a running maximum (see again).
+  // The maximum is that of the first block, R.m, for all: weights have the exponents of fp32, and are as exact at 2^60 as at 1;
+  // sums that have left their range are seen at the end, and the work is done again with a running maximum (see odd and again).
+  // A row's sum is that of its weights as they are rounded, in pairs.
   // load(k): something more for phase k, of the first.
   // HIDE: keys of the following block from next_key on, of which a lane's rows see those below sees.
   template <int N, bool HIDE, typename Load>
-  static __device__ __forceinline__ void block(Sets<DB, N>& R, Scores<N>& s, Scores<N>& sn, uint64_t& far, const float (&minus)[N],
-                                               const float (&limit)[N], const Queries<N>& q, float c, lds_t k_at, lds_t v_at, Load load,
+  static __device__ __forceinline__ void block(Sets<DB, N>& R, Scores<N>& s, Scores<N>& sn, const float (&minus)[N],
+                                               const Queries<N>& q, float c, lds_t k_at, lds_t v_at, Load load,
                                                unsigned next_key = 0, const unsigned* sees = nullptr) {
     constexpr int NS = L::NS, NV = 2 * DB, AHEAD = 3;
     Piece f[NS + NV][1];
@@ -518,9 +519,8 @@ struct Walk<__bf16, DB> {
     Piece y[2][N][1];
 #pragma unroll
     for (int n = 0; n < N; ++n) sn[n] = (f32x16){};
-    // The weights in the order in which the products need them, spread over the time until the last do; then the tops.
+    // The weights in the order in which the products need them, spread over the time until the last do.
     constexpr int SPOTS = (NS + DB) * N, REST = DB * N;
-    float big[N];
 #pragma unroll
     for (int i = 0; i < NS + NV; ++i)
 #pragma unroll
@@ -536,31 +536,30 @@ struct Walk<__bf16, DB> {
           if (e * SPOTS / (16 * N) == spot) {
             const int t = e / (8 * N), col = e / 8 % N, j = e % 8;
             const float p = __builtin_amdgcn_exp2f(fmaf(s[col][8 * t + j], c, minus[col]));
-            R.l[col] += p;
             y[t][col][0].b[j] = (__bf16)p;
+            R.l[col] += p;
           }
+        if (HIDE) {
 #pragma unroll
-        for (int e = 0; e < 16 * N; ++e)
-          if (SPOTS + e * REST / (16 * N) == spot) {
-            const int col = e / 16, j = e % 16;
-            if (HIDE) sn[col][j] = next_key + row_of(j) >= sees[col] ? -INFINITY : sn[col][j];
-            big[col] = j == 0 ? sn[col][0] : fmaxf(big[col], sn[col][j]);
-          }
+          for (int e = 0; e < 16 * N; ++e)
+            if (SPOTS + e * REST / (16 * N) == spot) {
+              const int col = e / 16, j = e % 16;
+              sn[col][j] = next_key + row_of(j) >= sees[col] ? -INFINITY : sn[col][j];
+            }
+        }
         __builtin_amdgcn_sched_barrier(0);
       }
-#pragma unroll
-    for (int n = 0; n < N; ++n) far |= __ballot(big[n] > limit[n]);
   }
   // The first block's scores: the maximum for all.
   template <int N>
-  static __device__ __forceinline__ void settle(Sets<DB, N>& R, const Scores<N>& s, float c, float (&minus)[N], float (&limit)[N]) {
+  static __device__ __forceinline__ void settle(Sets<DB, N>& R, const Scores<N>& s, float c, float (&minus)[N]) {
     float top[N];
     tops<N>(top, s);
 #pragma unroll
     for (int n = 0; n < N; ++n) {
       R.m[n] = top[n] * c;
-      minus[n] = R.m[n] == -INFINITY ? 0.f : -R.m[n];
-      limit[n] = (R.m[n] + 64.f) / c;  // of scores as they are.  (-inf stays -inf.)
+      // (where the first block has nothing, nor must later ones: any score above -inf makes an infinite weight)
+      minus[n] = R.m[n] == -INFINITY ? 3.4e38f : -R.m[n];
     }
   }
   template <int N>
@@ -573,11 +572,20 @@ struct Walk<__bf16, DB> {
       R.l[n] = 0.f;
     }
   }
+  // Sums that scores far above the first block's have made large, so large that parts of a row could not be added, or that
+  // are not finite.
   template <int N>
   static __device__ __forceinline__ bool odd(const Sets<DB, N>& R) {
     bool b = false;
 #pragma unroll
-    for (int n = 0; n < N; ++n) b = b || not_finite(R.o[n]);
+    for (int n = 0; n < N; ++n) {
+      float most = 0.f;
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) most = fmaxf(most, fabsf(R.o[n][db][i]));
+      b = b | !(R.l[n] < 0x1p64f) | (most > 0x1p100f) | not_finite(R.o[n]);
+    }
     return b;
   }
 
@@ -698,8 +706,7 @@ struct Walk<__bf16, DB> {
     begin<1>(A, S, B, g, 0, q, sees);
     clear<1>(R);
     const lds_t k_at = kt + k_lane() + wave * 32 * L::PITCH, v_at = vt + v_lane() + wave * 32 * L::PITCH;
-    float minus[1] = {0.f}, limit[1] = {0.f};
-    uint64_t far = 0;
+    float minus[1] = {0.f};
 #pragma unroll 1
     for (int s = first - 2; s < last; ++s) {
       const lds_t buf = (s - first) & 1 ? TILE : 0;
@@ -713,11 +720,8 @@ struct Walk<__bf16, DB> {
           asm volatile("");  // a branch, not selections in every step
           hide(a[0], key, sees[0]);
         }
-        if (s == first) settle<1>(R, a, A.c, minus, limit);
-        float t = a[0][0], sum = 0.f;
-#pragma unroll
-        for (int i = 1; i < 16; ++i) t = fmaxf(t, a[0][i]);
-        far |= __ballot(t > limit[0]);
+        if (s == first) settle<1>(R, a, A.c, minus);
+        float sum = 0.f;
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           a[0][i] = __builtin_amdgcn_exp2f(fmaf(a[0][i], A.c, minus[0]));
@@ -732,7 +736,7 @@ struct Walk<__bf16, DB> {
         f.issue(A, kt + buf, vt + buf, s + 2, all);
       }
     }
-    if (any_wave<4>(kt + BYTES - kFlags, far != 0 || odd<1>(R))) again<1>(A, f, kt, vt, g, first, last, all, 1, wave, q, sees, R);
+    if (any_wave<4>(kt + BYTES - kFlags, odd<1>(R))) again<1>(A, f, kt, vt, g, first, last, all, 1, wave, q, sees, R);
     join<1>(A, shared, R, B, to);
   }
 
@@ -760,12 +764,11 @@ struct Walk<__bf16, DB> {
       const lds_t k_at0 = kt + k_lane() + kh * nb * 32 * L::PITCH, v_at0 = vt + v_lane() + kh * nb * 32 * L::PITCH;
       lds_t buf = 0;  // of the step at hand
       Scores<N> a, b;
-      float minus[N], limit[N];
-      uint64_t far = 0;
+      float minus[N];
       scores<N>(a, q, k_at0);
 #pragma unroll
       for (int n = 0; n < N; ++n) hide(a[n], (unsigned)first * KT + kh * nb * 32, sees[n]);
-      settle<N>(R, a, A.c, minus, limit);
+      settle<N>(R, a, A.c, minus);
       int s = first;
       auto nothing = [](int) {};
       // Steps after which another comes and all of whose keys, and the next one's first, all rows see.  The next step's rows are
@@ -777,15 +780,15 @@ struct Walk<__bf16, DB> {
           if (!f.quick(A, s + 1, all)) break;
           const lds_t k_at = k_at0 + buf, v_at = v_at0 + buf;
           const lds_t kw = kt + (buf ^ TILE) + wave * 32 * L::PITCH, vw = vt + (buf ^ TILE) + wave * 32 * L::PITCH;
-          block<N, false>(R, a, b, far, minus, limit, q, A.c, k_at + 32 * L::PITCH, v_at, [&](int k) { if (k < F::U / 2) f.group(kw, vw, s + 1, k); });
-          block<N, false>(R, b, a, far, minus, limit, q, A.c, k_at + 64 * L::PITCH, v_at + 32 * L::PITCH,
+          block<N, false>(R, a, b, minus, q, A.c, k_at + 32 * L::PITCH, v_at, [&](int k) { if (k < F::U / 2) f.group(kw, vw, s + 1, k); });
+          block<N, false>(R, b, a, minus, q, A.c, k_at + 64 * L::PITCH, v_at + 32 * L::PITCH,
                           [&](int k) { if (k < F::U / 2) f.group(kw, vw, s + 1, F::U / 2 + k); });
-          block<N, false>(R, a, b, far, minus, limit, q, A.c, k_at + 96 * L::PITCH, v_at + 64 * L::PITCH, nothing);
+          block<N, false>(R, a, b, minus, q, A.c, k_at + 96 * L::PITCH, v_at + 64 * L::PITCH, nothing);
           buf ^= TILE;
           // the next step is here
           wait_loads<0>();
           meet();
-          block<N, false>(R, b, a, far, minus, limit, q, A.c, k_at0 + buf, v_at + 96 * L::PITCH, nothing);
+          block<N, false>(R, b, a, minus, q, A.c, k_at0 + buf, v_at + 96 * L::PITCH, nothing);
           // all have read this one
           wait_lds();
           meet();
@@ -808,7 +811,7 @@ struct Walk<__bf16, DB> {
         // (after the last block: scores of what lies there, all hidden)
         const lds_t next = ends ? k_at0 + (buf ^ TILE) : k_at0 + buf + (j + 1) * 32 * L::PITCH;
         const unsigned key = !ends ? (unsigned)s * KT + (kh * nb + j + 1) * 32 : more ? (unsigned)(s + 1) * KT + kh * nb * 32 : 0x80000000u;
-        block<N, true>(R, a, b, far, minus, limit, q, A.c, next, v_at0 + buf + j * 32 * L::PITCH, nothing, key, sees);
+        block<N, true>(R, a, b, minus, q, A.c, next, v_at0 + buf + j * 32 * L::PITCH, nothing, key, sees);
 #pragma unroll
         for (int n = 0; n < N; ++n) a[n] = b[n];
         ++j;
@@ -820,7 +823,7 @@ struct Walk<__bf16, DB> {
         wait_lds();
         meet();
       }
-      if (any_wave<4>(kt + BYTES - kFlags, far != 0 || odd<N>(R))) again<N>(A, f, kt, vt, g, first, last, all, nb, kh, q, sees, R);
+      if (any_wave<4>(kt + BYTES - kFlags, odd<N>(R))) again<N>(A, f, kt, vt, g, first, last, all, nb, kh, q, sees, R);
     }
     if (KH > 1) {
       join<N>(A, shared, R, B, to);
@@ -947,6 +950,53 @@ __global__ __launch_bounds__(kThreads) void k_paged_join(PArgs A, int max_rows) 
   int split = 1;  // groups to a row: where there are few rows
   while (split < S.parts && split < G && S.rows * 2 * split <= (int)gridDim.y * G) split *= 2;
   const int grp = threadIdx.x / LANES, c = threadIdx.x % LANES, at = grp % split, rows = G / split;
+  if (split == 1) {  // four rows a group at once, for loads in flight
+    constexpr int R = 4;
+    for (int r0 = blockIdx.y * (R * G); r0 < S.rows; r0 += gridDim.y * (R * G)) {
+      float M[R], sum[R];
+      f32x4 o[R];
+#pragma unroll
+      for (int k = 0; k < R; ++k) {
+        M[k] = -INFINITY;
+        sum[k] = 0.f;
+        o[k] = (f32x4){};
+      }
+#pragma unroll 2
+      for (int i = 0; i < S.parts; ++i) {
+        const float* p = A.part + (int64_t)(2 * (w + i) + (i == 0)) * part_floats<DB>(max_rows);
+        float mi[R], li[R];
+        f32x4 v[R];
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+          const int r = min(r0 + k * G + grp, S.rows - 1);
+          mi[k] = p[max_rows * DP + r];
+          li[k] = p[max_rows * (DP + 1) + r];
+          v[k] = *reinterpret_cast<const f32x4*>(p + (int64_t)r * DP + min(4 * c, DP - 4));
+        }
+#pragma unroll
+        for (int k = 0; k < R; ++k) {
+          const float top = fmaxf(M[k], mi[k]), t = top == -INFINITY ? 0.f : top;
+          const float x = __builtin_amdgcn_exp2f(M[k] - t), y = __builtin_amdgcn_exp2f(mi[k] - t);
+          M[k] = top;
+          sum[k] = sum[k] * x + li[k] * y;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) o[k][j] = o[k][j] * x + v[k][j] * y;
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < R; ++k) {
+        const int r = r0 + k * G + grp, m = S.m0 + r;
+        if (r >= S.rows) break;
+        const int query = query_of(A, m), head = S.g * A.per + m - query * A.per;
+        const int64_t qrow = (int64_t)S.q0 + query;
+        const float f = sum[k] == 0.f ? 0.f : 1.f / sum[k];
+        typedef T four __attribute__((ext_vector_type(4)));
+        if (4 * c < A.d) *reinterpret_cast<four*>((T*)A.o + (qrow * A.heads + head) * A.d + 4 * c) = (four){(T)(o[k][0] * f), (T)(o[k][1] * f), (T)(o[k][2] * f), (T)(o[k][3] * f)};
+        if (c == 0 && A.lse) A.lse[(int64_t)head * A.rq + qrow] = sum[k] == 0.f ? -INFINITY : (M[k] + log2f(sum[k])) * kLn2;
+      }
+    }
+    return;
+  }
   for (int r0 = blockIdx.y * rows; r0 < S.rows; r0 += gridDim.y * rows) {
     const int r = r0 + grp / split;
     float M = -INFINITY, sum = 0.f;
@@ -1002,7 +1052,7 @@ hipError_t run_paged(const PArgs& A, int max_rows, hipStream_t st) {
   hipLaunchKernelGGL((k_paged<M, DB>), dim3(A.W), dim3(kThreads), BYTES, st, A, max_rows);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || A.W == 1) return e;
-  hipLaunchKernelGGL((k_paged_join<T, DB>), dim3(A.W - 1, max_rows / 8), dim3(kThreads), 0, st, A, max_rows);
+  hipLaunchKernelGGL((k_paged_join<T, DB>), dim3(A.W - 1, max_rows <= 32 ? 4 : max_rows / 32), dim3(kThreads), 0, st, A, max_rows);
   return hipGetLastError();
 }
 
