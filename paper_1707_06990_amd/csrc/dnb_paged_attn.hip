@@ -840,7 +840,7 @@ struct Walk<__bf16, DB> {
 };
 
 template <typename T, int DB>
-__global__ __launch_bounds__(kThreads, 1) void k_paged(PArgs A, int max_rows) {
+__global__ __launch_bounds__(kThreads, (std::is_same<T, __bf16>::value || DB > 2 ? 1 : 2)) void k_paged(PArgs A, int max_rows) {
   using K = Walk<T, DB>;
   constexpr int KT = K::KT, NC = K::NC;
   using B_ = Blocks<KT, NC>;
@@ -854,7 +854,7 @@ __global__ __launch_bounds__(kThreads, 1) void k_paged(PArgs A, int max_rows) {
     mine += u;
   }
   const int64_t scan = block_scan(mine, red, &total);
-  const int W = (int)min((int64_t)A.W, max(total / A.least, (int64_t)1));
+  const int W = (int)fmin((double)A.W, fmax((double)total / A.least, 1.0));
   // workgroups that lie side by side on the line run on one XCD, whose cache has the keys that they share
   const int w = A.W % 8 == 0 ? (int)(blockIdx.x % 8) * (A.W / 8) + (int)blockIdx.x / 8 : (int)blockIdx.x;
   if (tid == 0) A.shared[w].parts = 0;
@@ -885,20 +885,26 @@ __global__ __launch_bounds__(kThreads, 1) void k_paged(PArgs A, int max_rows) {
   {
     const B_ B(A, S);
     // key/value head and block at a
-    int64_t H = 0;
-    for (int t0 = 0; t0 < B.count; t0 += 64) H += bcast64(wave_scan(t0 + l < B.count ? B.units(A, S, t0 + l) : 0), 63);
-    g = (int)((double)(a - a0) / (double)H);
-    a0 += g * H;
-    for (int t0 = 0; t0 < B.count; t0 += 64) {
-      const int64_t v = t0 + l < B.count ? B.units(A, S, t0 + l) : 0, end = a0 + wave_scan(v);
-      const uint64_t past = __ballot(end > a);
-      if (past) {
-        const int at = __builtin_ctzll(past);
-        t = t0 + at;
-        a0 = bcast64(end - v, at);
-        break;
+    if (B.count == 1) {
+      const int64_t H = B.units(A, S, 0);
+      g = (int)((double)(a - a0) / (double)H);
+      a0 += g * H;
+    } else {
+      int64_t H = 0;
+      for (int t0 = 0; t0 < B.count; t0 += 64) H += bcast64(wave_scan(t0 + l < B.count ? B.units(A, S, t0 + l) : 0), 63);
+      g = (int)((double)(a - a0) / (double)H);
+      a0 += g * H;
+      for (int t0 = 0; t0 < B.count; t0 += 64) {
+        const int64_t v = t0 + l < B.count ? B.units(A, S, t0 + l) : 0, end = a0 + wave_scan(v);
+        const uint64_t past = __ballot(end > a);
+        if (past) {
+          const int at = __builtin_ctzll(past);
+          t = t0 + at;
+          a0 = bcast64(end - v, at);
+          break;
+        }
+        a0 = bcast64(end, 63);
       }
-      a0 = bcast64(end, 63);
     }
   }
   for (;;) {
@@ -1097,14 +1103,14 @@ int dnb_paged_attn_create(const dnb_paged_attn_desc* desc, dnb_paged_attn** out)
   dnb_paged_attn* p = new (std::nothrow) dnb_paged_attn();
   if (!p) return DNB_E_NOMEM;
   p->d = d;
-  p->W = 256;
+  p->W = d.cache.dtype == DNB_F32 && d.cache.head_dim <= 64 ? 512 : 256;
   const int64_t M = d.rows_q * per;
   const bool bf16 = d.cache.dtype == DNB_BF16;
   if (bf16) p->max_rows = M <= 32 ? 32 : M <= 128 ? 128 : 256;
   else p->max_rows = M <= 64 ? 64 : 128;
-  const int cost[3] = {5, 5, 8}, extra_bf[3] = {15, 12, 40}, extra_f[3] = {5, 8, 10};
+  const int cost[3] = {5, 5, 8}, extra_bf[3] = {8, 12, 40}, extra_f[3] = {2, 3, 4};
   for (int i = 0; i < 3; ++i) { p->cost[i] = cost[i]; p->extra[i] = bf16 ? extra_bf[i] : extra_f[i]; }
-  p->least = 10;
+  p->least = 5;
   const int dp = (d.cache.head_dim + 31) / 32 * 32;
   p->ws_part = ((size_t)p->W * sizeof(Shared) + 255) / 256 * 256;
   p->ws_bytes = p->ws_part + (size_t)2 * p->W * p->max_rows * (dp + 2) * sizeof(float);
