@@ -151,6 +151,81 @@ class Cache:
         dnb.dnb_attn_destroy(self.attn)
 
 
+class PagedCache:
+    """Keys and values of up to `requests` requests in a pool of pages: prompts of any lengths beside single tokens, requests that go on
+    from another's, pages that are given back and moved together.  capacity: the most tokens of a request."""
+
+    def __init__(self, block, requests, capacity, pages, page_size=16):
+        m = self.m = block
+        self.requests, self.columns = requests, -(-capacity // page_size)
+        self.layout = dnb.dnb_paged_layout(pages, page_size, m.kv_heads, m.dim, requests, self.columns, dtype=m.code)
+        self.pool = torch.empty(2, pages, page_size, m.kv_heads * m.dim, dtype=m.dtype, device="cuda")
+        self.books = dnb.dnb_pages_create(pages, page_size, requests, self.columns)
+        self.plans = {}
+
+    def plan(self, rows):
+        if rows not in self.plans:
+            m = self.m
+            plan = dnb.dnb_paged_attn_create(self.layout, m.heads, rows, q_stride=(m.heads + 2 * m.kv_heads) * m.dim)
+            self.plans[rows] = plan, torch.empty(dnb.dnb_paged_attn_workspace_bytes(plan), dtype=torch.uint8, device="cuda")
+        return self.plans[rows]
+
+    def moved(self):
+        """Does what copying the books ask for."""
+        pairs = dnb.dnb_pages_copies(self.books)
+        if len(pairs):
+            plane = self.pool[0].nbytes
+            dnb.dnb_op_paged_copy(self.pool, self.layout.pages, plane // self.layout.pages, 2, plane, torch.from_numpy(pairs).cuda(), len(pairs))
+
+    def next(self, texts):
+        """Logits after the last of some more tokens of each request (a list each, which may be empty), a row for each that has any.
+        Where there is no room for all of them (DnbError), none has been taken."""
+        before = dnb.dnb_pages_table(self.books, self.requests, self.columns)[1]
+        try:
+            for s, text in enumerate(texts):
+                dnb.dnb_pages_extend(self.books, s, len(text))
+        except dnb.DnbError:
+            for s, n in enumerate(before):
+                dnb.dnb_pages_truncate(self.books, s, int(n))
+            self.moved()
+            raise
+        self.moved()
+        put = lambda v: torch.from_numpy(np.ascontiguousarray(v, dtype=np.int32)).cuda()  # noqa: E731
+        table, lengths = (put(v) for v in dnb.dnb_pages_table(self.books, self.requests, self.columns))
+        ends = np.cumsum([0] + [len(t) for t in texts] + [0] * (self.requests - len(texts)))
+        offsets, m, rows = put(ends), self.m, int(ends[-1])
+        tokens = torch.tensor([t for text in texts for t in text], dtype=torch.long, device="cuda")
+        x = m.p["embed"].to(m.dtype)[tokens]
+        qkv = m.product(x, m.p["qkv"])
+        q, k, v = qkv.split([m.heads * m.dim, m.kv_heads * m.dim, m.kv_heads * m.dim], 1)
+        qk = dnb.dnb_qk_layout(rows, m.heads, m.kv_heads, m.dim, m.dim, dtype=m.code, q_stride=qkv.shape[1], k_stride=qkv.shape[1],
+                               v_stride=qkv.shape[1], q_out_stride=qkv.shape[1])
+        dnb.dnb_op_paged_append(qk, self.layout, q, k, v, None, None, None, m.turns, offsets, lengths, table, q, *self.pool)
+        out = torch.empty(rows, m.heads * m.dim, dtype=m.dtype, device="cuda")
+        plan, workspace = self.plan(rows)
+        dnb.dnb_paged_attn_forward(plan, q, *self.pool, offsets, lengths, table, out, None, workspace)
+        last = torch.tensor([e - 1 for e, t in zip(ends[1:], texts) if len(t)], dtype=torch.long, device="cuda")
+        return m.product(m.norms(m.product(out[last], m.p["out"]), x[last])[1], m.p["head"]).float()
+
+    def fork(self, request, to):
+        dnb.dnb_pages_fork(self.books, request, to)
+
+    def cut(self, request, length=0):
+        dnb.dnb_pages_truncate(self.books, request, length)
+
+    def compact(self):
+        dnb.dnb_pages_compact(self.books)
+        self.moved()
+
+    def free(self):
+        return dnb.dnb_pages_free_count(self.books)
+
+    def close(self):
+        for plan, _ in self.plans.values():
+            dnb.dnb_paged_attn_destroy(plan)
+        dnb.dnb_pages_destroy(self.books)
+
+
 def documents(rng, lengths, symbols):
     """Tokens, the next tokens, and which of those count: those of a document's second half."""
     tokens, targets, weight = [], [], []
@@ -201,6 +276,18 @@ def main(argv=None):
     cache.close()
     for r in zip(*texts):  # one request a line
         print(" ".join(map(str, r)), flush=True)
+    # prompts of some lengths, in one call; the last goes on twice
+    prompts = [d[:n].tolist() for d, n in zip(documents(rng, [40] * 3, args.symbols)[0].split(40), (7, 23, 40))]
+    paged = PagedCache(block, 4, 64, 16)
+    token = paged.next(prompts).argmax(1).tolist()
+    paged.fork(2, 3)
+    texts = [[t] for t in token + [prompts[2][-1]]]
+    for _ in range(15):
+        for text, t in zip(texts, paged.next([text[-1:] for text in texts]).argmax(1).tolist()):
+            text.append(t)
+    paged.close()
+    for prompt, text in zip(prompts + prompts[2:], texts):
+        print(" ".join(map(str, prompt)), "|", " ".join(map(str, text)), flush=True)
     return losses
 
 
