@@ -517,6 +517,7 @@ struct Walk<__bf16, DB> {
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) read(i);
     Piece y[2][N][1];
+    float p[2][N][8];
 #pragma unroll
     for (int n = 0; n < N; ++n) sn[n] = (f32x16){};
     // The weights in the order in which the products need them, spread over the time until the last do.
@@ -532,13 +533,20 @@ struct Walk<__bf16, DB> {
         if (i < NS && n == 0) load(i);
         asm volatile("" : "+s"(c));  // the weights that follow here, and not together with others
 #pragma unroll
-        for (int e = 0; e < 16 * N; ++e)
-          if (e * SPOTS / (16 * N) == spot) {
-            const int t = e / (8 * N), col = e / 8 % N, j = e % 8;
-            const float p = __builtin_amdgcn_exp2f(fmaf(s[col][8 * t + j], c, minus[col]));
-            y[t][col][0].b[j] = (__bf16)p;
-            R.l[col] += p;
+        for (int e = 0; e < 16 * N; ++e) {
+          const int t = e / (8 * N), col = e / 8 % N, j = e % 8, at = e * (SPOTS - 2) / (16 * N);
+          float& x = p[t][col][j];
+          if (at == spot) x = fmaf(s[col][8 * t + j], c, minus[col]);
+          if (at + 1 == spot) {
+            asm volatile("" : "+v"(x));
+            x = __builtin_amdgcn_exp2f(x);
           }
+          if (at + 2 == spot) {
+            asm volatile("" : "+v"(x));
+            R.l[col] += x;
+            y[t][col][0].b[j] = (__bf16)x;
+          }
+        }
         if (HIDE) {
 #pragma unroll
           for (int e = 0; e < 16 * N; ++e)
