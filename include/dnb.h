@@ -600,7 +600,9 @@ typedef struct {
  * h / (heads / kv_heads).  A query that sees no key has out 0 and lse -inf.  Rows of no sequence are neither read nor written.
  *   q, out (rows_q, heads, head_dim) of the type, out dense; lse (heads, rows_q) fp32, or null.
  * Roundings, and infinities and NaN in what is seen, as for dnb_attn_forward.  In DNB_BF16 infinities and NaN in values that a causal mask
- * hides from a query may reach it as NaN, as there; what lies past a sequence's length never does.
+ * hides from a query may reach it as NaN, as there; what lies past a sequence's length never does.  DNB_BF16: a block of up to
+ * 256 rows whose scores rise by more than about 40 above the largest of its first 32 keys, or whose sums are not finite, is
+ * done twice and takes some three times as long.
  * Workspace: 16-byte aligned; nothing in it lasts from one call to the next. */
 typedef struct dnb_paged_attn dnb_paged_attn; /* opaque, host side only */
 typedef struct {
@@ -660,10 +662,11 @@ int dnb_op_paged_copy(void* pool, int64_t pages, int64_t page_bytes, int64_t pla
 /* Who has which pages, on the host: every page is counted by the sequences that have it.  One thread at a time.
  *   extend    gives sequence `s` room for `tokens` more.  A last page that is not full and is shared is replaced by a copy.
  *             DNB_E_NOMEM: not that many free pages; nothing has changed then.
- *   fork      sequence `to`, which must be empty, gets what `from` has: the same pages.
+ *   fork      sequence `to`, which must be empty, gets what `from` has: the same pages.  What `from` has room for must have
+ *             been written by then (or be written on the stream before anything of `to` is).
  *   truncate  leaves the first `length` tokens; 0 frees the sequence.
  *   compact   moves the pages in use to the lowest numbers.  Pages whose content a copy that has not been taken yet needs
- *             stay: taken, a second call moves on.
+ *             stay, and are not free: when the copies have been taken, a second call moves on.
  *   copies    takes the copies that extend and compact have asked for since the last call, as pairs for dnb_op_paged_copy (in
  *             one call, before anything new is written to the pages).  *count: how many there are; DNB_E_RANGE if they are
  *             more than `capacity`, and they stay.  pairs null with capacity 0: how many there are.
