@@ -5,7 +5,7 @@ import math
 import pytest
 import torch
 
-from paged_util import Cache, offsets
+from paged_util import Cache, ints, offsets
 from seq_util import DTYPES, assert_within, attn_forward
 from test_gpu_paged_attn import check, run
 
@@ -120,3 +120,49 @@ def test_on_another_stream_than_the_tensors(dnb):
     with torch.cuda.stream(side):
         again, _ = run(dnb, cache, q, [1, 30], 4, stream=side)
     assert torch.equal(first, again)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("nq", [1, 20, 90, 400])
+def test_pages_not_of_the_pool_in_long_sequences(dnb, dtype, nq):
+    """Zeros, in steps among others whose pages are all there, and in the first and the last."""
+    cache = Cache([2100], 16, 1, 128, DTYPES[dtype])
+    q = torch.randn(nq, 4, 128, generator=torch.Generator().manual_seed(7)).to(DTYPES[dtype])
+    table, k, v = cache.table.copy(), cache.k.clone(), cache.v.clone()
+    for page, at in ((-1, 0), (cache.pages, 9), (2 ** 31 - 1, 40), (-2 ** 31, 41), (cache.pages + 7, 100), (-5, 131)):
+        table[0, at] = page
+        k[16 * at:16 * at + 16], v[16 * at:16 * at + 16] = 0, 0
+    out, lse = run(dnb, cache, q.cuda(), [nq], 4, table=ints(table))
+    want, lwant, tol, ltol = attn_forward(q, k, v, [0, nq], [0, 2100], None, True)
+    assert_within(out, want, tol, "out")
+    assert_within(lse, lwant, ltol, "lse")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("gap", [0, 2 ** 26])
+@pytest.mark.parametrize("nq", [1, 150])
+def test_rows_far_apart(dnb, dtype, gap, nq):
+    """A pool of which the same row of all pages lies together, also with more than 2^26 elements from row to row."""
+    page, kv, dim, keys = 4, 2, 32, 390
+    pages = 100
+    row = pages * kv * dim + gap
+    pools = [torch.zeros((page - 1) * row + pages * kv * dim, dtype=DTYPES[dtype], device="cuda") for _ in range(2)]
+    gen = torch.Generator().manual_seed(8)
+    k, v = (torch.randn(keys, kv, dim, generator=gen).to(DTYPES[dtype]) for _ in range(2))
+    order = torch.randperm(pages, generator=gen)
+    for t, pool in zip((k, v), pools):
+        for r in range(page):
+            rows = t[r::page]
+            pool[r * row:r * row + pages * kv * dim].view(pages, kv, dim)[order[:len(rows)].cuda()] = rows.cuda()
+    layout = dnb.dnb_paged_layout(pages, page, kv, dim, 1, 98, dtype=dnb.DNB_BF16 if dtype == "bf16" else dnb.DNB_F32, page_stride=kv * dim,
+                                  row_stride=row, head_stride=dim)
+    q = torch.randn(nq, 4, dim, generator=gen).to(DTYPES[dtype])
+    plan = dnb.dnb_paged_attn_create(layout, 4, nq)
+    ws = torch.empty(dnb.dnb_paged_attn_workspace_bytes(plan), dtype=torch.uint8, device="cuda")
+    out, lse = torch.zeros(nq, 4, dim, dtype=DTYPES[dtype], device="cuda"), torch.zeros(4, nq, device="cuda")
+    dnb.dnb_paged_attn_forward(plan, q.cuda(), *pools, ints([0, nq]), ints([keys]), ints(order[:98].numpy()), out, lse, ws)
+    torch.cuda.synchronize()
+    dnb.dnb_paged_attn_destroy(plan)
+    want, lwant, tol, ltol = attn_forward(q, k, v, [0, nq], [0, keys], None, True)
+    assert_within(out, want, tol, "out")
+    assert_within(lse, lwant, ltol, "lse")
