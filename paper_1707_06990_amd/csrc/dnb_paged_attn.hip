@@ -9,8 +9,8 @@
 // units lie on one line, in units of their cost, which is cut into equal parts, one a workgroup.  A block that several
 // workgroups share leaves its sums, not yet divided, in the workspace, and k_paged_join adds them.
 //
-// What bounds it, at 32 heads over 8 of 128 in bf16 with pages of 16: single tokens the reading of the cache (22 of them over 80091
-// keys, 328 MB: 72 us, 4.5 TB/s; of a large copy 5.05), chunks of prompts the issue of products and exponentials by the one wave a SIMD
+// What bounds it, at 32 heads over 8 of 128 in bf16 with pages of 16: single tokens the reading of the cache (21 of them over 78039
+// keys, 320 MB: 72 us, 4.4 TB/s; of a large copy 5.05), chunks of prompts the issue of products and exponentials by the one wave a SIMD
 // (4 x 1024 over 8192 keys: 527 us, 930 TFLOP/s; a large product 1321), a lone token over 777 keys latency alone: 11 us of the first
 // kernel's 13 are finding its part, the queries and the first keys, one after another, and 4 the join.  In fp32 six products of bf16
 // parts stand for one (16 heads over 4 of 64, 4 x 1024 over 4096 keys: 408 us, 147 of 220 TFLOP/s): two workgroups a CU, 488 us with one.
@@ -1126,7 +1126,7 @@ int dnb_paged_attn_create(const dnb_paged_attn_desc* desc, dnb_paged_attn** out)
   else p->max_rows = M <= 64 ? 64 : 128;
   // Measured at 16 to 32 heads of 64 and 128, in units of about a thousand cycles: a step, and what a block's beginning and end take (queries,
   // first keys, masked steps, results), for one, two and four sets of rows side by side.  An end that counts too little leaves
-  // the workgroups with many short blocks behind: chunks of mixed lengths 690 us with 10 for 40, 505 with 40; 22 single tokens 107 us
+  // the workgroups with many short blocks behind: chunks of mixed lengths 690 us with 10 for 40, 505 with 40; 21 single tokens 107 us
   // with 1 for 8, 97 with 2, 72 with 8, 79 with 40.
   const int cost[3] = {5, 5, 8}, extra_bf[3] = {8, 12, 40}, extra_f[3] = {2, 3, 4};
   for (int i = 0; i < 3; ++i) { p->cost[i] = cost[i]; p->extra[i] = bf16 ? extra_bf[i] : extra_f[i]; }
