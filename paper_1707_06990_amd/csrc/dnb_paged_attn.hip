@@ -336,11 +336,14 @@ struct Fetch {
     place(A);
     look(A, base + WINDOW, nk);
   }
+  // `from` comes out of v_readlane, and a memory instruction must not take its address from scalar registers within five wait states of a
+  // vector instruction that writes them: one for s_mov, four for s_nop 3 (the compiler does not count for instructions that it
+  // does not know).  m0 needs one.
   static __device__ __forceinline__ void load(lds_t to, uint32_t voff, uint64_t from) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(voff), "s"(from) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(voff), "s"(from) : "memory", "m0");
   }
   static __device__ __forceinline__ void load(lds_t to, const char* from) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(from) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(from) : "memory", "m0");
   }
   // Whether all rows of a step (of this window) are there, with as many pieces as a tile's, in groups within a page and with
   // offsets of 32 bits.  The same for all waves.
