@@ -543,7 +543,7 @@ __device__ __forceinline__ X apart(X x) {
   if (is_whole<F>) asm volatile("" : "+v"(x));
   return x;
 }
-// v of any of the workgroup's WAVES waves, through kFlags bytes of LDS at `at`
+// v of any of the workgroup's WAVES waves, through kFlags bytes of LDS at `at`; v is the same in all of a wave
 constexpr int kFlags = 64;
 template <int WAVES>
 __device__ __forceinline__ bool any_wave(lds_t at, bool v) {

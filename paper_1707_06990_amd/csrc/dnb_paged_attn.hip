@@ -590,7 +590,7 @@ struct Walk<__bf16, DB> {
     }
   }
   // Sums that scores far above the first block's have made large, so large that parts of a row could not be added, or that
-  // are not finite.
+  // are not finite, in any of the wave's rows.
   template <int N>
   static __device__ __forceinline__ bool odd(const Sets<DB, N>& R) {
     bool b = false;
@@ -603,7 +603,7 @@ struct Walk<__bf16, DB> {
         for (int i = 0; i < 16; ++i) most = fmaxf(most, fabsf(R.o[n][db][i]));
       b = b | !(R.l[n] < 0x1p64f) | (most > 0x1p100f) | not_finite(R.o[n]);
     }
-    return b;
+    return __any(b);
   }
 
   // The KH waves of a set of rows join, and the results go where they belong.  Each wave's sums go to LDS, a row after
