@@ -575,7 +575,8 @@ int dnb_clip_run(const dnb_clip* plan, const void* table, float max_norm, float*
  * of page table[s][j / page_size]; row r of page p, head g is at p * page_stride + r * row_stride + g * head_stride
  * elements.  (Tokens first: row_stride kv_heads * head_dim, head_stride head_dim, which is what 0 for all three means.
  * Heads first: head_stride page_size * row_stride, row_stride head_dim.  A page_stride of two pages lets keys and values
- * lie by turns.)  Keys and values have the same layout.
+ * lie by turns.)  Any order of the three will do in which no two rows share memory: by size, each stride must reach past all that
+ * the smaller ones reach (else DNB_E_RANGE).  Keys and values have the same layout.
  *   table      (sequences, max_pages) int32 on the device; entries past a sequence's length are not read
  *   k_lengths  `sequences` int32 on the device: tokens that each has in the cache, those of this call among them
  *   q_offsets  sequences + 1 int32 on the device, not decreasing: sequence s has the rows q_offsets[s] .. q_offsets[s+1] - 1

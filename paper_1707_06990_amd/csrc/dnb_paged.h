@@ -3,6 +3,8 @@
 
 #include <stdint.h>
 
+#include <utility>
+
 #include "../../include/dnb.h"
 
 namespace dnb {
@@ -25,6 +27,18 @@ inline int check_layout(const dnb_paged_layout& in, dnb_paged_layout* out) {
   for (const int64_t s : {c.page_stride, c.row_stride, c.head_stride})
     if (s % vec != 0 || s > (1 << 30)) return DNB_E_RANGE;
   if (c.row_stride < c.head_dim || c.head_stride < c.head_dim) return DNB_E_RANGE;
+  // No two of (page, row, head) may share memory, in whichever order they lie: by stride, each is at least as long as all below it.
+  struct Way {
+    int64_t stride, count;
+  } ways[3] = {{c.page_stride, c.pages}, {c.row_stride, c.page_size}, {c.head_stride, c.kv_heads}};
+  for (const int i : {0, 1, 0})
+    if (ways[i].stride > ways[i + 1].stride) std::swap(ways[i], ways[i + 1]);
+  int64_t extent = c.head_dim;
+  for (const Way& w : ways) {
+    if (w.count <= 1) continue;
+    if (w.stride < extent) return DNB_E_RANGE;
+    extent += (w.count - 1) * w.stride;
+  }
   *out = c;
   return DNB_OK;
 }

@@ -271,3 +271,43 @@ def test_a_fork_and_its_copy(dnb):
     dnb.dnb_pages_extend(p, 0, 13)
     assert status(lambda: dnb.dnb_pages_extend(p, 2, 20)) == -7
     dnb.dnb_pages_destroy(p)
+
+
+OVERLAPS = [dict(row_stride=64, head_stride=1024),   # heads first, the page's stride forgotten
+            dict(page_stride=8), dict(row_stride=64), dict(head_stride=128), dict(page_stride=2040), dict(page_stride=64, row_stride=6400),
+            dict(page_stride=16 * 1024, row_stride=64, head_stride=1016), dict(page_stride=1024, row_stride=64, head_stride=50 * 1024),
+            dict(page_size=1, row_stride=64)]   # page p + 1 begins 64 on, where page p's second head lies
+APART = [dict(page_stride=2048, row_stride=64, head_stride=1024), dict(page_stride=4096), dict(row_stride=256), dict(row_stride=200, head_stride=72),
+         dict(page_stride=128, row_stride=12800, head_stride=64), dict(page_stride=64, row_stride=6400, head_stride=102400),
+         dict(page_stride=4096 - 128, row_stride=256),   # rows of keys and of values by turns, pages as close as they go
+         dict(pages=1, page_stride=8), dict(page_size=1, page_stride=128, row_stride=64), dict(kv_heads=1, head_stride=4096)]
+
+
+@pytest.mark.parametrize("kw", OVERLAPS)
+def test_pages_that_lie_in_one_another_are_refused(dnb, kw):
+    """By the plan and by what writes to them."""
+    cache = dnb.dnb_paged_layout(**{**LAYOUT, **kw})
+    assert status(lambda: dnb.dnb_paged_attn_create(cache, 8, 50)) == -6
+    p = [4096 * (i + 1) for i in range(13)]
+    assert status(lambda: dnb.dnb_op_paged_append(dnb.dnb_qk_layout(**QK), cache, *p, stream=0)) == -6
+
+
+@pytest.mark.parametrize("kw", APART)
+def test_pages_in_any_order_of_strides(dnb, kw):
+    dnb.dnb_paged_attn_destroy(dnb.dnb_paged_attn_create(dnb.dnb_paged_layout(**{**LAYOUT, **kw}), 8, 50))
+
+
+def test_no_two_rows_of_what_is_taken_share_memory(dnb):
+    rng, taken = random.Random(3), 0
+    for _ in range(3000):
+        pages, page, kv, dim = rng.choice([1, 2, 3, 5]), rng.choice([1, 2, 4]), rng.choice([1, 2, 3]), 8
+        strides = [8 * rng.choice([1, 2, 3, 4, 6, 8, 9, 12, 15, 24]) for _ in range(3)]
+        cache = dnb.dnb_paged_layout(pages, page, kv, dim, 1, 4, page_stride=strides[0], row_stride=strides[1], head_stride=strides[2])
+        try:
+            dnb.dnb_paged_attn_destroy(dnb.dnb_paged_attn_create(cache, kv, 5))
+        except dnb.DnbError:
+            continue
+        taken += 1
+        at = [p * strides[0] + r * strides[1] + h * strides[2] for p in range(pages) for r in range(page) for h in range(kv)]
+        assert all(b - a >= dim for a, b in zip(sorted(at), sorted(at)[1:])), (pages, page, kv, strides)
+    assert taken > 300
