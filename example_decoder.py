@@ -161,14 +161,17 @@ class PagedCache:
         self.layout = dnb.dnb_paged_layout(pages, page_size, m.kv_heads, m.dim, requests, self.columns, dtype=m.code)
         self.pool = torch.empty(2, pages, page_size, m.kv_heads * m.dim, dtype=m.dtype, device="cuda")
         self.books = dnb.dnb_pages_create(pages, page_size, requests, self.columns)
-        self.plans = {}
+        self.workspace = torch.empty(0, dtype=torch.uint8, device="cuda")
 
-    def plan(self, rows):
-        if rows not in self.plans:
-            m = self.m
-            plan = dnb.dnb_paged_attn_create(self.layout, m.heads, rows, q_stride=(m.heads + 2 * m.kv_heads) * m.dim)
-            self.plans[rows] = plan, torch.empty(dnb.dnb_paged_attn_workspace_bytes(plan), dtype=torch.uint8, device="cuda")
-        return self.plans[rows]
+    def attend(self, q, offsets, lengths, table, out):
+        """A plan for as many rows as there are, which is a few numbers on the host; one workspace for all, as large as the largest."""
+        m = self.m
+        plan = dnb.dnb_paged_attn_create(self.layout, m.heads, q.shape[0], q_stride=q.stride(0))
+        need = dnb.dnb_paged_attn_workspace_bytes(plan)
+        if need > len(self.workspace):
+            self.workspace = torch.empty(need, dtype=torch.uint8, device="cuda")
+        dnb.dnb_paged_attn_forward(plan, q, *self.pool, offsets, lengths, table, out, None, self.workspace)
+        dnb.dnb_paged_attn_destroy(plan)
 
     def moved(self):
         """Does what copying the books ask for."""
@@ -202,8 +205,7 @@ class PagedCache:
                                v_stride=qkv.shape[1], q_out_stride=qkv.shape[1])
         dnb.dnb_op_paged_append(qk, self.layout, q, k, v, None, None, None, m.turns, offsets, lengths, table, q, *self.pool)
         out = torch.empty(rows, m.heads * m.dim, dtype=m.dtype, device="cuda")
-        plan, workspace = self.plan(rows)
-        dnb.dnb_paged_attn_forward(plan, q, *self.pool, offsets, lengths, table, out, None, workspace)
+        self.attend(q, offsets, lengths, table, out)
         last = torch.tensor([e - 1 for e, t in zip(ends[1:], texts) if len(t)], dtype=torch.long, device="cuda")
         return m.product(m.norms(m.product(out[last], m.p["out"]), x[last])[1], m.p["head"]).float()
 
@@ -221,8 +223,6 @@ class PagedCache:
         return dnb.dnb_pages_free_count(self.books)
 
     def close(self):
-        for plan, _ in self.plans.values():
-            dnb.dnb_paged_attn_destroy(plan)
         dnb.dnb_pages_destroy(self.books)
 
 
