@@ -744,9 +744,15 @@ def dnb_op_paged_copy(pool, pages, page_bytes, planes, plane_stride, pairs, coun
     _check(_lib.dnb_op_paged_copy(_ptr(pool), pages, page_bytes, planes, plane_stride, _ptr(pairs), count, _stream(stream)))
 
 
+class _Pages(_vp):
+    """A dnb_pages with the sizes of its table, for which dnb_pages_table makes room."""
+    shape = None
+
+
 def dnb_pages_create(pages, page_size, sequences, max_pages):
-    out = _vp()
+    out = _Pages()
     _check(_lib.dnb_pages_create(pages, page_size, sequences, max_pages, C.byref(out)))
+    out.shape = sequences, max_pages
     return out
 
 
@@ -786,8 +792,10 @@ def dnb_pages_copies(p):
 
 
 def dnb_pages_table(p, sequences, max_pages):
-    """(table, lengths) as numpy arrays of int32, to be copied to the device; the sizes are those that p was made with."""
+    """(table, lengths) as numpy arrays of int32, to be copied to the device; the sizes are those that p was made with (else DNB_E_RANGE)."""
     import numpy as np
+    if p and (sequences, max_pages) != p.shape:
+        raise DnbError(DNB_E_RANGE)
     table, lengths = np.empty((sequences, max_pages), dtype=np.int32), np.empty(sequences, dtype=np.int32)
     _check(_lib.dnb_pages_table(p, table.ctypes.data, lengths.ctypes.data))
     return table, lengths

@@ -311,3 +311,13 @@ def test_no_two_rows_of_what_is_taken_share_memory(dnb):
         at = [p * strides[0] + r * strides[1] + h * strides[2] for p in range(pages) for r in range(page) for h in range(kv)]
         assert all(b - a >= dim for a, b in zip(sorted(at), sorted(at)[1:])), (pages, page, kv, strides)
     assert taken > 300
+
+
+def test_a_table_of_other_sizes_is_refused(dnb):
+    """The call writes as many entries as the books have, whatever room it is given."""
+    p = dnb.dnb_pages_create(10, 4, 3, 5)
+    for sizes in ((2, 5), (3, 4), (4, 5), (3, 6), (5, 3), (0, 0)):
+        assert status(lambda: dnb.dnb_pages_table(p, *sizes)) == -6, sizes
+    table, lengths = dnb.dnb_pages_table(p, 3, 5)
+    assert table.shape == (3, 5) and lengths.shape == (3,)
+    dnb.dnb_pages_destroy(p)
