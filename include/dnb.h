@@ -487,7 +487,8 @@ int dnb_op_maxpool3s2_backward(const void* dout, const void* pos, void* din, int
  * as arithmetic makes it.  In DNB_BF16, and where few rows have long keys, it may also reach as NaN those
  * of the same sequence that a causal mask keeps from it (a hidden weight is 0, and 0 times infinity is
  * NaN); in DNB_F32 else it does not.  DNB_F32: work with results that are not finite is done twice and
- * takes about five times as long. */
+ * takes about five times as long.  Scores, scale q . k, are fp32 in units of log 2: rows with scores of more
+ * than 1e9 in magnitude may come out as 0, infinite or NaN. */
 typedef struct dnb_attn dnb_attn; /* opaque, host side only */
 typedef struct {
   int32_t heads, kv_heads;  /* heads a multiple of kv_heads                                      */
@@ -600,10 +601,10 @@ typedef struct {
  * over all j, or with `causal` over j <= i + nk - nq (the last query sees the last key).  Head h reads key/value head
  * h / (heads / kv_heads).  A query that sees no key has out 0 and lse -inf.  Rows of no sequence are neither read nor written.
  *   q, out (rows_q, heads, head_dim) of the type, out dense; lse (heads, rows_q) fp32, or null.
- * Roundings, and infinities and NaN in what is seen, as for dnb_attn_forward.  In DNB_BF16 infinities and NaN in values that a causal mask
- * hides from a query may reach it as NaN, as there; what lies past a sequence's length never does.  DNB_BF16: a block of up to
- * 256 rows whose scores rise by more than about 40 above the largest of its first 32 keys, or whose sums are not finite, is
- * done twice and takes some three times as long.
+ * Roundings, the range of scores, and infinities and NaN in what is seen, as for dnb_attn_forward.  In DNB_BF16 infinities and NaN in values that a causal mask
+ * hides from a query may reach it as NaN, as there; what lies past a sequence's length never does.  DNB_BF16: where scores of a row rise
+ * by more than about 40 above the largest of the first 32 keys that a wave takes of it, or sums are very large or not finite, a
+ * workgroup does its part of the block of up to 256 rows twice; where all do, a call takes 1.5 (single tokens) to 2.5 times as long.
  * Workspace: 16-byte aligned; nothing in it lasts from one call to the next. */
 typedef struct dnb_paged_attn dnb_paged_attn; /* opaque, host side only */
 typedef struct {
@@ -623,6 +624,8 @@ int dnb_paged_attn_forward(const dnb_paged_attn* plan, const void* q, const void
 /* Queries and keys of a block, before the attention: every head's norm and its rotation in one pass,
  *   n = x / sqrt(mean(x^2) + eps) * w        y = n turned as by dnb_op_rope_forward (turns, positions, order, factor)
  * w_q, w_k (head_dim fp32; any may be null: those heads are not normed).  rotary_dim 0: nothing is turned (turns and positions may be null).
+ * Squares and their sums are fp32: heads of values from 1.1e18 (at head_dim 256) or 6e18 (at 8) on leave its range and become 0, their
+ * gradients 0 or NaN.
  * backward: from q and k as they were, the gradients of both outputs, gives dq, dk, dw_q (if w_q) and dw_k (if w_k); sums
  * over rows in an order that does not change.  scratch: dnb_op_qk_rope_scratch_bytes, 16-byte aligned.
  * An output may be its own input's memory (y of x, dx of dy, with equal strides). */

@@ -24,7 +24,7 @@ constexpr int kThreads = 256;
 constexpr int kMaxAngles = 1024;  // (row, pair) angles of a workgroup in LDS
 constexpr int kMaxRows = 64;      // rows of a workgroup at a time
 constexpr unsigned kAcross = 1u << 22;
-constexpr int kGroups = 1024;     // workgroups of the backward pass, each of which leaves sums (step of 16381 rows 195 us; 1536: 211, 2048: 199)
+constexpr int kGroups = 1024;     // workgroups of the backward pass, each of which leaves sums (step of 16381 rows 190 us; 1536: 205, 2048: 193)
 
 // One of queries, keys, values.
 struct Part {

@@ -73,3 +73,22 @@ def test_rotation_of_more_rows_than_2_22_workgroups(dnb):
         # half a step of bf16 of the result, and some 40 of fp32 of the terms on either side
         tol = want.abs() * 2.0 ** -8 + part.abs().sum(1, keepdim=True) * 80 * 2.0 ** -24
         assert bool(((y[a:a + (1 << 24)].float() - want).abs() <= tol).all()), a
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("dim,most", [(256, 1.1e18), (8, 6e18)])
+def test_norms_up_to_the_range_of_their_sums(dnb, dtype, dim, most):
+    """A head of equal magnitudes comes out as the weight with its signs; one whose sum of squares is infinite as 0."""
+    dt = DTYPES[dtype]
+    gen = torch.Generator().manual_seed(3)
+    sign = torch.randint(0, 2, (40, 3, dim), generator=gen) * 2 - 1
+    w = (torch.rand(dim, generator=gen) + 0.5)
+    for size, factor in ((most, 1.0), (3e19, 0.0)):
+        x = (sign * size).to(dt).cuda()
+        y = torch.full_like(x, 9.0)
+        code = dnb.DNB_BF16 if dtype == "bf16" else dnb.DNB_F32
+        dnb.dnb_op_qk_rope_forward(dnb.dnb_qk_layout(40, 3, 0, dim, 0, dtype=code), x, None, w.cuda(), None, None, None, y, None)
+        want = (sign * w * factor).double()
+        # the sum of 256 squares and the root, the type's rounding (all of a head are rounded alike)
+        tol = want.abs() * (torch.finfo(dt).eps / 2 + 300 * 2.0 ** -24)
+        assert bool(((y.cpu().double() - want).abs() <= tol).all()), size
