@@ -336,11 +336,13 @@ struct Fetch {
     place(A);
     look(A, base + WINDOW, nk);
   }
-  // `from` comes out of v_readlane, and a memory instruction must not take its address from scalar registers within five wait states of a
-  // vector instruction that writes them: one for s_mov, four for s_nop 3 (the compiler does not count for instructions that it
-  // does not know).  m0 needs one.
-  static __device__ __forceinline__ void load(lds_t to, uint32_t voff, uint64_t from) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(voff), "s"(from) : "memory", "m0");
+  // A group of keys and its values.  `from` comes out of v_readlane, and a memory instruction must not take its address from scalar
+  // registers within five wait states of a vector instruction that writes them: one for s_mov, four for s_nop 3 (the compiler does not
+  // count for instructions that it does not know).  m0 needs one.  Both loads in one block, so that the second has waited too (four
+  // chunks 440 us; 449 with the wait before each).
+  static __device__ __forceinline__ void load(lds_t kt, lds_t vt, uint32_t voff, uint64_t k, uint64_t v) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tglobal_load_lds_dwordx4 %2, %3\n\ts_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %2, %4"
+                 ::"s"(__builtin_amdgcn_readfirstlane(kt)), "s"(__builtin_amdgcn_readfirstlane(vt)), "v"(voff), "s"(k), "s"(v) : "memory", "m0");
   }
   static __device__ __forceinline__ void load(lds_t to, const char* from) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" ::"s"(__builtin_amdgcn_readfirstlane(to)), "v"(from) : "memory", "m0");
@@ -356,8 +358,7 @@ struct Fetch {
     const uint64_t f = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(from >> 32), i) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)from, i);
     uint32_t c = c16 ^ (uint32_t)(L::swz(u * RPI) * 16);
     if (L::CH < L::PC) c = min(c, (uint32_t)(L::CH - 1) * 16);  // (pieces past a row's are not read)
-    load(kt + u * 1024, row_at + c, f);
-    load(vt + u * 1024, row_at + c, f + apart_by);
+    load(kt + u * 1024, vt + u * 1024, row_at + c, f, f + apart_by);
   }
   // Step `step` into the tiles at kt and vt; nk: keys that exist.
   __device__ __forceinline__ void issue(const PArgs& A, lds_t kt, lds_t vt, int step, unsigned nk) const {
