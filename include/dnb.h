@@ -601,10 +601,11 @@ typedef struct {
  * over all j, or with `causal` over j <= i + nk - nq (the last query sees the last key).  Head h reads key/value head
  * h / (heads / kv_heads).  A query that sees no key has out 0 and lse -inf.  Rows of no sequence are neither read nor written.
  *   q, out (rows_q, heads, head_dim) of the type, out dense; lse (heads, rows_q) fp32, or null.
- * Roundings, the range of scores, and infinities and NaN in what is seen, as for dnb_attn_forward.  In DNB_BF16 infinities and NaN in values that a causal mask
- * hides from a query may reach it as NaN, as there; what lies past a sequence's length never does.  DNB_BF16: where scores of a row rise
- * by more than about 40 above the largest of the first 32 keys that a wave takes of it, or sums are very large or not finite, a
- * workgroup does its part of the block of up to 256 rows twice; where all do, a call takes 1.5 (single tokens) to 2.5 times as long.
+ * Roundings, the range of scores, and infinities and NaN in what is seen, as for dnb_attn_forward.  In DNB_BF16 infinities and
+ * NaN in values that a causal mask hides from a query may reach it as NaN, as there; what lies past a sequence's length never
+ * does.  DNB_BF16: where scores of a row rise by more than about 40 above the largest of the first 32 keys that a wave takes of
+ * it, or sums are very large or not finite, a workgroup does its part of the block of up to 256 rows twice; where all do, a call
+ * takes 1.5 (single tokens) to 2.5 times as long.
  * Workspace: 16-byte aligned; nothing in it lasts from one call to the next. */
 typedef struct dnb_paged_attn dnb_paged_attn; /* opaque, host side only */
 typedef struct {

@@ -11,8 +11,8 @@
 //
 // What bounds it, at 32 heads over 8 of 128 in bf16 with pages of 16: single tokens the reading of the cache (21 of them over 78039
 // keys, 320 MB: 72 us, 4.4 TB/s; of a large copy 5.05), chunks of prompts the issue of products and exponentials by the one wave a SIMD
-// (4 x 1024 over 8192 keys: 515 to 563 us on different cards, 1001 to 915 TFLOP/s; a large product 1321), a lone token over 777 keys latency alone: 11 us of the first
-// kernel's 13 are finding its part, the queries and the first keys, one after another, and 4 the join.  In fp32 six products of bf16
+// (4 x 1024 over 8192 keys: 515 to 563 us on different cards, 1001 to 915 TFLOP/s; a large product 1321), a lone token over 777 keys
+// latency alone: 11 us of the first kernel's 13 are finding its part, the queries and the first keys, one after another, and 4 the join.  In fp32 six products of bf16
 // parts stand for one (16 heads over 4 of 64, 4 x 1024 over 4096 keys: 408 us, 147 of 220 TFLOP/s): two workgroups a CU, 488 us with one.
 #include <hip/hip_runtime.h>
 
@@ -681,8 +681,8 @@ struct Walk<__bf16, DB> {
     return L::at(4 * (l >> 5) + ((l >> 2) & 3), 2 * ((l >> 4) & 1) + ((l >> 1) & 1)) + (l & 1) * 8;
   }
   // The steps with a running maximum, for scores that leave the first block's far behind, and sums that are not finite: one after
-  // another, all four waves together.  Where nearly every part has to, 4 x 1024 over 8192 keys take 1225 us for 563, the 21 single
-  // tokens 120 for 66, 64 over 1024 keys each 81 for 53 (inputs in the caches).
+  // another, all four waves together.  Where nearly every part has to, 4 x 1024 over 8192 keys take 1213 us for 539, 21 single
+  // tokens over 78039 keys 127 for 72, 64 over 1024 keys each 95 for 64.
   template <int N>
   static __device__ __forceinline__ void again(const PArgs& A, F& f, lds_t kt, lds_t vt, int g, int first, int last, unsigned all, int nb, int kh,
                                                const Queries<N>& q, const unsigned (&sees)[N], Sets<DB, N>& R) {
